@@ -2,7 +2,7 @@
 
 Argument marshalling only: every step runs in the HIP kernels of the shared library.  PyTorch is
 used for device memory and streams.  The functions mirror the C ABI in include/silenzio_pbs.h
-one to one.  There is no CPU fallback: if the library is missing and cannot be built, importing
+one to one; those of include/silenzio_clear.h are in clear.py.  There is no CPU fallback: if the library is missing and cannot be built, importing
 a function raises.
 """
 from __future__ import annotations
@@ -45,7 +45,10 @@ EXPORTS = ("slz_ctx_create", "slz_ctx_destroy", "slz_ctx_set_option", "slz_lut_e
            "slz_shift2msbs_luts", "slz_shift2msbs_workspace", "slz_shift2msbs_plus", "slz_shift2msbs_pm",
            "slz_bivariate_workspace", "slz_bivariate_lookup", "slz_loss_luts", "slz_loss_workspace", "slz_int_ce_loss_deriv",
            "slz_weight_update_luts", "slz_weight_update",
-           "slz_matmul_highres_luts", "slz_matmul_highres_workspace", "slz_matmul_highres")
+           "slz_matmul_highres_luts", "slz_matmul_highres_workspace", "slz_matmul_highres",
+           "slz_quantize_i8", "slz_matmul_i8_workspace", "slz_matmul_i8", "slz_linear_i8_workspace", "slz_linear_i8",
+           "slz_matmul_i8_grad_workspace", "slz_matmul_i8_grad", "slz_linear_ce_workspace", "slz_linear_ce",
+           "slz_linear_ce_grad_workspace", "slz_linear_ce_grad", "slz_orthogonalize_workspace", "slz_orthogonalize")
 
 
 def lib():
@@ -98,6 +101,8 @@ def lib():
         L.slz_int_ce_loss_deriv.argtypes = [vp, ctypes.POINTER(SlzLossShape), vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.slz_weight_update_luts.argtypes = [ctypes.POINTER(SlzParams), u32, vp]
         L.slz_weight_update.argtypes = [vp, u32, vp, vp, vp, vp, vp, vp, u32, vp, sz, vp]
+        from . import clear
+        clear.declare(L)
         L.slz_strerror.argtypes = [ctypes.c_int]
         L.slz_strerror.restype = ctypes.c_char_p
         for name in EXPORTS:
@@ -579,3 +584,6 @@ class Context:
         _check(lib().slz_lwe_lincomb_batch(self._h, _dev_u64(cts, "cts"), w.data_ptr(), _dev_u64(out, "out"), G, J, O,
                                            _stream()), "slz_lwe_lincomb_batch")
         return out
+
+
+from .clear import quantize_i8, matmul_i8, linear_i8, matmul_i8_grad, linear_ce, linear_ce_grad, orthogonalize  # noqa: E402,F401

@@ -1,0 +1,112 @@
+// Declarations shared by the sources of include/silenzio_clear.h: element types, argument checks, operands of the matrix product.
+#pragma once
+#include "slz_internal.h"
+#include "slz_gadget_util.h"
+#include "../../include/silenzio_clear.h"
+
+__host__ __device__ static inline uint32_t slz_type_bytes(int type) { return type == SLZ_F32 ? 4 : 2; }
+static inline bool slz_type_ok(int type) { return type == SLZ_F32 || type == SLZ_BF16 || type == SLZ_F16; }
+
+// longest row distance in elements: 256 rows stay below 2^31 bytes, the reach of a buffer descriptor's offsets
+#define SLZ_CLEAR_MAX_LD ((int64_t)1 << 22)
+#define SLZ_CLEAR_MAX_LEN 0x7fffffffu
+
+// SLZ_OK, or what is wrong with a matrix of rows x cols elements
+static inline int slz_matrix_check(const void *p, uint32_t rows, uint32_t cols, int64_t ld, uint32_t bytes) {
+    if (rows > SLZ_CLEAR_MAX_LEN || cols > SLZ_CLEAR_MAX_LEN) return SLZ_E_TOO_LARGE;
+    if (ld < (int64_t)cols) return SLZ_E_INVALID_ARG;
+    if (rows == 0 || cols == 0) return SLZ_OK;
+    if (!p || ((uintptr_t)p % bytes)) return SLZ_E_INVALID_ARG;
+    return ld > SLZ_CLEAR_MAX_LD ? SLZ_E_TOO_LARGE : SLZ_OK;
+}
+static inline bool slz_in_place(const void *p, uint32_t cols, int64_t ld, uint32_t bytes) {
+    return !(((uintptr_t)p | ((uint64_t)cols * bytes) | ((uint64_t)ld * bytes)) & 15u);
+}
+
+static inline bool slz_ws_ok(const void *ws, size_t have, size_t need) { return need == 0 || (ws && have >= need && !((uintptr_t)ws & 255u)); }
+
+#ifdef __HIPCC__
+__device__ __forceinline__ float slz_bf16_to_f32(uint16_t b) { return __builtin_bit_cast(float, (uint32_t)b << 16); }
+__device__ __forceinline__ uint16_t slz_f32_to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+__device__ __forceinline__ float slz_f16_to_f32(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
+__device__ __forceinline__ uint16_t slz_f32_to_f16(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
+
+__device__ __forceinline__ float slz_get(const void *p, int type, size_t i) {
+    if (type == SLZ_F32) return ((const float *)p)[i];
+    const uint16_t b = ((const uint16_t *)p)[i];
+    return type == SLZ_BF16 ? slz_bf16_to_f32(b) : slz_f16_to_f32(b);
+}
+__device__ __forceinline__ uint16_t slz_half(float x, int type) { return type == SLZ_BF16 ? slz_f32_to_bf16(x) : slz_f32_to_f16(x); }
+__device__ __forceinline__ void slz_put(void *p, int type, size_t i, float x) {
+    if (type == SLZ_F32) ((float *)p)[i] = x;
+    else ((uint16_t *)p)[i] = slz_half(x, type);
+}
+// A 32-bit number as three bf16 whose sum it is: its leading 8 bits, the next 8, the last 8 (cut off, so none of them overflows).
+// An infinity or NaN is all in the first.
+__device__ __forceinline__ void slz_split3(float x, uint16_t (&q)[3]) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    if ((u & 0x7f800000u) == 0x7f800000u) {
+        q[0] = (uint16_t)(u >> 16) | ((u & 0x7fffffu) ? 0x40u : 0u);
+        q[1] = q[2] = 0;
+        return;
+    }
+    const float h = __builtin_bit_cast(float, u & 0xffff0000u), r = x - h;
+    const float l = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, r) & 0xffff0000u);
+    q[0] = (uint16_t)(u >> 16);
+    q[1] = (uint16_t)(__builtin_bit_cast(uint32_t, l) >> 16);
+    q[2] = (uint16_t)(__builtin_bit_cast(uint32_t, r - l) >> 16);
+}
+// C consecutive values v of one row at p[0 .. C), of which `valid` exist; aligned: p is a multiple of C elements
+template <int C> __device__ __forceinline__ void slz_put_run(void *p, int type, const float (&v)[C], uint32_t valid, bool aligned) {
+    static_assert(C % 4 == 0, "");
+    if (valid >= C && aligned) {
+        if (type == SLZ_F32) {
+#pragma unroll
+            for (int i = 0; i < C; i += 4) *(float4 *)((float *)p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+        } else {
+            uint32_t w[C / 2];
+#pragma unroll
+            for (int i = 0; i < C / 2; i++) w[i] = slz_half(v[2 * i], type) | ((uint32_t)slz_half(v[2 * i + 1], type) << 16);
+            if constexpr (C % 8 == 0) {
+#pragma unroll
+                for (int i = 0; i < C / 2; i += 4) *(uint4 *)((uint32_t *)p + i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < C / 2; i += 2) *(uint2 *)((uint32_t *)p + i) = make_uint2(w[i], w[i + 1]);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < C; i++)
+        if ((uint32_t)i < valid) slz_put(p, type, i, v[i]);
+}
+// sum and maximum over a wave, the same bits in every lane
+__device__ __forceinline__ float slz_wave_sum(float x) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
+    return x;
+}
+__device__ __forceinline__ float slz_wave_max(float x) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
+    return x;
+}
+#endif
+
+// ---- operands of the matrix product (slz_clear_common.hip) ---------------------------------------------------------------------
+// A matrix as the product takes it: 16-byte aligned rows of bf16, f16 or int8, one or three pieces `piece` bytes apart
+struct slz_operand {
+    const char *p;
+    int64_t ld, piece;               // bytes
+    uint32_t pieces;
+    int element;                     // SLZ_BF16, SLZ_F16, or 3 for int8
+};
+// bytes of workspace for laying out rows x cols of `type` (0 when it can be read in place)
+size_t slz_operand_bytes(const void *p, int type, uint32_t rows, uint32_t cols, int64_t ld);
+// and the operand; ws: that many bytes
+slz_operand slz_operand_of(const void *p, int type, uint32_t rows, uint32_t cols, int64_t ld, char *ws, hipStream_t s);
+size_t slz_operand_i8_bytes(const int8_t *p, uint32_t rows, uint32_t cols, int64_t ld);
+slz_operand slz_operand_i8_of(const int8_t *p, uint32_t rows, uint32_t cols, int64_t ld, char *ws, hipStream_t s);
+// *unit: the power of two at or above the largest magnitude of `count` values; what f16 could not hold is divided by it
+void slz_unit_of(const float *values, uint32_t count, float *unit, hipStream_t s);

@@ -1,0 +1,283 @@
+// Softmax cross entropy of a linear layer's outputs z = h w^T over a large vocabulary, and its gradient, without keeping z
+// (include/silenzio_clear.h).
+//
+// Forward: the tiled product; from a tile's z in its registers each row's maximum and sum of exp(z - maximum) go to memory, one
+// pair per tile row, and the label's z; a second kernel joins a token's pairs.
+// Gradient: in pieces of the vocabulary, z again, from it g = (exp(z - lse) - [v = label]) dloss to the workspace, then the two products
+// dw = g^T h (complete for the piece's rows) and dh += g w (summed over the pieces in 32 bits).
+#include "slz_gemm.h"
+
+// a piece's g takes this much at most (at least 1024 words of the vocabulary)
+#define CE_PIECE_BYTES ((size_t)256 << 20)
+// f16: g is held times this; |g| <= |dloss|, so that the largest stay finite and those from 2^-28 of the largest keep 11 bits
+#define CE_F16_UP 16384.0f
+
+struct ce_lse_epi {
+    float2 *pairs;                   // [tile][tokens]: maximum, sum
+    float *label_z;
+    const int64_t *labels;
+    uint32_t first_word, first_tile;
+    template <int MI, int NI, bool RUN, int WM, int WN, class ACC>
+    __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *lds) const {
+        static_assert(RUN, "");
+        const uint32_t n0 = slz_col<NI, RUN>(at, 0);
+        float2 *mine = (float2 *)lds + at.wave_n * (WM * MI * 16);
+#pragma unroll
+        for (int i = 0; i < MI; i++) {
+            const uint32_t m = slz_row(at, i);
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int c = 0; c < NI * 4; c++) top = n0 + c < p.N ? fmaxf(top, acc[i][c / 4][c % 4]) : top;
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            // a row whose z here are all -inf adds nothing
+            const float from = top == -__builtin_inff() ? 0.0f : top;
+            float sum = 0.0f;
+#pragma unroll
+            for (int c = 0; c < NI * 4; c++) sum += n0 + c < p.N ? __expf(acc[i][c / 4][c % 4] - from) : 0.0f;
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            if (m < p.M) {
+                const int64_t word = labels[m] - first_word - n0;
+                if (word >= 0 && word < NI * 4 && n0 + word < p.N) {
+                    float z = 0.0f;
+#pragma unroll
+                    for (int c = 0; c < NI * 4; c++) z = word == c ? acc[i][c / 4][c % 4] : z;
+                    label_z[m] = z;
+                }
+            }
+            if (at.lane < 16) mine[at.wave_m * (MI * 16) + i * 16 + at.lane] = make_float2(top, sum);
+        }
+        __syncthreads();
+        const uint32_t m0 = at.tile_m * (WM * MI * 16);
+        for (uint32_t r = threadIdx.x; r < WM * MI * 16; r += WM * WN * 64) {
+            if (m0 + r >= p.M) continue;
+            float2 all = ((const float2 *)lds)[r];
+#pragma unroll
+            for (int w = 1; w < WN; w++) {
+                const float2 o = ((const float2 *)lds)[w * (WM * MI * 16) + r];
+                const float top = fmaxf(all.x, o.x), from = top == -__builtin_inff() ? 0.0f : top;
+                all = make_float2(top, all.y * __expf(all.x - from) + o.y * __expf(o.x - from));
+            }
+            pairs[(size_t)(first_tile + at.tile_n) * p.M + m0 + r] = all;
+        }
+    }
+};
+
+// 64 tokens per workgroup, its waves take the tiles in turn
+#define CE_JOIN_WAVES 8
+__global__ void __launch_bounds__(CE_JOIN_WAVES * 64)
+k_ce_join(const float2 *__restrict__ pairs, const float *__restrict__ label_z, const int64_t *__restrict__ labels, float *__restrict__ loss,
+          float *__restrict__ lse, uint32_t tokens, uint32_t tiles, uint32_t vocab, int64_t ignore) {
+    __shared__ float2 part[CE_JOIN_WAVES][64];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, t = blockIdx.x * 64 + lane;
+    float top = -__builtin_inff(), sum = 0.0f;
+    if (t < tokens)
+        for (uint32_t i = wave; i < tiles; i += CE_JOIN_WAVES) {
+            const float2 o = pairs[(size_t)i * tokens + t];
+            const float next = fmaxf(top, o.x), from = next == -__builtin_inff() ? 0.0f : next;
+            sum = sum * expf(top - from) + o.y * expf(o.x - from);
+            top = next;
+        }
+    part[wave][lane] = make_float2(top, sum);
+    __syncthreads();
+    if (wave != 0 || t >= tokens) return;
+    for (int w = 1; w < CE_JOIN_WAVES; w++) {
+        const float2 o = part[w][lane];
+        const float next = fmaxf(top, o.x), from = next == -__builtin_inff() ? 0.0f : next;
+        sum = sum * expf(top - from) + o.y * expf(o.x - from);
+        top = next;
+    }
+    const float l = top + logf(sum);
+    const int64_t label = labels[t];
+    lse[t] = l;
+    loss[t] = label == ignore ? 0.0f : label < 0 || label >= (int64_t)vocab ? __builtin_nanf("") : l - label_z[t];
+}
+
+// g of a piece: [pieces][tokens][ld], columns from N to the next multiple of 8 zero
+struct ce_grad_epi {
+    char *g;
+    int64_t ld, piece;               // bytes
+    int type;
+    const float *lse, *dloss, *unit;
+    const int64_t *labels;
+    int64_t ignore;
+    uint32_t first_word, vocab;
+    template <int MI, int NI, bool RUN, int WM, int WN, class ACC>
+    __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *) const {
+        static_assert(RUN && NI % 2 == 0, "");
+        const uint32_t n0 = slz_col<NI, RUN>(at, 0), wide = (p.N + 7u) & ~7u;
+        const float up = type == SLZ_F16 ? CE_F16_UP / *unit : 1.0f;
+#pragma unroll
+        for (int i = 0; i < MI; i++) {
+            const uint32_t m = slz_row(at, i);
+            if (m >= p.M) continue;
+            const int64_t label = labels[m];
+            const bool counts = label != ignore;
+            const float by = label < 0 || label >= (int64_t)vocab ? __builtin_nanf("") : dloss[m] * up, l = lse[m];
+            const int64_t word = label - first_word - n0;
+#pragma unroll
+            for (int q = 0; q < NI / 2; q++) {
+                const uint32_t n = n0 + q * 8u;
+                if (n >= wide) continue;
+                float v[8];
+#pragma unroll
+                for (int c = 0; c < 8; c++) {
+                    const float z = acc[i][q * 2 + c / 4][c % 4], e = type == SLZ_F32 ? expf(z - l) : __expf(z - l);
+                    v[c] = counts && n + c < p.N ? (e - (word == q * 8 + c ? 1.0f : 0.0f)) * by : 0.0f;
+                }
+                char *to = g + (int64_t)m * ld + (int64_t)n * 2;
+                if (type == SLZ_F32) {
+                    uint32_t w[3][4];
+#pragma unroll
+                    for (int c = 0; c < 8; c += 2) {
+                        uint16_t x[3], y[3];
+                        slz_split3(v[c], x);
+                        slz_split3(v[c + 1], y);
+                        for (int k = 0; k < 3; k++) w[k][c / 2] = x[k] | ((uint32_t)y[k] << 16);
+                    }
+                    for (int k = 0; k < 3; k++) *(uint4 *)(to + k * piece) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+                } else slz_put_run<8>(to, type, v, 8, true);
+            }
+        }
+    }
+};
+
+struct ce_plan {
+    uint32_t words;                  // of a piece
+    uint32_t tiles;                  // forward: of the whole vocabulary
+    size_t h, w, pairs, label_z, g, dh, unit, total;
+    uint32_t g_row, dh_ld;
+};
+using ce_tiles = slz_tiles_128;
+
+static ce_plan plan_ce(const slz_ce_shape *sh, const void *h, const void *w, bool grad) {
+    ce_plan P = {};
+    const size_t pieces = sh->type == SLZ_F32 ? 3 : 1;
+    const bool w_there = slz_operand_bytes(w, sh->type, 1, sh->inner, sh->ld_w) == 0;
+    size_t words = sh->vocab;
+    if (grad) words = words < CE_PIECE_BYTES / (2 * pieces * (sh->tokens + 1)) ? words : CE_PIECE_BYTES / (2 * pieces * (sh->tokens + 1));
+    if (!w_there) words = words < CE_PIECE_BYTES / (2 * pieces * sh->inner) ? words : CE_PIECE_BYTES / (2 * pieces * sh->inner);
+    if (words < sh->vocab) words = words < 1024 ? 1024 : words & ~(size_t)255;
+    P.words = (uint32_t)(words < sh->vocab ? words : sh->vocab);
+    size_t o = 0;
+    P.h = o; o += slz_operand_bytes(h, sh->type, sh->tokens, sh->inner, sh->ld_h);
+    P.w = o; o += slz_operand_bytes(w, sh->type, P.words, sh->inner, sh->ld_w);
+    if (!grad) {
+        P.tiles = (sh->vocab / P.words) * ((P.words + ce_tiles::TN - 1) / ce_tiles::TN) + (sh->vocab % P.words + ce_tiles::TN - 1) / ce_tiles::TN;
+        P.pairs = o; o += up256((size_t)P.tiles * sh->tokens * 8);
+        P.label_z = o; o += up256((size_t)sh->tokens * 4);
+    } else {
+        P.g_row = (uint32_t)(((size_t)P.words * 2 + 127) / 128 * 128);
+        P.g = o; o += pieces * up256((size_t)sh->tokens * P.g_row);
+        P.dh_ld = (sh->inner + 15) / 16 * 16;
+        P.dh = o; o += P.words < sh->vocab ? up256((size_t)sh->tokens * P.dh_ld * 4) : 0;
+        P.unit = o; o += 256;
+    }
+    P.total = o;
+    return P;
+}
+
+static int ce_check(const slz_ce_shape *sh, const void *h, const void *w, const int64_t *labels) {
+    if (!sh || !slz_type_ok(sh->type) || sh->inner == 0 || sh->vocab == 0) return SLZ_E_INVALID_ARG;
+    const uint32_t eb = slz_type_bytes(sh->type);
+    int rc = slz_matrix_check(h, sh->tokens, sh->inner, sh->ld_h, eb);
+    if (rc == SLZ_OK) rc = slz_matrix_check(w, sh->vocab, sh->inner, sh->ld_w, eb);
+    if (rc == SLZ_OK) rc = slz_matrix_check(labels, sh->tokens, 1, 1, 8);
+    return rc;
+}
+static int ce_workspace(const slz_ce_shape *sh, const void *h, const void *w, bool grad, size_t *bytes) {
+    if (!sh || !bytes || !slz_type_ok(sh->type) || sh->inner == 0 || sh->vocab == 0) return SLZ_E_INVALID_ARG;
+    if (sh->tokens > SLZ_CLEAR_MAX_LEN || sh->vocab > SLZ_CLEAR_MAX_LEN || sh->inner > SLZ_CLEAR_MAX_LD) return SLZ_E_TOO_LARGE;
+    *bytes = plan_ce(sh, h, w, grad).total;
+    return SLZ_OK;
+}
+extern "C" int slz_linear_ce_workspace(const slz_ce_shape *sh, const void *h, const void *w, size_t *bytes) { return ce_workspace(sh, h, w, false, bytes); }
+extern "C" int slz_linear_ce_grad_workspace(const slz_ce_shape *sh, const void *h, const void *w, size_t *bytes) {
+    return ce_workspace(sh, h, w, true, bytes);
+}
+
+template <class EPI> static int ce_logits(int type, const slz_gemm &p, const EPI &epi, hipStream_t s) {
+    return type == SLZ_F16 ? slz_gemm_launch<ce_tiles, SLZ_EL_F16, false, false>(p, epi, 1, s) : slz_gemm_launch<ce_tiles, SLZ_EL_BF16, false, false>(p, epi, 1, s);
+}
+static const char *rows_of(const void *w, const slz_ce_shape *sh, uint32_t first) {
+    return (const char *)w + (int64_t)first * sh->ld_w * slz_type_bytes(sh->type);
+}
+
+extern "C" int slz_linear_ce(const slz_ce_shape *sh, const void *h, const void *w, const int64_t *labels, float *loss, float *lse, void *ws,
+                             size_t ws_bytes, void *stream) {
+    int rc = ce_check(sh, h, w, labels);
+    if (rc == SLZ_OK) rc = slz_matrix_check(loss, sh->tokens, 1, 1, 4);
+    if (rc == SLZ_OK) rc = slz_matrix_check(lse, sh->tokens, 1, 1, 4);
+    if (rc != SLZ_OK || sh->tokens == 0) return rc;
+    const ce_plan P = plan_ce(sh, h, w, false);
+    if (!slz_ws_ok(ws, ws_bytes, P.total)) return SLZ_E_INVALID_ARG;
+    hipStream_t s = (hipStream_t)stream;
+    char *base = (char *)ws;
+    float2 *pairs = (float2 *)(base + P.pairs);
+    float *label_z = (float *)(base + P.label_z);
+    const slz_operand oh = slz_operand_of(h, sh->type, sh->tokens, sh->inner, sh->ld_h, base + P.h, s);
+    uint32_t tile = 0;
+    for (uint32_t v = 0; v < sh->vocab; v += P.words) {
+        const uint32_t words = sh->vocab - v < P.words ? sh->vocab - v : P.words;
+        const slz_operand ow = slz_operand_of(rows_of(w, sh, v), sh->type, words, sh->inner, sh->ld_w, base + P.w, s);
+        const ce_lse_epi epi{pairs, label_z, labels, v, tile};
+        rc = ce_logits(sh->type, slz_gemm_of(oh, ow, sh->tokens, words, sh->inner), epi, s);
+        if (rc != SLZ_OK) return rc;
+        tile += (words + ce_tiles::TN - 1) / ce_tiles::TN;
+    }
+    hipLaunchKernelGGL(k_ce_join, dim3((sh->tokens + 63) / 64), dim3(CE_JOIN_WAVES * 64), 0, s, pairs, label_z, labels, loss, lse, sh->tokens, tile,
+                       sh->vocab, sh->ignore_index);
+    SLZ_HIP(hipGetLastError());
+    return SLZ_OK;
+}
+
+template <int EL> static int ce_products(const slz_ce_shape *sh, const ce_plan &P, const slz_operand &g, const slz_operand &oh, const slz_operand &ow,
+                                         uint32_t first, uint32_t words, void *dh, void *dw, float *dh_sum, const slz_times_unit &f, hipStream_t s) {
+    const uint32_t eb = slz_type_bytes(sh->type);
+    char *dw_rows = (char *)dw + (int64_t)first * sh->ld_dw * eb;
+    const slz_store_epi<slz_times_unit> to_dw{dw_rows, sh->type, sh->ld_dw, 0, slz_in_place(dw_rows, 16, sh->ld_dw, eb), f};
+    int rc = slz_gemm_launch<slz_tiles_128, EL, true, true>(slz_gemm_of(g, oh, words, sh->inner, sh->tokens), to_dw, 1, s);
+    if (rc != SLZ_OK) return rc;
+    const slz_gemm p = slz_gemm_of(g, ow, sh->tokens, sh->inner, words);
+    if (P.words == sh->vocab) {
+        const slz_store_epi<slz_times_unit> to_dh{dh, sh->type, sh->ld_dh, 0, slz_in_place(dh, 16, sh->ld_dh, eb), f};
+        return slz_gemm_launch<slz_tiles_128, EL, false, true>(p, to_dh, 1, s);
+    }
+    const slz_partial_epi<float> to_sum{dh_sum, P.dh_ld, 1, first != 0};
+    return slz_gemm_launch<slz_tiles_128, EL, false, true>(p, to_sum, 1, s);
+}
+
+extern "C" int slz_linear_ce_grad(const slz_ce_shape *sh, const void *h, const void *w, const int64_t *labels, const float *lse, const float *dloss,
+                                  void *dh, void *dw, void *ws, size_t ws_bytes, void *stream) {
+    int rc = ce_check(sh, h, w, labels);
+    if (rc == SLZ_OK) rc = slz_matrix_check(lse, sh->tokens, 1, 1, 4);
+    if (rc == SLZ_OK) rc = slz_matrix_check(dloss, sh->tokens, 1, 1, 4);
+    if (rc == SLZ_OK) rc = slz_matrix_check(dh, sh->tokens, sh->inner, sh->ld_dh, slz_type_bytes(sh->type));
+    if (rc == SLZ_OK) rc = slz_matrix_check(dw, sh->vocab, sh->inner, sh->ld_dw, slz_type_bytes(sh->type));
+    if (rc != SLZ_OK) return rc;
+    const ce_plan P = plan_ce(sh, h, w, true);
+    if (!slz_ws_ok(ws, ws_bytes, P.total)) return SLZ_E_INVALID_ARG;
+    hipStream_t s = (hipStream_t)stream;
+    char *base = (char *)ws;
+    float *dh_sum = (float *)(base + P.dh), *unit = (float *)(base + P.unit);
+    if (sh->type == SLZ_F16) slz_unit_of(dloss, sh->tokens, unit, s);
+    const slz_times_unit f{sh->type == SLZ_F16 ? unit : nullptr, 1.0f / CE_F16_UP};
+    const slz_operand oh = slz_operand_of(h, sh->type, sh->tokens, sh->inner, sh->ld_h, base + P.h, s);
+    const slz_operand g{base + P.g, (int64_t)P.g_row, (int64_t)up256((size_t)sh->tokens * P.g_row), oh.pieces, oh.element};
+    for (uint32_t v = 0; v < sh->vocab; v += P.words) {
+        const uint32_t words = sh->vocab - v < P.words ? sh->vocab - v : P.words;
+        const slz_operand ow = slz_operand_of(rows_of(w, sh, v), sh->type, words, sh->inner, sh->ld_w, base + P.w, s);
+        const ce_grad_epi epi{base + P.g, g.ld, g.piece, sh->type, lse, dloss, unit, labels, sh->ignore_index, v, sh->vocab};
+        rc = ce_logits(sh->type, slz_gemm_of(oh, ow, sh->tokens, words, sh->inner), epi, s);
+        if (rc == SLZ_OK)
+            rc = sh->type == SLZ_F16 ? ce_products<SLZ_EL_F16>(sh, P, g, oh, ow, v, words, dh, dw, dh_sum, f, s)
+                                     : ce_products<SLZ_EL_BF16>(sh, P, g, oh, ow, v, words, dh, dw, dh_sum, f, s);
+        if (rc != SLZ_OK) return rc;
+    }
+    if (P.words < sh->vocab && sh->tokens)
+        hipLaunchKernelGGL((k_join<float, slz_times_unit>), ew_grid((size_t)sh->tokens * ((sh->inner + 3) / 4)), dim3(256), 0, s, (const float *)dh_sum, 1u,
+                           sh->tokens, sh->inner, P.dh_ld, dh, sh->type, sh->ld_dh, f);
+    SLZ_HIP(hipGetLastError());
+    return SLZ_OK;
+}
