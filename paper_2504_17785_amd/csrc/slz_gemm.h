@@ -15,6 +15,8 @@
 // k, may read the next row; they only reach sums that no one stores.
 #pragma once
 #include "slz_clear.h"
+#include <type_traits>
+#include <utility>
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef int v4i32 __attribute__((ext_vector_type(4)));
@@ -138,9 +140,19 @@ __device__ __forceinline__ void slz_tile_of(uint32_t x, uint32_t tiles_m, uint32
     tn = in / rows;
 }
 
+// The order in which the compiler is to issue what stands before: so many reads of shared memory, then so many matrix instructions.
+template <int READS, int MATRIX> __device__ __forceinline__ void slz_order() {
+    if constexpr (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    if constexpr (MATRIX > 0) __builtin_amdgcn_sched_group_barrier(0x8, MATRIX, 0);
+}
+template <int MI, int NI, int A_LDS, int B_LDS, int... G> __device__ __forceinline__ void slz_order_groups(std::integer_sequence<int, G...>) {
+    (slz_order<(G + 2 < 2 * MI ? A_LDS : 0) + (G < MI ? B_LDS * ((G + 1) * NI / MI - G * NI / MI) : 0), NI>(), ...);
+}
+
 template <int EL, bool A_ROWS_K, bool B_ROWS_K, int TM, int TN, int WM, int WN, class EPI>
 __global__ void __launch_bounds__(WM *WN * 64) k_gemm(const slz_gemm p, const EPI epi) {
     constexpr int WAVES = WM * WN, MI = TM / WM / 16, NI = TN / WN / 16, ES = slz_el<EL>::bytes, KS = 128 / ES;
+    constexpr int A_LDS = A_ROWS_K ? 2 : 1, B_LDS = B_ROWS_K ? 2 : 1;           // instructions per operand
     using acc_t = typename slz_el<EL>::acc;
     using tile_a = slz_tile<A_ROWS_K, TM, WAVES, 0>;
     using tile_b = slz_tile<B_ROWS_K, TN, WAVES, B_ROWS_K ? 0 : NI * 4>;
@@ -187,18 +199,24 @@ __global__ void __launch_bounds__(WM *WN * 64) k_gemm(const slz_gemm p, const EP
         __syncthreads();                               // this step's pieces are there; everyone is done with the other buffer
         if (s + 1 < end) load_step(buffer ^ 1);
         const char *la = lds[buffer], *lb = la + tile_a::BYTES;
+        // 2 MI groups of NI matrix instructions, each with one operand of A; A's operands are read two groups ahead, B's for the
+        // second half during the first: shared memory and the matrix cores are busy for about as long, and so at the same time
+        v4i32 fa[3], fb[2][NI];
 #pragma unroll
-        for (int kk = 0; kk < 2; kk++) {
-            v4i32 fa[MI], fb[NI];
+        for (int j = 0; j < NI; j++) fb[0][j] = tb.template read<NI>(lb, wave_n * (NI * 16), j, 0, lane);
 #pragma unroll
-            for (int j = 0; j < NI; j++) fb[j] = tb.template read<NI>(lb, wave_n * (NI * 16), j, kk, lane);
+        for (int g = 0; g < 2; g++) fa[g] = ta.template read<MI>(la, wave_m * (MI * 16), g % MI, g / MI, lane);
+        slz_order<B_LDS * NI + A_LDS * 2, 0>();
 #pragma unroll
-            for (int i = 0; i < MI; i++) fa[i] = ta.template read<MI>(la, wave_m * (MI * 16), i, kk, lane);
+        for (int g = 0; g < 2 * MI; g++) {
+            if (g + 2 < 2 * MI) fa[(g + 2) % 3] = ta.template read<MI>(la, wave_m * (MI * 16), (g + 2) % MI, (g + 2) / MI, lane);
+            if (g < MI)
 #pragma unroll
-            for (int i = 0; i < MI; i++)
+                for (int j = g * NI / MI; j < (g + 1) * NI / MI; j++) fb[1][j] = tb.template read<NI>(lb, wave_n * (NI * 16), j, 1, lane);
 #pragma unroll
-                for (int j = 0; j < NI; j++) acc[i][j] = slz_mma<EL>(fb[j], fa[i], acc[i][j]);
+            for (int j = 0; j < NI; j++) acc[g % MI][j] = slz_mma<EL>(fb[g / MI][j], fa[g % 3], acc[g % MI][j]);
         }
+        slz_order_groups<MI, NI, A_LDS, B_LDS>(std::make_integer_sequence<int, 2 * MI>());
     }
     __syncthreads();                                   // the epilogue may use the shared memory
     const slz_place at{m0 + wave_m * (MI * 16), n0 + wave_n * (NI * 16), lane, wave_m, wave_n, tm, tn, batch, range};
@@ -286,6 +304,31 @@ __global__ void __launch_bounds__(256) k_join(const T *ws, uint32_t ranges, uint
 template <int TM_, int TN_, int WM_, int WN_> struct slz_tiling { static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_; };
 using slz_tiles_256 = slz_tiling<256, 256, 2, 4>;
 using slz_tiles_128 = slz_tiling<128, 128, 2, 2>;
+using slz_tiles_64 = slz_tiling<64, 64, 2, 2>;
+
+// Which tiling and how many ranges of k.  A step of 128 bytes of k takes a workgroup that has its compute unit to itself 1.6 (256 x 256), 0.7 (128)
+// and 0.33 us (64), and a full compute unit gives one every 1.6, 0.46 and 0.18 us: large tiles do 1.1 and 2.5 times the work of smaller
+// ones in the same time, small ones end sooner where there are few.  (8192^3 bf16: 1100, 1086, 645 TFLOP/s; 1024^3: 29, 14, 8 us.)  Ranges of k
+// cost a second launch that reads their sums.
+struct slz_choice { uint32_t side, split; };
+static inline slz_choice slz_choose(uint32_t M, uint32_t N, uint32_t steps, uint32_t batches, bool symmetric, uint32_t most_ranges) {
+    static const struct { uint32_t side; double alone, full; } kinds[3] = {{256, 1.6, 1.6}, {128, 0.7, 0.46}, {64, 0.33, 0.18}};
+    slz_choice best = {64, 1};
+    double least = 1e30;
+    for (const auto &k : kinds) {
+        const double tm = (M + k.side - 1) / k.side, tn = (N + k.side - 1) / k.side, tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batches;
+        for (uint32_t split = 1; split <= most_ranges && (split == 1 || steps >= 4 * split); split *= 2) {
+            const double rounds = (double)(uint64_t)((tiles * split + 255) / 256), step = rounds * k.full > k.alone ? rounds * k.full : k.alone;
+            double us = ((steps + split - 1) / split) * step;
+            if (split > 1) us += 4.0 + (double)M * N * batches * 4.0 * (split + 1) / 3e6;
+            if (us < least) { least = us; best = {k.side, split}; }
+        }
+    }
+    return best;
+}
+// workspace of the ranges' sums
+static inline uint32_t slz_ranges_ld(uint32_t N) { return (N + 15u) & ~15u; }
+static inline size_t slz_ranges_bytes(const slz_choice &c, uint32_t M, uint32_t N) { return c.split > 1 ? up256((size_t)c.split * M * slz_ranges_ld(N) * 4) : 0; }
 
 static inline slz_gemm slz_gemm_of(const slz_operand &a, const slz_operand &b, uint32_t M, uint32_t N, uint32_t K) {
     slz_gemm p = {};
@@ -310,12 +353,30 @@ template <class T, int EL, bool A_ROWS_K, bool B_ROWS_K, class EPI>
 static int slz_gemm_launch(slz_gemm p, const EPI &epi, uint32_t batches, hipStream_t s) {
     p.tiles_m = (p.M + T::TM - 1) / T::TM;
     p.tiles_n = (p.N + T::TN - 1) / T::TN;
-    const uint32_t steps = slz_gemm_steps(p, slz_el<EL>::bytes);
-    p.range = (steps + p.split - 1) / p.split;
+    p.range = (slz_gemm_steps(p, slz_el<EL>::bytes) + p.split - 1) / p.split;
     const uint64_t tiles = p.symmetric ? (uint64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (uint64_t)p.tiles_m * p.tiles_n;
     if (tiles == 0 || batches == 0) return SLZ_OK;
     if (tiles > 0x7fffffffu) return SLZ_E_TOO_LARGE;
     hipLaunchKernelGGL((k_gemm<EL, A_ROWS_K, B_ROWS_K, T::TM, T::TN, T::WM, T::WN, EPI>), dim3((uint32_t)tiles, p.split, batches),
                        dim3(T::WM * T::WN * 64), 0, s, p, epi);
+    return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
+}
+template <int EL, bool A_ROWS_K, bool B_ROWS_K, class EPI>
+static int slz_gemm_run(const slz_gemm &p, const EPI &epi, uint32_t side, uint32_t batches, hipStream_t s) {
+    if (side == 256) return slz_gemm_launch<slz_tiles_256, EL, A_ROWS_K, B_ROWS_K>(p, epi, batches, s);
+    if (side == 128) return slz_gemm_launch<slz_tiles_128, EL, A_ROWS_K, B_ROWS_K>(p, epi, batches, s);
+    return slz_gemm_launch<slz_tiles_64, EL, A_ROWS_K, B_ROWS_K>(p, epi, batches, s);
+}
+// out = f(sums): at once, or where the choice has several ranges of k by their sums in `ranges` (slz_ranges_bytes) and a second launch
+template <int EL, bool A_ROWS_K, bool B_ROWS_K, class F>
+static int slz_gemm_to(slz_gemm p, const slz_choice &c, const F &f, void *out, int type, int64_t ld, char *ranges, hipStream_t s) {
+    using sum_t = typename std::conditional<EL == SLZ_EL_I8, int, float>::type;
+    if (c.split == 1)
+        return slz_gemm_run<EL, A_ROWS_K, B_ROWS_K>(p, slz_store_epi<F>{out, type, ld, 0, slz_in_place(out, 16, ld, slz_type_bytes(type)), f}, c.side, 1, s);
+    p.split = c.split;
+    const uint32_t ld_r = slz_ranges_ld(p.N);
+    const int rc = slz_gemm_run<EL, A_ROWS_K, B_ROWS_K>(p, slz_partial_epi<sum_t>{(sum_t *)ranges, ld_r, 1, 0}, c.side, 1, s);
+    if (rc != SLZ_OK || p.M == 0 || p.N == 0) return rc;
+    hipLaunchKernelGGL((k_join<sum_t, F>), ew_grid((size_t)p.M * ((p.N + 3) / 4)), dim3(256), 0, s, (const sum_t *)ranges, c.split, p.M, p.N, ld_r, out, type, ld, f);
     return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
 }

@@ -61,17 +61,16 @@ static int i8_check(const slz_i8_shape *sh) {
     return SLZ_OK;
 }
 
-static int i8_product(const slz_i8_shape *sh, const slz_operand &a, const float *sa, const slz_operand &b, const float *sb, void *y, hipStream_t s) {
-    const slz_gemm p = slz_gemm_of(a, b, sh->m, sh->n, sh->k);
-    const slz_store_epi<scales_of> epi{y, sh->type, sh->ld_y, 0, slz_in_place(y, 16, sh->ld_y, slz_type_bytes(sh->type)), {sa, sb}};
-    return slz_gemm_launch<slz_tiles_128, SLZ_EL_I8, false, false>(p, epi, 1, s);
+static slz_choice i8_choice(const slz_i8_shape *sh) { return slz_choose(sh->m, sh->n, (sh->k + 127) / 128, 1, false, 16); }
+static int i8_product(const slz_i8_shape *sh, const slz_operand &a, const float *sa, const slz_operand &b, const float *sb, void *y, char *ranges, hipStream_t s) {
+    return slz_gemm_to<SLZ_EL_I8, false, false>(slz_gemm_of(a, b, sh->m, sh->n, sh->k), i8_choice(sh), scales_of{sa, sb}, y, sh->type, sh->ld_y, ranges, s);
 }
 
 extern "C" int slz_matmul_i8_workspace(const slz_i8_shape *sh, const int8_t *a, const int8_t *b, size_t *bytes) {
     const int rc = i8_check(sh);
     if (rc != SLZ_OK) return rc;
     if (!bytes) return SLZ_E_INVALID_ARG;
-    *bytes = slz_operand_i8_bytes(a, sh->m, sh->k, sh->ld_a) + slz_operand_i8_bytes(b, sh->n, sh->k, sh->ld_b);
+    *bytes = slz_operand_i8_bytes(a, sh->m, sh->k, sh->ld_a) + slz_operand_i8_bytes(b, sh->n, sh->k, sh->ld_b) + slz_ranges_bytes(i8_choice(sh), sh->m, sh->n);
     return SLZ_OK;
 }
 
@@ -90,25 +89,26 @@ extern "C" int slz_matmul_i8(const slz_i8_shape *sh, const int8_t *a, const floa
     if (rc == SLZ_OK) rc = slz_matrix_check(sa, sh->m, 1, 1, 4);
     if (rc != SLZ_OK || sh->m == 0 || sh->n == 0) return rc;
     const size_t for_a = slz_operand_i8_bytes(a, sh->m, sh->k, sh->ld_a), for_b = slz_operand_i8_bytes(b, sh->n, sh->k, sh->ld_b);
-    if (!slz_ws_ok(ws, ws_bytes, for_a + for_b)) return SLZ_E_INVALID_ARG;
+    if (!slz_ws_ok(ws, ws_bytes, for_a + for_b + slz_ranges_bytes(i8_choice(sh), sh->m, sh->n))) return SLZ_E_INVALID_ARG;
     hipStream_t s = (hipStream_t)stream;
     const slz_operand oa = slz_operand_i8_of(a, sh->m, sh->k, sh->ld_a, (char *)ws, s);
     const slz_operand ob = slz_operand_i8_of(b, sh->n, sh->k, sh->ld_b, (char *)ws + for_a, s);
-    rc = i8_product(sh, oa, sa, ob, sb, y, s);
+    rc = i8_product(sh, oa, sa, ob, sb, y, (char *)ws + for_a + for_b, s);
     if (rc != SLZ_OK) return rc;
     SLZ_HIP(hipGetLastError());
     return SLZ_OK;
 }
 
 // ---- a layer: quantised rows of x times the weights -----------------------------------------------------------------------------------
-struct linear_plan { size_t q, scale, b, total; int64_t ld_q; };
+struct linear_plan { size_t q, scale, b, ranges, total; int64_t ld_q; };
 static linear_plan plan_linear(const slz_i8_shape *sh, const int8_t *b) {
     linear_plan P;
     P.ld_q = ((int64_t)sh->k + 127) / 128 * 128;
     P.q = 0;
     P.scale = up256((size_t)sh->m * P.ld_q);
     P.b = P.scale + up256((size_t)sh->m * 4);
-    P.total = P.b + slz_operand_i8_bytes(b, sh->n, sh->k, sh->ld_b);
+    P.ranges = P.b + slz_operand_i8_bytes(b, sh->n, sh->k, sh->ld_b);
+    P.total = P.ranges + slz_ranges_bytes(i8_choice(sh), sh->m, sh->n);
     return P;
 }
 extern "C" int slz_linear_i8_workspace(const slz_i8_shape *sh, const void *x, const int8_t *b, size_t *bytes) {
@@ -132,7 +132,7 @@ extern "C" int slz_linear_i8(const slz_i8_shape *sh, const void *x, const int8_t
     if (rc != SLZ_OK) return rc;
     const slz_operand oa{(const char *)q, P.ld_q, 0, 1, 3};
     const slz_operand ob = slz_operand_i8_of(b, sh->n, sh->k, sh->ld_b, (char *)ws + P.b, s);
-    return i8_product(sh, oa, sa, ob, sb, y, s);
+    return i8_product(sh, oa, sa, ob, sb, y, (char *)ws + P.ranges, s);
 }
 
 // ---- gradient ------------------------------------------------------------------------------------------------------------------------------
@@ -165,7 +165,7 @@ k_values(const int8_t *__restrict__ q, const float *__restrict__ scale, const fl
     }
 }
 
-struct grad_plan { size_t dy, values[2], unit, total; uint32_t row; };
+struct grad_plan { size_t dy, values[2], unit, ranges, total; uint32_t row; slz_choice da, db; };
 static grad_plan plan_grad(const slz_i8_shape *sh, const void *dy) {
     grad_plan P;
     const size_t pieces = sh->type == SLZ_F32 ? 3 : 1;
@@ -174,7 +174,12 @@ static grad_plan plan_grad(const slz_i8_shape *sh, const void *dy) {
     P.values[0] = slz_operand_bytes(dy, sh->type, sh->m, sh->n, sh->ld_y);
     P.values[1] = P.values[0] + pieces * up256((size_t)sh->m * P.row);
     P.unit = P.values[1] + pieces * up256((size_t)sh->n * P.row);
-    P.total = P.unit + 256;
+    P.ranges = P.unit + 256;
+    const uint32_t pairs = sh->type == SLZ_F32 ? 6 : 1;
+    P.da = slz_choose(sh->m, sh->k, (sh->n + 63) / 64 * pairs, 1, false, 16);
+    P.db = slz_choose(sh->n, sh->k, (sh->m + 63) / 64 * pairs, 1, false, 16);
+    const size_t for_a = slz_ranges_bytes(P.da, sh->m, sh->k), for_b = slz_ranges_bytes(P.db, sh->n, sh->k);
+    P.total = P.ranges + (for_a > for_b ? for_a : for_b);
     return P;
 }
 extern "C" int slz_matmul_i8_grad_workspace(const slz_i8_shape *sh, const void *dy, size_t *bytes) {
@@ -187,17 +192,19 @@ extern "C" int slz_matmul_i8_grad_workspace(const slz_i8_shape *sh, const void *
 
 // out [M][k] = left times the values of q [rows][k]; left's rows are the sum's index where left_rows_k
 static int grad_product(const slz_i8_shape *sh, const slz_operand &left, bool left_rows_k, uint32_t M, const int8_t *q, int64_t ld_q, const float *scale,
-                        uint32_t rows, void *out, int64_t ld_out, char *values, float *unit, const grad_plan &P, hipStream_t s) {
+                        uint32_t rows, void *out, int64_t ld_out, char *values, float *unit, char *ranges, const grad_plan &P, hipStream_t s) {
     const int type = sh->type;
     const slz_operand right{values, (int64_t)P.row, (int64_t)up256((size_t)rows * P.row), left.pieces, left.element};
     if (type == SLZ_F16) slz_unit_of(scale, rows, unit, s);
     if (rows)
         hipLaunchKernelGGL(k_values, ew_grid((size_t)rows * P.row / 16), dim3(256), 0, s, q, scale, unit, type, rows, sh->k, ld_q, values, P.row, right.piece);
     const slz_gemm p = slz_gemm_of(left, right, M, sh->k, rows);
-    const slz_store_epi<slz_times_unit> epi{out, type, ld_out, 0, slz_in_place(out, 16, ld_out, slz_type_bytes(type)), {type == SLZ_F16 ? unit : nullptr, 1.0f}};
+    const slz_times_unit f{type == SLZ_F16 ? unit : nullptr, 1.0f};
     if (type == SLZ_F16)
-        return left_rows_k ? slz_gemm_launch<slz_tiles_128, SLZ_EL_F16, true, true>(p, epi, 1, s) : slz_gemm_launch<slz_tiles_128, SLZ_EL_F16, false, true>(p, epi, 1, s);
-    return left_rows_k ? slz_gemm_launch<slz_tiles_128, SLZ_EL_BF16, true, true>(p, epi, 1, s) : slz_gemm_launch<slz_tiles_128, SLZ_EL_BF16, false, true>(p, epi, 1, s);
+        return left_rows_k ? slz_gemm_to<SLZ_EL_F16, true, true>(p, P.db, f, out, type, ld_out, ranges, s)
+                           : slz_gemm_to<SLZ_EL_F16, false, true>(p, P.da, f, out, type, ld_out, ranges, s);
+    return left_rows_k ? slz_gemm_to<SLZ_EL_BF16, true, true>(p, P.db, f, out, type, ld_out, ranges, s)
+                       : slz_gemm_to<SLZ_EL_BF16, false, true>(p, P.da, f, out, type, ld_out, ranges, s);
 }
 
 extern "C" int slz_matmul_i8_grad(const slz_i8_shape *sh, const void *dy, const int8_t *a, const float *sa, const int8_t *b, const float *sb, void *da,
@@ -212,8 +219,8 @@ extern "C" int slz_matmul_i8_grad(const slz_i8_shape *sh, const void *dy, const 
     hipStream_t s = (hipStream_t)stream;
     char *w = (char *)ws;
     const slz_operand d = slz_operand_of(dy, sh->type, sh->m, sh->n, sh->ld_y, w + P.dy, s);
-    if (da && sh->m) rc = grad_product(sh, d, false, sh->m, b, sh->ld_b, sb, sh->n, da, ld_da, w + P.values[1], (float *)(w + P.unit), P, s);
-    if (rc == SLZ_OK && db && sh->n) rc = grad_product(sh, d, true, sh->n, a, sh->ld_a, sa, sh->m, db, ld_db, w + P.values[0], (float *)(w + P.unit) + 1, P, s);
+    if (da && sh->m) rc = grad_product(sh, d, false, sh->m, b, sh->ld_b, sb, sh->n, da, ld_da, w + P.values[1], (float *)(w + P.unit), w + P.ranges, P, s);
+    if (rc == SLZ_OK && db && sh->n) rc = grad_product(sh, d, true, sh->n, a, sh->ld_a, sa, sh->m, db, ld_db, w + P.values[0], (float *)(w + P.unit) + 1, w + P.ranges, P, s);
     if (rc != SLZ_OK) return rc;
     SLZ_HIP(hipGetLastError());
     return SLZ_OK;

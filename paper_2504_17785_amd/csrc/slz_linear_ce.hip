@@ -1,8 +1,8 @@
 // Softmax cross entropy of a linear layer's outputs z = h w^T over a large vocabulary, and its gradient, without keeping z
 // (include/silenzio_clear.h).
 //
-// Forward: the tiled product; from a tile's z in its registers each row's maximum and sum of exp(z - maximum) go to memory, one
-// pair per tile row, and the label's z; a second kernel joins a token's pairs.
+// Forward: the tiled product; from a tile's z in its registers the maximum and the sum of exp(z - maximum) of each 32 words go to memory, and
+// the label's z; a second kernel joins a token's pairs.
 // Gradient: in pieces of the vocabulary, z again, from it g = (exp(z - lse) - [v = label]) dloss to the workspace, then the two products
 // dw = g^T h (complete for the piece's rows) and dh += g w (summed over the pieces in 32 bits).
 #include "slz_gemm.h"
@@ -12,16 +12,23 @@
 // f16: g is held times this; |g| <= |dloss|, so that the largest stay finite and those from 2^-28 of the largest keep 11 bits
 #define CE_F16_UP 16384.0f
 
+// (maximum, sum of exp(z - maximum)) of two sets of z; a set whose z are all -inf has (-inf, 0) and adds nothing
+__device__ __forceinline__ float2 ce_both(float2 p, float2 q) {
+    const float top = fmaxf(p.x, q.x), from = top == -__builtin_inff() ? 0.0f : top;
+    return make_float2(top, p.y * expf(p.x - from) + q.y * expf(q.x - from));
+}
+
+// One pair for every 32 words, whatever the tiling: sums of eight, then of four such.  A token's loss so has the same bits alone and among others.
+#define CE_BLOCK 32
 struct ce_lse_epi {
-    float2 *pairs;                   // [tile][tokens]: maximum, sum
+    float2 *pairs;                   // [block of words][tokens]
     float *label_z;
     const int64_t *labels;
-    uint32_t first_word, first_tile;
+    uint32_t first_word;             // a multiple of CE_BLOCK
     template <int MI, int NI, bool RUN, int WM, int WN, class ACC>
-    __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *lds) const {
-        static_assert(RUN, "");
+    __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *) const {
+        static_assert(RUN && (NI == 2 || NI == 4), "a lane has 8 or 16 columns, four or two lanes a block");
         const uint32_t n0 = slz_col<NI, RUN>(at, 0);
-        float2 *mine = (float2 *)lds + at.wave_n * (WM * MI * 16);
 #pragma unroll
         for (int i = 0; i < MI; i++) {
             const uint32_t m = slz_row(at, i);
@@ -29,66 +36,53 @@ struct ce_lse_epi {
 #pragma unroll
             for (int c = 0; c < NI * 4; c++) top = n0 + c < p.N ? fmaxf(top, acc[i][c / 4][c % 4]) : top;
             top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            // a row whose z here are all -inf adds nothing
+            if (NI == 2) top = fmaxf(top, __shfl_xor(top, 32, 64));
             const float from = top == -__builtin_inff() ? 0.0f : top;
-            float sum = 0.0f;
+            float sums[NI / 2];
 #pragma unroll
-            for (int c = 0; c < NI * 4; c++) sum += n0 + c < p.N ? __expf(acc[i][c / 4][c % 4] - from) : 0.0f;
+            for (int h = 0; h < NI / 2; h++) {
+                sums[h] = 0.0f;
+#pragma unroll
+                for (int c = h * 8; c < h * 8 + 8; c++) sums[h] += n0 + c < p.N ? __expf(acc[i][c / 4][c % 4] - from) : 0.0f;
+            }
+            float sum = sums[0];
+            if (NI == 4) sum += sums[NI / 2 - 1];
             sum += __shfl_xor(sum, 16, 64);
-            sum += __shfl_xor(sum, 32, 64);
-            if (m < p.M) {
-                const int64_t word = labels[m] - first_word - n0;
-                if (word >= 0 && word < NI * 4 && n0 + word < p.N) {
-                    float z = 0.0f;
+            if (NI == 2) sum += __shfl_xor(sum, 32, 64);
+            if (m >= p.M || n0 >= p.N) continue;
+            const int64_t word = labels[m] - first_word - n0;
+            if (word >= 0 && word < NI * 4 && n0 + word < p.N) {
+                float z = 0.0f;
 #pragma unroll
-                    for (int c = 0; c < NI * 4; c++) z = word == c ? acc[i][c / 4][c % 4] : z;
-                    label_z[m] = z;
-                }
+                for (int c = 0; c < NI * 4; c++) z = word == c ? acc[i][c / 4][c % 4] : z;
+                label_z[m] = z;
             }
-            if (at.lane < 16) mine[at.wave_m * (MI * 16) + i * 16 + at.lane] = make_float2(top, sum);
-        }
-        __syncthreads();
-        const uint32_t m0 = at.tile_m * (WM * MI * 16);
-        for (uint32_t r = threadIdx.x; r < WM * MI * 16; r += WM * WN * 64) {
-            if (m0 + r >= p.M) continue;
-            float2 all = ((const float2 *)lds)[r];
-#pragma unroll
-            for (int w = 1; w < WN; w++) {
-                const float2 o = ((const float2 *)lds)[w * (WM * MI * 16) + r];
-                const float top = fmaxf(all.x, o.x), from = top == -__builtin_inff() ? 0.0f : top;
-                all = make_float2(top, all.y * __expf(all.x - from) + o.y * __expf(o.x - from));
-            }
-            pairs[(size_t)(first_tile + at.tile_n) * p.M + m0 + r] = all;
+            if (n0 % CE_BLOCK == 0) pairs[(size_t)((first_word + n0) / CE_BLOCK) * p.M + m] = make_float2(top, sum);
         }
     }
 };
 
-// 64 tokens per workgroup, its waves take the tiles in turn
-#define CE_JOIN_WAVES 8
-__global__ void __launch_bounds__(CE_JOIN_WAVES * 64)
+// 16 tokens per workgroup; each token's blocks go to 64 threads in turn, whose pairs are joined in a fixed order
+__global__ void __launch_bounds__(1024)
 k_ce_join(const float2 *__restrict__ pairs, const float *__restrict__ label_z, const int64_t *__restrict__ labels, float *__restrict__ loss,
-          float *__restrict__ lse, uint32_t tokens, uint32_t tiles, uint32_t vocab, int64_t ignore) {
-    __shared__ float2 part[CE_JOIN_WAVES][64];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, t = blockIdx.x * 64 + lane;
-    float top = -__builtin_inff(), sum = 0.0f;
+          float *__restrict__ lse, uint32_t tokens, uint32_t blocks, uint32_t vocab, int64_t ignore) {
+    __shared__ float2 part[64][16];
+    const uint32_t r = threadIdx.x & 15u, slice = threadIdx.x >> 4, t = blockIdx.x * 16 + r;
+    float2 all = make_float2(-__builtin_inff(), 0.0f);
     if (t < tokens)
-        for (uint32_t i = wave; i < tiles; i += CE_JOIN_WAVES) {
-            const float2 o = pairs[(size_t)i * tokens + t];
-            const float next = fmaxf(top, o.x), from = next == -__builtin_inff() ? 0.0f : next;
-            sum = sum * expf(top - from) + o.y * expf(o.x - from);
-            top = next;
+        for (uint32_t i = slice; i < blocks; i += 256) {
+            float2 four[4];
+#pragma unroll
+            for (int q = 0; q < 4; q++) four[q] = i + q * 64 < blocks ? pairs[(size_t)(i + q * 64) * tokens + t] : make_float2(-__builtin_inff(), 0.0f);
+            all = ce_both(all, ce_both(ce_both(four[0], four[1]), ce_both(four[2], four[3])));
         }
-    part[wave][lane] = make_float2(top, sum);
-    __syncthreads();
-    if (wave != 0 || t >= tokens) return;
-    for (int w = 1; w < CE_JOIN_WAVES; w++) {
-        const float2 o = part[w][lane];
-        const float next = fmaxf(top, o.x), from = next == -__builtin_inff() ? 0.0f : next;
-        sum = sum * expf(top - from) + o.y * expf(o.x - from);
-        top = next;
+    part[slice][r] = all;
+    for (uint32_t half = 32; half > 0; half >>= 1) {
+        __syncthreads();
+        if (slice < half) part[slice][r] = ce_both(part[slice][r], part[slice + half][r]);
     }
-    const float l = top + logf(sum);
+    if (slice != 0 || t >= tokens) return;
+    const float l = part[0][r].x + logf(part[0][r].y);
     const int64_t label = labels[t];
     lse[t] = l;
     loss[t] = label == ignore ? 0.0f : label < 0 || label >= (int64_t)vocab ? __builtin_nanf("") : l - label_z[t];
@@ -145,12 +139,11 @@ struct ce_grad_epi {
 
 struct ce_plan {
     uint32_t words;                  // of a piece
-    uint32_t tiles;                  // forward: of the whole vocabulary
     size_t h, w, pairs, label_z, g, dh, unit, total;
     uint32_t g_row, dh_ld;
+    uint32_t side;                   // of the tiles of z
+    slz_choice dh_choice, dw_choice;
 };
-using ce_tiles = slz_tiles_128;
-
 static ce_plan plan_ce(const slz_ce_shape *sh, const void *h, const void *w, bool grad) {
     ce_plan P = {};
     const size_t pieces = sh->type == SLZ_F32 ? 3 : 1;
@@ -160,18 +153,22 @@ static ce_plan plan_ce(const slz_ce_shape *sh, const void *h, const void *w, boo
     if (!w_there) words = words < CE_PIECE_BYTES / (2 * pieces * sh->inner) ? words : CE_PIECE_BYTES / (2 * pieces * sh->inner);
     if (words < sh->vocab) words = words < 1024 ? 1024 : words & ~(size_t)255;
     P.words = (uint32_t)(words < sh->vocab ? words : sh->vocab);
+    const uint32_t pairs = sh->type == SLZ_F32 ? 6 : 1;
+    P.side = slz_choose(sh->tokens, P.words, (sh->inner + 63) / 64 * pairs, 1, false, 1).side;
     size_t o = 0;
     P.h = o; o += slz_operand_bytes(h, sh->type, sh->tokens, sh->inner, sh->ld_h);
     P.w = o; o += slz_operand_bytes(w, sh->type, P.words, sh->inner, sh->ld_w);
     if (!grad) {
-        P.tiles = (sh->vocab / P.words) * ((P.words + ce_tiles::TN - 1) / ce_tiles::TN) + (sh->vocab % P.words + ce_tiles::TN - 1) / ce_tiles::TN;
-        P.pairs = o; o += up256((size_t)P.tiles * sh->tokens * 8);
+        P.pairs = o; o += up256(((size_t)sh->vocab + CE_BLOCK - 1) / CE_BLOCK * sh->tokens * 8);
         P.label_z = o; o += up256((size_t)sh->tokens * 4);
     } else {
         P.g_row = (uint32_t)(((size_t)P.words * 2 + 127) / 128 * 128);
         P.g = o; o += pieces * up256((size_t)sh->tokens * P.g_row);
-        P.dh_ld = (sh->inner + 15) / 16 * 16;
-        P.dh = o; o += P.words < sh->vocab ? up256((size_t)sh->tokens * P.dh_ld * 4) : 0;
+        P.dh_ld = slz_ranges_ld(sh->inner);
+        // dh: one launch over a piece, or its sums kept in ranges of the piece's words, to which each piece adds
+        P.dh_choice = slz_choose(sh->tokens, sh->inner, (P.words + 63) / 64 * pairs, 1, false, 64);
+        P.dw_choice = slz_choose(P.words, sh->inner, (sh->tokens + 63) / 64 * pairs, 1, false, 1);
+        P.dh = o; o += P.words < sh->vocab || P.dh_choice.split > 1 ? up256((size_t)P.dh_choice.split * sh->tokens * P.dh_ld * 4) : 0;
         P.unit = o; o += 256;
     }
     P.total = o;
@@ -197,8 +194,8 @@ extern "C" int slz_linear_ce_grad_workspace(const slz_ce_shape *sh, const void *
     return ce_workspace(sh, h, w, true, bytes);
 }
 
-template <class EPI> static int ce_logits(int type, const slz_gemm &p, const EPI &epi, hipStream_t s) {
-    return type == SLZ_F16 ? slz_gemm_launch<ce_tiles, SLZ_EL_F16, false, false>(p, epi, 1, s) : slz_gemm_launch<ce_tiles, SLZ_EL_BF16, false, false>(p, epi, 1, s);
+template <class EPI> static int ce_logits(int type, const slz_gemm &p, const EPI &epi, uint32_t side, hipStream_t s) {
+    return type == SLZ_F16 ? slz_gemm_run<SLZ_EL_F16, false, false>(p, epi, side, 1, s) : slz_gemm_run<SLZ_EL_BF16, false, false>(p, epi, side, 1, s);
 }
 static const char *rows_of(const void *w, const slz_ce_shape *sh, uint32_t first) {
     return (const char *)w + (int64_t)first * sh->ld_w * slz_type_bytes(sh->type);
@@ -217,16 +214,14 @@ extern "C" int slz_linear_ce(const slz_ce_shape *sh, const void *h, const void *
     float2 *pairs = (float2 *)(base + P.pairs);
     float *label_z = (float *)(base + P.label_z);
     const slz_operand oh = slz_operand_of(h, sh->type, sh->tokens, sh->inner, sh->ld_h, base + P.h, s);
-    uint32_t tile = 0;
     for (uint32_t v = 0; v < sh->vocab; v += P.words) {
         const uint32_t words = sh->vocab - v < P.words ? sh->vocab - v : P.words;
         const slz_operand ow = slz_operand_of(rows_of(w, sh, v), sh->type, words, sh->inner, sh->ld_w, base + P.w, s);
-        const ce_lse_epi epi{pairs, label_z, labels, v, tile};
-        rc = ce_logits(sh->type, slz_gemm_of(oh, ow, sh->tokens, words, sh->inner), epi, s);
+        const ce_lse_epi epi{pairs, label_z, labels, v};
+        rc = ce_logits(sh->type, slz_gemm_of(oh, ow, sh->tokens, words, sh->inner), epi, P.side, s);
         if (rc != SLZ_OK) return rc;
-        tile += (words + ce_tiles::TN - 1) / ce_tiles::TN;
     }
-    hipLaunchKernelGGL(k_ce_join, dim3((sh->tokens + 63) / 64), dim3(CE_JOIN_WAVES * 64), 0, s, pairs, label_z, labels, loss, lse, sh->tokens, tile,
+    hipLaunchKernelGGL(k_ce_join, dim3((sh->tokens + 15) / 16), dim3(1024), 0, s, pairs, label_z, labels, loss, lse, sh->tokens, (sh->vocab + CE_BLOCK - 1) / CE_BLOCK,
                        sh->vocab, sh->ignore_index);
     SLZ_HIP(hipGetLastError());
     return SLZ_OK;
@@ -234,18 +229,13 @@ extern "C" int slz_linear_ce(const slz_ce_shape *sh, const void *h, const void *
 
 template <int EL> static int ce_products(const slz_ce_shape *sh, const ce_plan &P, const slz_operand &g, const slz_operand &oh, const slz_operand &ow,
                                          uint32_t first, uint32_t words, void *dh, void *dw, float *dh_sum, const slz_times_unit &f, hipStream_t s) {
-    const uint32_t eb = slz_type_bytes(sh->type);
-    char *dw_rows = (char *)dw + (int64_t)first * sh->ld_dw * eb;
-    const slz_store_epi<slz_times_unit> to_dw{dw_rows, sh->type, sh->ld_dw, 0, slz_in_place(dw_rows, 16, sh->ld_dw, eb), f};
-    int rc = slz_gemm_launch<slz_tiles_128, EL, true, true>(slz_gemm_of(g, oh, words, sh->inner, sh->tokens), to_dw, 1, s);
+    char *dw_rows = (char *)dw + (int64_t)first * sh->ld_dw * slz_type_bytes(sh->type);
+    int rc = slz_gemm_to<EL, true, true>(slz_gemm_of(g, oh, words, sh->inner, sh->tokens), P.dw_choice, f, dw_rows, sh->type, sh->ld_dw, nullptr, s);
     if (rc != SLZ_OK) return rc;
-    const slz_gemm p = slz_gemm_of(g, ow, sh->tokens, sh->inner, words);
-    if (P.words == sh->vocab) {
-        const slz_store_epi<slz_times_unit> to_dh{dh, sh->type, sh->ld_dh, 0, slz_in_place(dh, 16, sh->ld_dh, eb), f};
-        return slz_gemm_launch<slz_tiles_128, EL, false, true>(p, to_dh, 1, s);
-    }
-    const slz_partial_epi<float> to_sum{dh_sum, P.dh_ld, 1, first != 0};
-    return slz_gemm_launch<slz_tiles_128, EL, false, true>(p, to_sum, 1, s);
+    slz_gemm p = slz_gemm_of(g, ow, sh->tokens, sh->inner, words);
+    if (P.words == sh->vocab) return slz_gemm_to<EL, false, true>(p, P.dh_choice, f, dh, sh->type, sh->ld_dh, (char *)dh_sum, s);
+    p.split = P.dh_choice.split;
+    return slz_gemm_run<EL, false, true>(p, slz_partial_epi<float>{dh_sum, P.dh_ld, 1, first != 0}, P.dh_choice.side, 1, s);
 }
 
 extern "C" int slz_linear_ce_grad(const slz_ce_shape *sh, const void *h, const void *w, const int64_t *labels, const float *lse, const float *dloss,
@@ -269,14 +259,14 @@ extern "C" int slz_linear_ce_grad(const slz_ce_shape *sh, const void *h, const v
         const uint32_t words = sh->vocab - v < P.words ? sh->vocab - v : P.words;
         const slz_operand ow = slz_operand_of(rows_of(w, sh, v), sh->type, words, sh->inner, sh->ld_w, base + P.w, s);
         const ce_grad_epi epi{base + P.g, g.ld, g.piece, sh->type, lse, dloss, unit, labels, sh->ignore_index, v, sh->vocab};
-        rc = ce_logits(sh->type, slz_gemm_of(oh, ow, sh->tokens, words, sh->inner), epi, s);
+        rc = ce_logits(sh->type, slz_gemm_of(oh, ow, sh->tokens, words, sh->inner), epi, P.side, s);
         if (rc == SLZ_OK)
             rc = sh->type == SLZ_F16 ? ce_products<SLZ_EL_F16>(sh, P, g, oh, ow, v, words, dh, dw, dh_sum, f, s)
                                      : ce_products<SLZ_EL_BF16>(sh, P, g, oh, ow, v, words, dh, dw, dh_sum, f, s);
         if (rc != SLZ_OK) return rc;
     }
     if (P.words < sh->vocab && sh->tokens)
-        hipLaunchKernelGGL((k_join<float, slz_times_unit>), ew_grid((size_t)sh->tokens * ((sh->inner + 3) / 4)), dim3(256), 0, s, (const float *)dh_sum, 1u,
+        hipLaunchKernelGGL((k_join<float, slz_times_unit>), ew_grid((size_t)sh->tokens * ((sh->inner + 3) / 4)), dim3(256), 0, s, (const float *)dh_sum, P.dh_choice.split,
                            sh->tokens, sh->inner, P.dh_ld, dh, sh->type, sh->ld_dh, f);
     SLZ_HIP(hipGetLastError());
     return SLZ_OK;

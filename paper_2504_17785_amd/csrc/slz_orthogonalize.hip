@@ -14,16 +14,34 @@
 #define ORTH_UP 64.0f                // operands are held times this: the second halves stay out of the subnormal numbers
 #define ORTH_NORM_BLOCKS 64
 
-struct orth_view {                   // a batch of matrices of two f16 each
+struct orth_view {                   // a batch of matrices of two f16 each; rows of a multiple of 64 elements
     uint16_t *hi, *lo;               // lo may be null
     uint32_t ld;
     size_t stride;                   // elements from matrix to matrix
 };
-__device__ __forceinline__ void orth_put(const orth_view &v, size_t at, float x) {
+__device__ __forceinline__ uint32_t orth_pack(float a, float b) { return slz_f32_to_f16(a) | ((uint32_t)slz_f32_to_f16(b) << 16); }
+// the two halves of ORTH_UP x
+__device__ __forceinline__ void orth_halves(float x, float &hi, float &lo) {
     const float u = x * ORTH_UP;
-    const _Float16 h = (_Float16)u;
-    v.hi[at] = __builtin_bit_cast(uint16_t, h);
-    if (v.lo) v.lo[at] = slz_f32_to_f16(u - (float)h);
+    hi = (float)(_Float16)u;
+    lo = u - hi;
+}
+// four in a row, at a multiple of four
+__device__ __forceinline__ void orth_put4(const orth_view &v, size_t at, const float (&x)[4]) {
+    float hi[4], lo[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) orth_halves(x[i], hi[i], lo[i]);
+    *(uint2 *)(v.hi + at) = make_uint2(orth_pack(hi[0], hi[1]), orth_pack(hi[2], hi[3]));
+    if (v.lo) *(uint2 *)(v.lo + at) = make_uint2(orth_pack(lo[0], lo[1]), orth_pack(lo[2], lo[3]));
+}
+__device__ __forceinline__ void orth_get4(const orth_view &v, size_t at, float (&x)[4]) {
+    const uint2 h = *(const uint2 *)(v.hi + at);
+    uint2 l = make_uint2(0, 0);
+    if (v.lo) l = *(const uint2 *)(v.lo + at);
+    const uint32_t hw[2] = {h.x, h.y}, lw[2] = {l.x, l.y};
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        x[i] = (slz_f16_to_f32((uint16_t)(hw[i / 2] >> (16 * (i & 1)))) + slz_f16_to_f32((uint16_t)(lw[i / 2] >> (16 * (i & 1))))) * (1.0f / ORTH_UP);
 }
 __device__ __forceinline__ float orth_get(const orth_view &v, size_t at) {
     const float h = slz_f16_to_f32(v.hi[at]);
@@ -72,9 +90,11 @@ k_orth_load(const void *__restrict__ g, int type, uint32_t rows, uint32_t cols, 
     }
     __syncthreads();
     const uint32_t m = tall ? cols : rows, wide = ((tall ? rows : cols) + 7u) & ~7u;
-    for (uint32_t i = t; i < 4096; i += 256) {
-        const uint32_t a = i / 64, b = i % 64, r = (tall ? c0 : r0) + a, c = (tall ? r0 : c0) + b;
-        if (r < m && c < wide) orth_put(x, blockIdx.z * x.stride + (size_t)r * x.ld + c, tall ? tile[b][a] : tile[a][b]);
+    for (uint32_t i = t; i < 1024; i += 256) {
+        const uint32_t a = i / 16, b = i % 16 * 4, r = (tall ? c0 : r0) + a, c = (tall ? r0 : c0) + b;
+        float v[4];
+        for (int q = 0; q < 4; q++) v[q] = tall ? tile[b + q][a] : tile[a][b + q];
+        if (r < m && c < wide) orth_put4(x, blockIdx.z * x.stride + (size_t)r * x.ld + c, v);
     }
 }
 __global__ void __launch_bounds__(256)
@@ -87,41 +107,61 @@ k_orth_store(orth_view x, const float *__restrict__ factor, void *__restrict__ o
 }
 
 // ---- the three products of a step -----------------------------------------------------------------------------------------------------------
-// A symmetric product's result: `diagonal` apart, the rest to `out` with zeros on the diagonal and in the columns up to the next multiple of 8.
+// A symmetric product's result: the diagonal apart, the rest to `out` with zeros on the diagonal and in the columns up to the next multiple of 8.
+// A tile below the diagonal is stored a second time, transposed through shared memory, half by half.
 template <class F> struct orth_symmetric_epi {
     orth_view out;
     float *diagonal;                 // [batch][m]
     F f;
     template <int MI, int NI, bool RUN, int WM, int WN, class ACC>
-    __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *) const {
-        const uint32_t wide = (p.M + 7u) & ~7u;
+    __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *lds) const {
+        // 2-byte words; the pitch keeps 16-byte alignment, and without the 8 the tile of 256 x 256 fills the shared memory of its operands
+        constexpr uint32_t TM = WM * MI * 16, TN = WN * NI * 16, PITCH = TM + (TM < 256 ? 8 : 0);
+        static_assert(TN * PITCH * 2 <= 2 * (TM + TN) * 128, "fits the operands' buffers");
+        const uint32_t wide = (p.M + 7u) & ~7u, m0 = at.tile_m * TM, n0 = at.tile_n * TN;
         const size_t base = at.batch * out.stride;
+        uint16_t *turned = (uint16_t *)lds;
+        const int halves = out.lo && at.tile_m != at.tile_n ? 2 : 1;
+        for (int half = 0; half < halves; half++) {
 #pragma unroll
-        for (int i = 0; i < MI; i++) {
-            const uint32_t m = slz_row(at, i);
+            for (int i = 0; i < MI; i++) {
+                const uint32_t m = slz_row(at, i);
 #pragma unroll
-            for (int j = 0; j < NI; j++) {
-                const uint32_t n = slz_col<NI, RUN>(at, j);
+                for (int j = 0; j < NI; j++) {
+                    const uint32_t n = slz_col<NI, RUN>(at, j);
+                    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    if (m < p.M && n < p.M) f(at.batch, m, n, acc[i][j], v);
 #pragma unroll
-                for (int c = 0; c < 4; c++) {
-                    const bool real = m < p.M && n + c < p.M;
-                    float v = real ? f(at.batch, m, n + c, acc[i][j][c]) : 0.0f;
-                    if (real && m == n + c) {
-                        diagonal[at.batch * p.M + m] = f.finish(v);
-                        v = 0.0f;
+                    for (int c = 0; c < 4; c++) {
+                        if (m < p.M && m == n + c) {
+                            diagonal[at.batch * p.M + m] = f.finish(v[c]);
+                            v[c] = 0.0f;
+                        }
+                        if (n + c >= p.M) v[c] = 0.0f;
+                        float hi, lo;
+                        orth_halves(v[c], hi, lo);
+                        turned[(n - n0 + c) * PITCH + m - m0] = slz_f32_to_f16(half ? lo : hi);
                     }
-                    if (m < p.M && n + c < wide) orth_put(out, base + (size_t)m * out.ld + n + c, v);
-                    if (at.tile_m != at.tile_n && n + c < p.M && m < wide) orth_put(out, base + (size_t)(n + c) * out.ld + m, v);
+                    if (half == 0 && m < p.M && n < wide) orth_put4(out, base + (size_t)m * out.ld + n, v);
                 }
             }
+            if (at.tile_m == at.tile_n) return;
+            __syncthreads();
+            uint16_t *to = (half ? out.lo : out.hi) + base;
+            for (uint32_t g = threadIdx.x; g < TN * (TM / 8); g += WM * WN * 64) {
+                const uint32_t n = g / (TM / 8), m = g % (TM / 8) * 8;
+                if (n0 + n < p.M && m0 + m < wide) *(uint4 *)(to + (size_t)(n0 + n) * out.ld + m0 + m) = *(const uint4 *)(turned + n * PITCH + m);
+            }
+            __syncthreads();
         }
     }
 };
 struct orth_gram {
     const float *factor;             // or null
-    __device__ __forceinline__ float operator()(uint32_t batch, uint32_t, uint32_t, float sum) const {
-        const float f = factor ? factor[batch] : 1.0f;
-        return sum * (f * f / (ORTH_UP * ORTH_UP));
+    __device__ __forceinline__ void operator()(uint32_t batch, uint32_t, uint32_t, const v4f &sum, float (&v)[4]) const {
+        const float f = factor ? factor[batch] : 1.0f, by = f * f / (ORTH_UP * ORTH_UP);
+#pragma unroll
+        for (int c = 0; c < 4; c++) v[c] = sum[c] * by;
     }
     __device__ __forceinline__ float finish(float v) const { return v; }
 };
@@ -130,10 +170,17 @@ struct orth_polynomial {
     const float *d;                  // of A
     uint32_t m_all;
     float a, b, c;
-    __device__ __forceinline__ float operator()(uint32_t batch, uint32_t m, uint32_t n, float sum) const {
-        const float x = orth_get(o, batch * o.stride + (size_t)m * o.ld + n), dm = d[batch * m_all + m], dn = d[batch * m_all + n];
-        const float square = sum * (1.0f / (ORTH_UP * ORTH_UP)) + (dm + dn) * x + (m == n ? dm * dm : 0.0f);
-        return b * (m == n ? dm : x) + c * square;
+    __device__ __forceinline__ void operator()(uint32_t batch, uint32_t m, uint32_t n, const v4f &sum, float (&v)[4]) const {
+        float x[4];
+        orth_get4(o, batch * o.stride + (size_t)m * o.ld + n, x);
+        const float dm = d[batch * m_all + m];
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const bool on = m == n + q;
+            const float dn = d[batch * m_all + min(n + q, m_all - 1)];
+            const float square = sum[q] * (1.0f / (ORTH_UP * ORTH_UP)) + (dm + dn) * x[q] + (on ? dm * dm : 0.0f);
+            v[q] = b * (on ? dm : x[q]) + c * square;
+        }
     }
     __device__ __forceinline__ float finish(float v) const { return a + v; }
 };
@@ -143,6 +190,7 @@ struct orth_apply_epi {
     const float *factor;             // or null
     void *out;                       // the last step's result goes here, or null
     int type, tall;
+    uint32_t aligned;                // its rows begin at multiples of 16 bytes
     int64_t ld_out, stride_out;
     template <int MI, int NI, bool RUN, int WM, int WN, class ACC>
     __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *) const {
@@ -156,13 +204,20 @@ struct orth_apply_epi {
 #pragma unroll
             for (int j = 0; j < NI; j++) {
                 const uint32_t n = slz_col<NI, RUN>(at, j);
+                if (n >= wide) continue;
+                const size_t here = at.batch * x.stride + (size_t)m * x.ld + n;
+                float old[4], v[4];
+                orth_get4(x, here, old);
 #pragma unroll
-                for (int c = 0; c < 4; c++) {
-                    if (n + c >= wide) continue;
-                    const size_t here = at.batch * x.stride + (size_t)m * x.ld + n + c;
-                    const float v = n + c < p.N ? f * (d * orth_get(x, here) + acc[i][j][c] * (1.0f / (ORTH_UP * ORTH_UP))) : 0.0f;
-                    if (!out) orth_put(next, here, v);
-                    else if (n + c < p.N) slz_put(out, type, at.batch * stride_out + (tall ? (int64_t)(n + c) * ld_out + m : (int64_t)m * ld_out + n + c), v);
+                for (int c = 0; c < 4; c++) v[c] = n + c < p.N ? f * (d * old[c] + acc[i][j][c] * (1.0f / (ORTH_UP * ORTH_UP))) : 0.0f;
+                if (!out) orth_put4(next, here, v);
+                else if (n < p.N) {
+                    const int64_t first = at.batch * stride_out;
+                    if (!tall) slz_put_run<4>((char *)out + (first + (int64_t)m * ld_out + n) * slz_type_bytes(type), type, v, p.N - n, aligned);
+                    else
+#pragma unroll
+                        for (int c = 0; c < 4; c++)
+                            if (n + c < p.N) slz_put(out, type, first + (int64_t)(n + c) * ld_out + m, v[c]);
                 }
             }
         }
@@ -174,6 +229,7 @@ struct orth_plan {
     uint32_t ld_x, ld_a;
     size_t one_x, one_a;             // bytes of a piece of X, of A or B
     size_t x[2], a, b, da, db, factor, part, total;
+    uint32_t gram, polynomial, apply;                // sides of their tiles
 };
 static orth_plan plan_orth(const slz_orth_shape *sh) {
     orth_plan P;
@@ -193,6 +249,10 @@ static orth_plan plan_orth(const slz_orth_shape *sh) {
     P.factor = o; o += up256((size_t)sh->batch * 4);
     P.part = o; o += up256((size_t)sh->batch * ORTH_NORM_BLOCKS * 8);
     P.total = o;
+    const uint32_t pairs = P.pieces == 2 ? 3 : 1;
+    P.gram = slz_choose(P.m, P.m, (P.n + 63) / 64 * pairs, sh->batch, true, 1).side;
+    P.polynomial = slz_choose(P.m, P.m, (P.m + 63) / 64 * pairs, sh->batch, true, 1).side;
+    P.apply = slz_choose(P.m, P.n, (P.m + 63) / 64 * pairs, sh->batch, false, 1).side;
     return P;
 }
 static int orth_check(const slz_orth_shape *sh) {
@@ -243,6 +303,7 @@ extern "C" int slz_orthogonalize(const slz_orth_shape *sh, const void *g, void *
     b = {(uint16_t *)(w + P.b), P.pieces == 2 ? (uint16_t *)(w + P.b + P.one_a) : nullptr, P.ld_a, as};
     float *da = (float *)(w + P.da), *db = (float *)(w + P.db), *factor = (float *)(w + P.factor);
     double *part = (double *)(w + P.part);
+    const uint32_t aligned = slz_in_place(out, 16, sh->ld_out, eb) && (sh->batch == 1 || sh->stride_out * eb % 16 == 0);
     const uint32_t parts = sh->rows < ORTH_NORM_BLOCKS ? sh->rows : ORTH_NORM_BLOCKS;
     hipLaunchKernelGGL(k_orth_norm, dim3(parts, sh->batch), dim3(256), 0, s, g, sh->type, sh->rows, sh->cols, sh->ld_g, sh->stride_g, part);
     hipLaunchKernelGGL(k_orth_load, dim3((sh->cols + 63) / 64, (sh->rows + 63) / 64, sh->batch), dim3(256), 0, s, g, sh->type, sh->rows, sh->cols, sh->ld_g,
@@ -254,15 +315,15 @@ extern "C" int slz_orthogonalize(const slz_orth_shape *sh, const void *g, void *
         const float *f = i == 0 ? factor : nullptr;
         slz_gemm p = orth_product(now, now, P.pieces, P.m, P.m, P.n);
         p.symmetric = 1;
-        int rc = slz_gemm_launch<slz_tiles_128, SLZ_EL_F16, false, false>(p, orth_symmetric_epi<orth_gram>{a, da, {f}}, sh->batch, s);
+        int rc = slz_gemm_run<SLZ_EL_F16, false, false>(p, orth_symmetric_epi<orth_gram>{a, da, {f}}, P.gram, sh->batch, s);
         if (rc != SLZ_OK) return rc;
         p = orth_product(a, a, P.pieces, P.m, P.m, P.m);
         p.symmetric = 1;
-        rc = slz_gemm_launch<slz_tiles_128, SLZ_EL_F16, false, false>(p, orth_symmetric_epi<orth_polynomial>{b, db, {a, da, P.m, sh->a, sh->b, sh->c}}, sh->batch, s);
+        rc = slz_gemm_run<SLZ_EL_F16, false, false>(p, orth_symmetric_epi<orth_polynomial>{b, db, {a, da, P.m, sh->a, sh->b, sh->c}}, P.polynomial, sh->batch, s);
         if (rc != SLZ_OK) return rc;
         p = orth_product(b, now, P.pieces, P.m, P.n, P.m);
-        const orth_apply_epi epi{now, next, db, f, i + 1 == sh->steps ? out : nullptr, sh->type, tall, sh->ld_out, sh->stride_out};
-        rc = slz_gemm_launch<slz_tiles_128, SLZ_EL_F16, false, true>(p, epi, sh->batch, s);
+        const orth_apply_epi epi{now, next, db, f, i + 1 == sh->steps ? out : nullptr, sh->type, tall, aligned, sh->ld_out, sh->stride_out};
+        rc = slz_gemm_run<SLZ_EL_F16, false, true>(p, epi, P.apply, sh->batch, s);
         if (rc != SLZ_OK) return rc;
     }
     SLZ_HIP(hipGetLastError());
