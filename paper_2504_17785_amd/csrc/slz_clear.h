@@ -81,16 +81,33 @@ template <int C> __device__ __forceinline__ void slz_put_run(void *p, int type, 
     for (int i = 0; i < C; i++)
         if ((uint32_t)i < valid) slz_put(p, type, i, v[i]);
 }
-// sum and maximum over a wave, the same bits in every lane
-__device__ __forceinline__ float slz_wave_sum(float x) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
-    return x;
+// maximum over a wave, in every lane: over 16 lanes by lane permutations within the row, then over the four rows
+template <int CONTROL> __device__ __forceinline__ float slz_dpp_max(float x) {
+    return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, true)));
 }
 __device__ __forceinline__ float slz_wave_max(float x) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
-    return x;
+    x = slz_dpp_max<0xb1>(x);                          // lanes 1 apart, 2 apart, mirrored in 8, mirrored in 16
+    x = slz_dpp_max<0x4e>(x);
+    x = slz_dpp_max<0x141>(x);
+    x = slz_dpp_max<0x140>(x);
+    const int v = __builtin_bit_cast(int, x);
+    const float a = __builtin_bit_cast(float, __builtin_amdgcn_readlane(v, 0)), b = __builtin_bit_cast(float, __builtin_amdgcn_readlane(v, 16));
+    const float c = __builtin_bit_cast(float, __builtin_amdgcn_readlane(v, 32)), d = __builtin_bit_cast(float, __builtin_amdgcn_readlane(v, 48));
+    return fmaxf(fmaxf(a, b), fmaxf(c, d));
+}
+template <int CONTROL> __device__ __forceinline__ float slz_dpp_add(float x) {
+    return x + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, true));
+}
+// sum over a wave, the same bits in every lane
+__device__ __forceinline__ float slz_wave_sum(float x) {
+    x = slz_dpp_add<0xb1>(x);
+    x = slz_dpp_add<0x4e>(x);
+    x = slz_dpp_add<0x141>(x);
+    x = slz_dpp_add<0x140>(x);
+    const int v = __builtin_bit_cast(int, x);
+    const float a = __builtin_bit_cast(float, __builtin_amdgcn_readlane(v, 0)), b = __builtin_bit_cast(float, __builtin_amdgcn_readlane(v, 16));
+    const float c = __builtin_bit_cast(float, __builtin_amdgcn_readlane(v, 32)), d = __builtin_bit_cast(float, __builtin_amdgcn_readlane(v, 48));
+    return (a + b) + (c + d);
 }
 #endif
 
@@ -102,11 +119,15 @@ struct slz_operand {
     uint32_t pieces;
     int element;                     // SLZ_BF16, SLZ_F16, or 3 for int8
 };
+// what is to be laid out before a product: matrices of elements of 1, 2 or 4 bytes (these into three bf16), in one launch
+struct slz_layout { const char *x; char *out; int64_t ld, piece; uint32_t rows, cols, ld_out, bytes; };
+struct slz_layouts { slz_layout job[2]; uint32_t count; };
+void slz_layout_run(const slz_layouts &jobs, hipStream_t s);
 // bytes of workspace for laying out rows x cols of `type` (0 when it can be read in place)
 size_t slz_operand_bytes(const void *p, int type, uint32_t rows, uint32_t cols, int64_t ld);
-// and the operand; ws: that many bytes
-slz_operand slz_operand_of(const void *p, int type, uint32_t rows, uint32_t cols, int64_t ld, char *ws, hipStream_t s);
+// and the operand; ws: that many bytes, which the job that is added fills
+slz_operand slz_operand_of(const void *p, int type, uint32_t rows, uint32_t cols, int64_t ld, char *ws, slz_layouts &jobs);
 size_t slz_operand_i8_bytes(const int8_t *p, uint32_t rows, uint32_t cols, int64_t ld);
-slz_operand slz_operand_i8_of(const int8_t *p, uint32_t rows, uint32_t cols, int64_t ld, char *ws, hipStream_t s);
+slz_operand slz_operand_i8_of(const int8_t *p, uint32_t rows, uint32_t cols, int64_t ld, char *ws, slz_layouts &jobs);
 // *unit: the power of two at or above the largest magnitude of `count` values; what f16 could not hold is divided by it
 void slz_unit_of(const float *values, uint32_t count, float *unit, hipStream_t s);

@@ -2,73 +2,75 @@
 // three of bf16.
 #include "slz_clear.h"
 
-// rows x cols elements of SRC bytes, rows padded with zeros to ld_out bytes; one thread per 16 bytes of the result
-template <int SRC>
-__global__ void __launch_bounds__(256) k_align(const char *__restrict__ x, char *__restrict__ out, uint32_t rows, uint32_t cols, int64_t ld, uint32_t ld_out) {
+// A thread makes 16 bytes of each piece of a job's result; jobs by grid y.
+template <int SRC> __device__ __forceinline__ void align_16(const slz_layout &j, size_t r, uint32_t c, char *to) {
     constexpr int C = 16 / SRC;
-    const uint32_t per_row = ld_out / 16u;
-    const size_t total = (size_t)rows * per_row;
+    union { uint8_t b[16]; uint16_t h[8]; uint4 v; } u;
+    u.v = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < C; i++)
+        if (c + i < j.cols) {
+            if (SRC == 1) u.b[i] = ((const uint8_t *)j.x)[r * j.ld + c + i];
+            else u.h[i % 8] = ((const uint16_t *)j.x)[r * j.ld + c + i];
+        }
+    *(uint4 *)to = u.v;
+}
+__global__ void __launch_bounds__(256) k_layout(const slz_layouts jobs) {
+    const slz_layout j = jobs.job[blockIdx.y];
+    const uint32_t per_row = j.ld_out / 16u;
+    const size_t total = (size_t)j.rows * per_row;
     for (size_t g = (size_t)blockIdx.x * 256 + threadIdx.x; g < total; g += (size_t)gridDim.x * 256) {
         const size_t r = g / per_row;
-        const uint32_t c = (uint32_t)(g % per_row) * C;
-        union { uint8_t b[16]; uint16_t h[8]; uint4 v; } u;
-        u.v = make_uint4(0, 0, 0, 0);
-        for (int i = 0; i < C; i++)
-            if (c + i < cols) {
-                if (SRC == 1) u.b[i] = ((const uint8_t *)x)[r * ld + c + i];
-                else u.h[i % 8] = ((const uint16_t *)x)[r * ld + c + i];
+        const uint32_t at = (uint32_t)(g % per_row) * 16u;
+        char *to = j.out + r * j.ld_out + at;
+        if (j.bytes == 1) align_16<1>(j, r, at, to);
+        else if (j.bytes == 2) align_16<2>(j, r, at / 2, to);
+        else {
+            uint32_t w[3][4];
+            uint16_t t[2][3];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                slz_split3(at / 2 + i < j.cols ? ((const float *)j.x)[r * j.ld + at / 2 + i] : 0.0f, t[i & 1]);
+                if (i & 1)
+                    for (int k = 0; k < 3; k++) w[k][i / 2] = t[0][k] | ((uint32_t)t[1][k] << 16);
             }
-        *(uint4 *)(out + r * ld_out + (size_t)c * SRC) = u.v;
+            for (int k = 0; k < 3; k++) *(uint4 *)(to + k * j.piece) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+        }
     }
 }
-__global__ void __launch_bounds__(256) k_split3(const float *__restrict__ x, char *__restrict__ out, uint32_t rows, uint32_t cols, int64_t ld, uint32_t ld_out, int64_t piece) {
-    const uint32_t per_row = ld_out / 16u;
-    const size_t total = (size_t)rows * per_row;
-    for (size_t g = (size_t)blockIdx.x * 256 + threadIdx.x; g < total; g += (size_t)gridDim.x * 256) {
-        const size_t r = g / per_row;
-        const uint32_t c = (uint32_t)(g % per_row) * 8;
-        uint16_t q[3][8];
-        for (int i = 0; i < 8; i++) {
-            uint16_t t[3] = {0, 0, 0};
-            if (c + i < cols) slz_split3(x[r * ld + c + i], t);
-            for (int k = 0; k < 3; k++) q[k][i] = t[k];
-        }
-        for (int k = 0; k < 3; k++) {
-            uint32_t w[4];
-            for (int i = 0; i < 4; i++) w[i] = q[k][2 * i] | ((uint32_t)q[k][2 * i + 1] << 16);
-            *(uint4 *)(out + k * piece + r * ld_out + (size_t)c * 2) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+void slz_layout_run(const slz_layouts &jobs, hipStream_t s) {
+    size_t most = 0;
+    for (uint32_t i = 0; i < jobs.count; i++) {
+        const size_t n = (size_t)jobs.job[i].rows * (jobs.job[i].ld_out / 16u);
+        most = n > most ? n : most;
     }
+    if (most) hipLaunchKernelGGL(k_layout, dim3(ew_grid(most).x, jobs.count), dim3(256), 0, s, jobs);
 }
 
 static size_t row_bytes(uint32_t cols, uint32_t bytes) { return ((size_t)cols * bytes + 127) / 128 * 128; }
+static void add(slz_layouts &jobs, const void *p, uint32_t rows, uint32_t cols, int64_t ld, uint32_t bytes, const slz_operand &o, char *ws) {
+    if (rows && cols) jobs.job[jobs.count++] = {(const char *)p, ws, ld, o.piece, rows, cols, (uint32_t)o.ld, bytes};
+}
 
 size_t slz_operand_bytes(const void *p, int type, uint32_t rows, uint32_t cols, int64_t ld) {
     if (type == SLZ_F32) return 3 * up256(rows * row_bytes(cols, 2));
     return slz_in_place(p, cols, ld, 2) ? 0 : up256(rows * row_bytes(cols, 2));
 }
-slz_operand slz_operand_of(const void *p, int type, uint32_t rows, uint32_t cols, int64_t ld, char *ws, hipStream_t s) {
+slz_operand slz_operand_of(const void *p, int type, uint32_t rows, uint32_t cols, int64_t ld, char *ws, slz_layouts &jobs) {
     const int64_t row = row_bytes(cols, 2);
-    if (type == SLZ_F32) {
-        const slz_operand o{ws, row, (int64_t)up256(rows * row), 3, SLZ_BF16};
-        if (rows && cols)
-            hipLaunchKernelGGL(k_split3, ew_grid((size_t)rows * row / 16), dim3(256), 0, s, (const float *)p, ws, rows, cols, ld, (uint32_t)row, o.piece);
-        return o;
-    }
-    if (slz_in_place(p, cols, ld, 2)) return {(const char *)p, ld * 2, 0, 1, type};
-    if (rows && cols)
-        hipLaunchKernelGGL(k_align<2>, ew_grid((size_t)rows * row / 16), dim3(256), 0, s, (const char *)p, ws, rows, cols, ld, (uint32_t)row);
-    return {ws, row, 0, 1, type};
+    if (type != SLZ_F32 && slz_in_place(p, cols, ld, 2)) return {(const char *)p, ld * 2, 0, 1, type};
+    const slz_operand o = type == SLZ_F32 ? slz_operand{ws, row, (int64_t)up256(rows * row), 3, SLZ_BF16} : slz_operand{ws, row, 0, 1, type};
+    add(jobs, p, rows, cols, ld, slz_type_bytes(type), o, ws);
+    return o;
 }
 size_t slz_operand_i8_bytes(const int8_t *p, uint32_t rows, uint32_t cols, int64_t ld) {
     return slz_in_place(p, cols, ld, 1) ? 0 : up256(rows * row_bytes(cols, 1));
 }
-slz_operand slz_operand_i8_of(const int8_t *p, uint32_t rows, uint32_t cols, int64_t ld, char *ws, hipStream_t s) {
+slz_operand slz_operand_i8_of(const int8_t *p, uint32_t rows, uint32_t cols, int64_t ld, char *ws, slz_layouts &jobs) {
     if (slz_in_place(p, cols, ld, 1)) return {(const char *)p, ld, 0, 1, 3};
-    const int64_t row = row_bytes(cols, 1);
-    if (rows && cols)
-        hipLaunchKernelGGL(k_align<1>, ew_grid((size_t)rows * row / 16), dim3(256), 0, s, (const char *)p, ws, rows, cols, ld, (uint32_t)row);
-    return {ws, row, 0, 1, 3};
+    const slz_operand o{ws, (int64_t)row_bytes(cols, 1), 0, 1, 3};
+    add(jobs, p, rows, cols, ld, 1, o, ws);
+    return o;
 }
 
 // One workgroup: the power of two at or above the largest of the magnitudes (1 where there is none that is finite)

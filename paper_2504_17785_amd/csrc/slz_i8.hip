@@ -2,7 +2,6 @@
 #include "slz_gemm.h"
 
 // ---- quantisation ------------------------------------------------------------------------------------------------------------------
-// One workgroup per row: its largest magnitude, then its entries, read again from the cache.
 // A row whose largest entry is below 2^-100 is moved up by 2^100 first, so that 127 / top stays finite.
 __device__ __forceinline__ float quantize_scale(float top, bool finite, float &up, float &inv) {
     up = top < 0x1p-100f ? 0x1p100f : 1.0f;
@@ -14,28 +13,112 @@ __device__ __forceinline__ int8_t quantize_one(float x, float up, float inv) {
     return (int8_t)(int)fminf(fmaxf(rintf(x * up * inv), -127.0f), 127.0f);
 }
 
-__global__ void __launch_bounds__(256)
-k_quantize(const void *__restrict__ x, int type, uint32_t cols, int64_t ld_x, int8_t *__restrict__ q, int64_t ld_q, float *__restrict__ scale) {
-    const size_t row = blockIdx.x;
-    __shared__ float tops[4];
-    __shared__ int bad[4];
+// Eight elements of a row of `cols` at c (a multiple of 8), zeros past its end; the row may begin at any address.  Where the row ends inside,
+// its last eight are read and moved down.  In two parts, so that several loads are under way before the first is looked at.
+typedef v4i32 v4i32_any __attribute__((aligned(1)));
+template <int TYPE> struct row8 { v4i32 w[TYPE == SLZ_F32 ? 2 : 1]; };
+template <int TYPE> __device__ __forceinline__ row8<TYPE> row8_load(const void *x, size_t row, uint32_t c, uint32_t cols) {
+    row8<TYPE> q;
+    if (cols < 8u) {                                   // all of it, in the first threads
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = c + i < cols ? slz_get(x, TYPE, row + c + i) : 0.0f;
+        if constexpr (TYPE == SLZ_F32) {
+            q.w[0] = v4i32{__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
+            q.w[1] = v4i32{__float_as_int(v[4]), __float_as_int(v[5]), __float_as_int(v[6]), __float_as_int(v[7])};
+        } else {
+            uint32_t h[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) h[i] = slz_half(v[2 * i], TYPE) | ((uint32_t)slz_half(v[2 * i + 1], TYPE) << 16);
+            q.w[0] = v4i32{(int)h[0], (int)h[1], (int)h[2], (int)h[3]};
+        }
+        return q;
+    }
+    const uint32_t from = min(c, cols - 8u);
+    const v4i32_any *p = (const v4i32_any *)((const char *)x + (row + from) * slz_type_bytes(TYPE));
+    q.w[0] = p[0];
+    if constexpr (TYPE == SLZ_F32) q.w[1] = p[1];
+    return q;
+}
+template <int TYPE> __device__ __forceinline__ void row8_values(const row8<TYPE> &q, uint32_t c, uint32_t cols, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        if constexpr (TYPE == SLZ_F32) v[i] = __int_as_float(q.w[i / 4][i % 4]);
+        else {
+            const uint16_t h = (uint16_t)((uint32_t)q.w[0][i / 2] >> (16 * (i & 1)));
+            v[i] = TYPE == SLZ_BF16 ? slz_bf16_to_f32(h) : slz_f16_to_f32(h);
+        }
+    }
+    if (c + 8u <= cols) return;
+    const uint32_t gone = c >= cols ? 8u : cols < 8u ? 0u : c + 8u - cols;
+#pragma unroll
+    for (uint32_t b = 1; b < 16; b <<= 1)
+#pragma unroll
+        for (uint32_t i = 0; i < 8; i++) v[i] = gone & b ? (i + b < 8 ? v[(i + b) % 8] : 0.0f) : v[i];
+}
+__device__ __forceinline__ float top_of(const float (&v)[8]) {
     float top = 0.0f;
-    bool odd = false;
-    for (uint32_t c = threadIdx.x; c < cols; c += 256) {
-        const float v = fabsf(slz_get(x, type, row * ld_x + c));
-        odd |= !(v < __builtin_inff());
-        top = fmaxf(top, v);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float a = fabsf(v[i]);
+        top = a < __builtin_inff() ? fmaxf(top, a) : __builtin_inff();             // NaN too; stays
+    }
+    return top;
+}
+__device__ __forceinline__ uint2 quantize8(const float (&v)[8], bool finite, float up, float inv) {
+    uint32_t w[2] = {0, 0};
+    if (finite)
+#pragma unroll
+        for (int i = 0; i < 8; i++) w[i / 4] |= (uint32_t)(uint8_t)quantize_one(v[i], up, inv) << (8 * (i & 3));
+    return make_uint2(w[0], w[1]);
+}
+// One workgroup per row.  A row of up to 16 entries a thread stays in registers, of a longer one the rest is read again from the cache.
+#define QUANTIZE_KEPT 2
+template <int TYPE>
+__global__ void __launch_bounds__(256)
+k_quantize(const void *__restrict__ x, uint32_t cols, int64_t ld_x, int8_t *__restrict__ q, int64_t ld_q, uint32_t words, float *__restrict__ scale) {
+    const size_t row = blockIdx.x, at = row * ld_x;
+    __shared__ float tops[4];
+    float kept[QUANTIZE_KEPT][8], top = 0.0f;
+    row8<TYPE> first[QUANTIZE_KEPT];
+#pragma unroll
+    for (int k = 0; k < QUANTIZE_KEPT; k++) first[k] = row8_load<TYPE>(x, at, (threadIdx.x + k * 256) * 8, cols);
+#pragma unroll
+    for (int k = 0; k < QUANTIZE_KEPT; k++) {
+        row8_values<TYPE>(first[k], (threadIdx.x + k * 256) * 8, cols, kept[k]);
+        top = fmaxf(top, top_of(kept[k]));
+    }
+    for (uint32_t c = (threadIdx.x + QUANTIZE_KEPT * 256) * 8; c < cols; c += 2048) {
+        float v[8];
+        row8_values<TYPE>(row8_load<TYPE>(x, at, c, cols), c, cols, v);
+        top = fmaxf(top, top_of(v));
     }
     top = slz_wave_max(top);
-    const bool any = __any(odd);
-    if ((threadIdx.x & 63) == 0) { tops[threadIdx.x >> 6] = top; bad[threadIdx.x >> 6] = any; }
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
     __syncthreads();
     top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    const bool finite = !(bad[0] | bad[1] | bad[2] | bad[3]);
+    const bool finite = top < __builtin_inff();
     float up, inv;
     const float sc = quantize_scale(top, finite, up, inv);
     if (threadIdx.x == 0) scale[row] = sc;
-    for (uint32_t c = threadIdx.x; c < cols; c += 256) q[row * ld_q + c] = finite ? quantize_one(slz_get(x, type, row * ld_x + c), up, inv) : (int8_t)0;
+    int8_t *out = q + row * ld_q;
+    for (uint32_t k = 0, c = threadIdx.x * 8; c < cols; k++, c += 2048) {
+        float v[8];
+        if (k < QUANTIZE_KEPT)
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] = k == 0 ? kept[0][i] : kept[1][i];
+        else row8_values<TYPE>(row8_load<TYPE>(x, at, c, cols), c, cols, v);
+        const uint2 w = quantize8(v, finite, up, inv);
+        if (words && c + 8 <= cols) *(uint2 *)(out + c) = w;
+        else
+            for (uint32_t i = 0; i < 8 && c + i < cols; i++) out[c + i] = (int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+    }
+}
+static int quantize_rows(const void *x, int type, uint32_t rows, uint32_t cols, int64_t ld_x, int8_t *q, int64_t ld_q, float *scale, hipStream_t s) {
+    const uint32_t words = !(((uintptr_t)q | (uint64_t)ld_q) & 7u);               // rows of q begin at multiples of eight
+    const auto k = type == SLZ_F32 ? k_quantize<SLZ_F32> : type == SLZ_BF16 ? k_quantize<SLZ_BF16> : k_quantize<SLZ_F16>;
+    hipLaunchKernelGGL(k, dim3(rows), dim3(256), 0, s, x, cols, ld_x, q, ld_q, words, scale);
+    return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
 }
 
 extern "C" int slz_quantize_i8(const void *x, int type, uint32_t rows, uint32_t cols, int64_t ld_x, int8_t *q, int64_t ld_q, float *scale, void *stream) {
@@ -44,9 +127,229 @@ extern "C" int slz_quantize_i8(const void *x, int type, uint32_t rows, uint32_t 
     if (rc == SLZ_OK) rc = slz_matrix_check(q, rows, cols, ld_q, 1);
     if (rc == SLZ_OK) rc = slz_matrix_check(scale, rows, 1, 1, 4);
     if (rc != SLZ_OK || rows == 0) return rc;
-    hipLaunchKernelGGL(k_quantize, dim3(rows), dim3(256), 0, (hipStream_t)stream, x, type, cols, ld_x, q, ld_q, scale);
-    SLZ_HIP(hipGetLastError());
-    return SLZ_OK;
+    return quantize_rows(x, type, rows, cols, ld_x, q, ld_q, scale, (hipStream_t)stream);
+}
+
+// ---- few rows ------------------------------------------------------------------------------------------------------------------------
+// Up to 32 rows of a: every byte of b is used for at most 32 products, so b is streamed once from memory straight into the matrix
+// instructions' registers, and what counts is how much of it is under way.  A workgroup of eight waves has 16 NB rows of b, each wave an
+// eighth of k with its first loads issued before anything else; a (quantised here, if it is x) lies in shared memory; the
+// eight waves' sums meet there.  Rows of b may begin at any address.
+#define THIN_WAVES 8
+#define THIN_AHEAD 8                 // loads of 1 KiB under way in each wave
+#define THIN_LDS (144u << 10)
+#define THIN_MAX_ROWS 32u
+#define THIN_SLOTS 8                 // parts of 512 elements of x that a wave quantises
+#ifndef THIN_WIDE
+#define THIN_WIDE 8192
+#endif
+
+// 16 bytes at k (a multiple of 16) of a row of `count` bytes, zeros past its end.  Where the row ends inside, its last 16 are read and moved down.
+__device__ __forceinline__ v4i32 thin_load(const int8_t *row, uint32_t k, uint32_t count) {
+    union { int8_t b[16]; uint64_t d[2]; v4i32 v; } u;
+    u.v = v4i32{0, 0, 0, 0};
+    if (k >= count) return u.v;
+    if (count < 16u) {
+#pragma unroll
+        for (uint32_t i = 0; i < 15u; i++)
+            if (i < count) u.b[i] = row[i];
+        return u.v;
+    }
+    const uint32_t from = min(k, count - 16u), bits = (k - from) * 8u;
+    u.v = *(const v4i32_any *)(row + from);
+    if (bits >= 64u) {
+        u.d[0] = u.d[1] >> (bits - 64u);
+        u.d[1] = 0;
+    } else if (bits) {
+        u.d[0] = (u.d[0] >> bits) | (u.d[1] << (64u - bits));
+        u.d[1] >>= bits;
+    }
+    return u.v;
+}
+
+typedef v4i32 v4i32_4 __attribute__((aligned(4)));
+
+struct thin_args {
+    const void *a;                   // int8, or x where it is quantised here
+    const float *sa;                 // scales of a, or null
+    int type;                        // of y and x
+    int64_t ld_a;
+    const int8_t *b;
+    const float *sb;
+    int64_t ld_b;
+    void *y;
+    int64_t ld_y;
+    uint32_t M, N, K, pitch;         // pitch: bytes of a row of a in shared memory
+};
+
+// XTYPE: x's type where a is x and quantised here, or -1 where a is int8
+template <int MI, int NB, int XTYPE>
+__global__ void __launch_bounds__(THIN_WAVES * 64) k_thin_i8(const thin_args p) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float tops[THIN_WAVES][THIN_SLOTS], scales[THIN_MAX_ROWS];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15u, g = lane >> 4;
+    const uint32_t n0 = blockIdx.x * (16 * NB), steps = (p.K + 63u) / 64u;
+    const uint32_t begin = wave * steps / THIN_WAVES, end = (wave + 1) * steps / THIN_WAVES;
+    const uint32_t whole = min(end, p.K / 64u);        // steps that end inside the rows; at most one is left, in the last wave
+    constexpr int DEPTH = THIN_AHEAD / NB;
+    // x: several waves share a row where there are fewer rows than waves; each wave's 512-element parts of its rows are its slots
+    constexpr int SLOTS = XTYPE >= 0 ? THIN_SLOTS : 1;
+    const uint32_t per_row = p.M >= THIN_WAVES ? 1u : p.M > 2 ? 2u : p.M == 2 ? 4u : 8u, parts = (p.K + per_row * 512u - 1) / (per_row * 512u);
+    const uint32_t used = (p.M * per_row + THIN_WAVES - 1) / THIN_WAVES * parts;
+    row8<XTYPE < 0 ? SLZ_F32 : XTYPE> x[SLOTS];
+    uint32_t slot_row[SLOTS], slot_part[SLOTS], slot_first[SLOTS];                  // the slot's row, its part of it, the slot of the row's first part
+    {
+        uint32_t m = wave / per_row, part = 0, first = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < SLOTS; i++) {
+            slot_row[i] = m; slot_part[i] = part; slot_first[i] = first;
+            if (++part == parts) { part = 0; m += THIN_WAVES / per_row; first = i + 1; }
+        }
+    }
+    const auto slot_col = [&](int i) { return ((slot_part[i] * per_row + wave % per_row) * 64u + lane) * 8u; };
+    if constexpr (XTYPE >= 0)
+#pragma unroll
+        for (int i = 0; i < SLOTS; i++)
+            if (i < used) x[i] = row8_load<XTYPE>(p.a, (size_t)min(slot_row[i], p.M - 1) * p.ld_a, slot_col(i), p.K);
+    // rows that do not begin at a multiple of 4 bytes: 16 bytes at any address take the memory path several times as long as 16 at a multiple of
+    // 4, so these and the 4 behind them are read and shifted (those 4 hold bytes of the row, or are not looked at)
+    const bool odd = (((uintptr_t)p.b | (uint64_t)p.ld_b) & 3u) != 0;
+    const char *row[NB];
+    uint32_t shift[NB];
+#pragma unroll
+    for (int j = 0; j < NB; j++) {
+        const char *at = (const char *)p.b + (int64_t)min(n0 + j * 16 + r, p.N - 1) * p.ld_b + g * 16u;
+        shift[j] = (uint32_t)(uintptr_t)at & 3u;
+        row[j] = at - shift[j];
+    }
+    const auto b_load = [&](int j, uint32_t step, v4i32 &v, uint32_t &next) {
+        const char *at = row[j] + step * 64u;
+        v = *(const v4i32_4 *)at;
+        if (odd) next = *(const uint32_t *)(at + (shift[j] ? 16 : 12));
+    };
+    const auto b_value = [&](int j, const v4i32 &v, uint32_t next) {
+        if (!odd) return v;
+        v4i32 o;
+#pragma unroll
+        for (int i = 0; i < 4; i++) o[i] = (int)__builtin_amdgcn_alignbyte(i < 3 ? (uint32_t)v[(i + 1) % 4] : next, (uint32_t)v[i], shift[j]);
+        return o;
+    };
+    v4i32 ahead[DEPTH][NB];
+    uint32_t behind[DEPTH][NB] = {};
+    if (begin < whole)
+#pragma unroll
+        for (int d = 0; d < DEPTH; d++)
+#pragma unroll
+            for (int j = 0; j < NB; j++) b_load(j, min(begin + d, whole - 1), ahead[d][j], behind[d][j]);
+    __builtin_amdgcn_sched_barrier(0);
+
+    // a's rows to shared memory, zeros behind them up to a whole step
+    if constexpr (XTYPE >= 0) {
+#pragma unroll
+        for (int i = 0; i < SLOTS; i++) {
+            if (i >= used) continue;
+            float v[8];
+            row8_values<XTYPE>(x[i], slot_col(i), p.K, v);
+            const float top = slz_wave_max(top_of(v));
+            if (lane == 0) tops[wave][i] = top;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < SLOTS; i++) {
+            const uint32_t m = slot_row[i], c = slot_col(i);
+            if (i >= used || m >= p.M) continue;
+            float top = 0.0f, up, inv;
+            // per_row waves have parts of it, each in `parts` slots: at most 64 values, one a lane
+            const uint32_t k = lane % THIN_SLOTS, w = lane / THIN_SLOTS;
+            if (k < parts && w < per_row) top = tops[wave / per_row * per_row + w][slot_first[i] + k];
+            top = slz_wave_max(top);
+            const bool finite = top < __builtin_inff();
+            const float scale = quantize_scale(top, finite, up, inv);
+            if (c == 0) scales[m] = scale;
+            float v[8];
+            row8_values<XTYPE>(x[i], c, p.K, v);
+            if (c < steps * 64u) *(uint2 *)(lds + (size_t)m * p.pitch + c) = quantize8(v, finite, up, inv);
+        }
+    } else {
+        for (uint32_t i = threadIdx.x; i < p.M * steps * 4u; i += THIN_WAVES * 64) {
+            const uint32_t m = i / (steps * 4u), c = i % (steps * 4u) * 16u;
+            *(v4i32 *)(lds + (size_t)m * p.pitch + c) = thin_load((const int8_t *)p.a + (int64_t)m * p.ld_a, c, p.K);
+        }
+        if (threadIdx.x < p.M) scales[threadIdx.x] = p.sa[threadIdx.x];
+    }
+    __syncthreads();
+
+    v4i32 acc[MI][NB];
+#pragma unroll
+    for (int i = 0; i < MI; i++)
+#pragma unroll
+        for (int j = 0; j < NB; j++) acc[i][j] = v4i32{0, 0, 0, 0};
+    const auto a_at = [&](int i, uint32_t step) {
+        return i * 16 + r < p.M ? *(const v4i32 *)(lds + (size_t)(i * 16 + r) * p.pitch + step * 64u + g * 16u) : v4i32{0, 0, 0, 0};
+    };
+    for (uint32_t s0 = begin; s0 < whole; s0 += DEPTH)
+#pragma unroll
+        for (int d = 0; d < DEPTH; d++) {
+            const uint32_t s = s0 + d;
+            if (s >= whole) break;
+            v4i32 fa[MI];
+#pragma unroll
+            for (int i = 0; i < MI; i++) fa[i] = a_at(i, s);
+#pragma unroll
+            for (int j = 0; j < NB; j++) {
+#pragma unroll
+                for (int i = 0; i < MI; i++) acc[i][j] = slz_mma<SLZ_EL_I8>(b_value(j, ahead[d][j], behind[d][j]), fa[i], acc[i][j]);
+                if (s + DEPTH < whole) b_load(j, s + DEPTH, ahead[d][j], behind[d][j]);
+            }
+        }
+    if (whole < end)
+#pragma unroll
+        for (int j = 0; j < NB; j++) {
+            const v4i32 last = thin_load((const int8_t *)row[j] + shift[j] - g * 16u, whole * 64u + g * 16u, p.K);
+#pragma unroll
+            for (int i = 0; i < MI; i++) acc[i][j] = slz_mma<SLZ_EL_I8>(last, a_at(i, whole), acc[i][j]);
+        }
+    __syncthreads();
+    int *sums = (int *)lds;                            // [wave][row of a][row of b]
+#pragma unroll
+    for (int i = 0; i < MI; i++)
+#pragma unroll
+        for (int j = 0; j < NB; j++) *(v4i32 *)(sums + ((wave * MI + i) * 16 + r) * (NB * 16) + j * 16 + g * 4) = acc[i][j];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < MI * 16 * NB * 16; i += THIN_WAVES * 64) {
+        const uint32_t m = i / (NB * 16), n = n0 + i % (NB * 16);
+        if (m >= p.M || n >= p.N) continue;
+        int sum = 0;
+#pragma unroll
+        for (int w = 0; w < THIN_WAVES; w++) sum += sums[w * (MI * 16 * NB * 16) + i];
+        slz_put(p.y, p.type, (size_t)m * p.ld_y + n, (float)sum * (scales[m] * p.sb[n]));
+    }
+}
+
+// where it is taken: few rows that fit the shared memory
+static uint32_t thin_pitch(uint32_t k) { return (k + 63u) / 64u * 64u + 16u; }
+static bool thin_takes(const slz_i8_shape *sh, const int8_t *b) {
+    if (sh->m > THIN_MAX_ROWS || sh->k == 0 || (size_t)sh->m * thin_pitch(sh->k) > THIN_LDS) return false;
+    return sh->m <= 16 || sh->n <= 4096 || !slz_in_place(b, sh->k, sh->ld_b, 1);
+}
+// x is quantised by every workgroup as long as that is little work for all of them
+static bool thin_quantizes(uint32_t m, uint32_t n, uint32_t k) {
+    if ((size_t)m * k > (n <= 2048 ? 32768 : 8192)) return false;
+    const uint32_t per_row = m >= THIN_WAVES ? 1u : m > 2 ? 2u : m == 2 ? 4u : 8u, rows = (m * per_row + THIN_WAVES - 1) / THIN_WAVES;
+    return rows * ((k + per_row * 512u - 1) / (per_row * 512u)) <= THIN_SLOTS;
+}
+
+template <int MI, int NB> static void thin_launch(const thin_args &p, int x_type, size_t bytes, hipStream_t s) {
+    const auto k = x_type < 0 ? k_thin_i8<MI, NB, -1> : x_type == SLZ_F32 ? k_thin_i8<MI, NB, SLZ_F32> : x_type == SLZ_BF16 ? k_thin_i8<MI, NB, SLZ_BF16> : k_thin_i8<MI, NB, SLZ_F16>;
+    hipLaunchKernelGGL(k, dim3((p.N + 16 * NB - 1) / (16 * NB)), dim3(THIN_WAVES * 64), bytes, s, p);
+}
+// x_type: of a where it is x, or -1
+static int thin_product(const thin_args &p, int x_type, hipStream_t s) {
+    const uint32_t mi = p.M > 16 ? 2 : 1, nb = p.N >= THIN_WIDE ? 2 : 1;
+    const size_t a = (size_t)p.M * p.pitch, sums = (size_t)THIN_WAVES * mi * nb * 1024, bytes = a > sums ? a : sums;
+    if (mi == 1) nb == 1 ? thin_launch<1, 1>(p, x_type, bytes, s) : thin_launch<1, 2>(p, x_type, bytes, s);
+    else nb == 1 ? thin_launch<2, 1>(p, x_type, bytes, s) : thin_launch<2, 2>(p, x_type, bytes, s);
+    return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
 }
 
 // ---- product ---------------------------------------------------------------------------------------------------------------------------
@@ -70,7 +373,7 @@ extern "C" int slz_matmul_i8_workspace(const slz_i8_shape *sh, const int8_t *a, 
     const int rc = i8_check(sh);
     if (rc != SLZ_OK) return rc;
     if (!bytes) return SLZ_E_INVALID_ARG;
-    *bytes = slz_operand_i8_bytes(a, sh->m, sh->k, sh->ld_a) + slz_operand_i8_bytes(b, sh->n, sh->k, sh->ld_b) + slz_ranges_bytes(i8_choice(sh), sh->m, sh->n);
+    *bytes = thin_takes(sh, b) ? 0 : slz_operand_i8_bytes(a, sh->m, sh->k, sh->ld_a) + slz_operand_i8_bytes(b, sh->n, sh->k, sh->ld_b) + slz_ranges_bytes(i8_choice(sh), sh->m, sh->n);
     return SLZ_OK;
 }
 
@@ -88,11 +391,15 @@ extern "C" int slz_matmul_i8(const slz_i8_shape *sh, const int8_t *a, const floa
     int rc = i8_checks(sh, a, 1, b, sb, y);
     if (rc == SLZ_OK) rc = slz_matrix_check(sa, sh->m, 1, 1, 4);
     if (rc != SLZ_OK || sh->m == 0 || sh->n == 0) return rc;
+    if (thin_takes(sh, b))
+        return thin_product({a, sa, sh->type, sh->ld_a, b, sb, sh->ld_b, y, sh->ld_y, sh->m, sh->n, sh->k, thin_pitch(sh->k)}, -1, (hipStream_t)stream);
     const size_t for_a = slz_operand_i8_bytes(a, sh->m, sh->k, sh->ld_a), for_b = slz_operand_i8_bytes(b, sh->n, sh->k, sh->ld_b);
     if (!slz_ws_ok(ws, ws_bytes, for_a + for_b + slz_ranges_bytes(i8_choice(sh), sh->m, sh->n))) return SLZ_E_INVALID_ARG;
     hipStream_t s = (hipStream_t)stream;
-    const slz_operand oa = slz_operand_i8_of(a, sh->m, sh->k, sh->ld_a, (char *)ws, s);
-    const slz_operand ob = slz_operand_i8_of(b, sh->n, sh->k, sh->ld_b, (char *)ws + for_a, s);
+    slz_layouts jobs = {};
+    const slz_operand oa = slz_operand_i8_of(a, sh->m, sh->k, sh->ld_a, (char *)ws, jobs);
+    const slz_operand ob = slz_operand_i8_of(b, sh->n, sh->k, sh->ld_b, (char *)ws + for_a, jobs);
+    slz_layout_run(jobs, s);
     rc = i8_product(sh, oa, sa, ob, sb, y, (char *)ws + for_a + for_b, s);
     if (rc != SLZ_OK) return rc;
     SLZ_HIP(hipGetLastError());
@@ -109,6 +416,7 @@ static linear_plan plan_linear(const slz_i8_shape *sh, const int8_t *b) {
     P.b = P.scale + up256((size_t)sh->m * 4);
     P.ranges = P.b + slz_operand_i8_bytes(b, sh->n, sh->k, sh->ld_b);
     P.total = P.ranges + slz_ranges_bytes(i8_choice(sh), sh->m, sh->n);
+    if (thin_takes(sh, b)) P.total = thin_quantizes(sh->m, sh->n, sh->k) ? 0 : P.b;
     return P;
 }
 extern "C" int slz_linear_i8_workspace(const slz_i8_shape *sh, const void *x, const int8_t *b, size_t *bytes) {
@@ -125,13 +433,20 @@ extern "C" int slz_linear_i8(const slz_i8_shape *sh, const void *x, const int8_t
     const linear_plan P = plan_linear(sh, b);
     if (!slz_ws_ok(ws, ws_bytes, P.total)) return SLZ_E_INVALID_ARG;
     hipStream_t s = (hipStream_t)stream;
+    const bool thin = thin_takes(sh, b);
+    const uint32_t pitch = thin_pitch(sh->k);
+    if (thin && thin_quantizes(sh->m, sh->n, sh->k))
+        return thin_product({x, nullptr, sh->type, sh->ld_a, b, sb, sh->ld_b, y, sh->ld_y, sh->m, sh->n, sh->k, pitch}, sh->type, s);
     int8_t *q = (int8_t *)ws + P.q;
     float *sa = (float *)((char *)ws + P.scale);
     // a row's last 16 entries may end with whatever was there: b's are zero in those places
-    rc = slz_quantize_i8(x, sh->type, sh->m, sh->k, sh->ld_a, q, P.ld_q, sa, stream);
+    rc = quantize_rows(x, sh->type, sh->m, sh->k, sh->ld_a, q, P.ld_q, sa, s);
     if (rc != SLZ_OK) return rc;
+    if (thin) return thin_product({q, sa, sh->type, P.ld_q, b, sb, sh->ld_b, y, sh->ld_y, sh->m, sh->n, sh->k, pitch}, -1, s);
     const slz_operand oa{(const char *)q, P.ld_q, 0, 1, 3};
-    const slz_operand ob = slz_operand_i8_of(b, sh->n, sh->k, sh->ld_b, (char *)ws + P.b, s);
+    slz_layouts jobs = {};
+    const slz_operand ob = slz_operand_i8_of(b, sh->n, sh->k, sh->ld_b, (char *)ws + P.b, jobs);
+    slz_layout_run(jobs, s);
     return i8_product(sh, oa, sa, ob, sb, y, (char *)ws + P.ranges, s);
 }
 
@@ -218,7 +533,9 @@ extern "C" int slz_matmul_i8_grad(const slz_i8_shape *sh, const void *dy, const 
     if (!slz_ws_ok(ws, ws_bytes, P.total)) return SLZ_E_INVALID_ARG;
     hipStream_t s = (hipStream_t)stream;
     char *w = (char *)ws;
-    const slz_operand d = slz_operand_of(dy, sh->type, sh->m, sh->n, sh->ld_y, w + P.dy, s);
+    slz_layouts jobs = {};
+    const slz_operand d = slz_operand_of(dy, sh->type, sh->m, sh->n, sh->ld_y, w + P.dy, jobs);
+    slz_layout_run(jobs, s);
     if (da && sh->m) rc = grad_product(sh, d, false, sh->m, b, sh->ld_b, sb, sh->n, da, ld_da, w + P.values[1], (float *)(w + P.unit), w + P.ranges, P, s);
     if (rc == SLZ_OK && db && sh->n) rc = grad_product(sh, d, true, sh->n, a, sh->ld_a, sa, sh->m, db, ld_db, w + P.values[0], (float *)(w + P.unit) + 1, w + P.ranges, P, s);
     if (rc != SLZ_OK) return rc;

@@ -137,6 +137,177 @@ struct ce_grad_epi {
     }
 };
 
+// ---- few classes ---------------------------------------------------------------------------------------------------------------------------
+// A classifier's head: w fits a workgroup's shared memory in 32 bits, a wave computes all of a token's z, and the whole call is one launch (the
+// gradient of many tokens: two), where the tiled products would be four to eight.  Taken by the sizes of w alone, so that a token's loss does not
+// depend on how many there are.
+#define FEW_CLASSES 32
+#define FEW_WEIGHTS 8192
+#define FEW_THREADS 1024
+#define FEW_TOKENS_LDS 16384         // entries of h that a workgroup holds
+#define FEW_BLOCKS 256
+struct few_args {
+    const void *h, *w;
+    int type;
+    int64_t ld_h, ld_w;
+    const int64_t *labels;
+    int64_t ignore;
+    uint32_t tokens, inner, vocab;
+};
+// z of a token in every lane; h: its entries in shared memory
+template <int C> __device__ __forceinline__ void few_logits(const float *h, const float *w, uint32_t inner, uint32_t vocab, uint32_t lane, float (&z)[C]) {
+#pragma unroll
+    for (int v = 0; v < C; v++) z[v] = 0.0f;
+    for (uint32_t d = lane; d < inner; d += 64) {
+        const float x = h[d];
+#pragma unroll
+        for (int v = 0; v < C; v++)
+            if ((uint32_t)v < vocab) z[v] = __builtin_fmaf(x, w[v * inner + d], z[v]);
+    }
+#pragma unroll
+    for (int v = 0; v < C; v++)
+        if ((uint32_t)v < vocab) z[v] = slz_wave_sum(z[v]);
+}
+template <int C> __device__ __forceinline__ float few_lse(const float (&z)[C], uint32_t vocab) {
+    float top = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < C; v++) top = (uint32_t)v < vocab ? fmaxf(top, z[v]) : top;
+    const float from = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+    for (int v = 0; v < C; v++) sum += (uint32_t)v < vocab ? expf(z[v] - from) : 0.0f;
+    return top + logf(sum);
+}
+__device__ __forceinline__ void few_weights(const few_args &p, float *w) {
+    for (uint32_t i = threadIdx.x; i < p.vocab * p.inner; i += FEW_THREADS) w[i] = slz_get(p.w, p.type, (size_t)(i / p.inner) * p.ld_w + i % p.inner);
+}
+__device__ __forceinline__ void few_tokens(const few_args &p, uint32_t first, uint32_t count, float *h) {
+    for (uint32_t i = threadIdx.x; i < count * p.inner; i += FEW_THREADS) h[i] = slz_get(p.h, p.type, (size_t)(first + i / p.inner) * p.ld_h + i % p.inner);
+}
+
+// `group` tokens at a time
+template <int C>
+__global__ void __launch_bounds__(FEW_THREADS) k_few_loss(const few_args p, uint32_t group, float *__restrict__ loss, float *__restrict__ lse) {
+    extern __shared__ __attribute__((aligned(16))) float few[];
+    float *w = few, *h = few + p.vocab * p.inner;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    few_weights(p, w);
+    for (uint32_t first = blockIdx.x * group; first < p.tokens; first += gridDim.x * group) {
+        const uint32_t count = min(group, p.tokens - first);
+        few_tokens(p, first, count, h);
+        __syncthreads();
+        for (uint32_t t = wave; t < count; t += FEW_THREADS / 64) {
+            float z[C], at_label = 0.0f;
+            few_logits<C>(h + t * p.inner, w, p.inner, p.vocab, lane, z);
+            const float l = few_lse<C>(z, p.vocab);
+            const int64_t label = p.labels[first + t];
+#pragma unroll
+            for (int v = 0; v < C; v++) at_label = label == v ? z[v] : at_label;
+            if (lane == 0) {
+                lse[first + t] = l;
+                loss[first + t] = label == p.ignore ? 0.0f : label < 0 || label >= (int64_t)p.vocab ? __builtin_nanf("") : l - at_label;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// dw: the sums of each workgroup's tokens go to `part` [workgroup][vocab][inner], or with one workgroup to dw
+template <int C>
+__global__ void __launch_bounds__(FEW_THREADS)
+k_few_grad(const few_args p, uint32_t group, const float *__restrict__ lse, const float *__restrict__ dloss, void *__restrict__ dh, int64_t ld_dh,
+           void *__restrict__ dw, int64_t ld_dw, float *__restrict__ part) {
+    extern __shared__ __attribute__((aligned(16))) float few[];
+    const uint32_t weights = p.vocab * p.inner;
+    float *w = few, *g = w + weights, *h = g + group * p.vocab;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    constexpr int OWN = FEW_WEIGHTS / FEW_THREADS;                  // entries of dw of a thread
+    float sum[OWN];
+    uint32_t own_v[OWN], own_d[OWN];
+#pragma unroll
+    for (int i = 0; i < OWN; i++) {
+        const uint32_t e = i * FEW_THREADS + threadIdx.x;
+        sum[i] = 0.0f;
+        own_v[i] = e < weights ? e / p.inner : 0u;
+        own_d[i] = e < weights ? e % p.inner : 0u;
+    }
+    few_weights(p, w);
+    for (uint32_t first = blockIdx.x * group; first < p.tokens; first += gridDim.x * group) {
+        const uint32_t count = min(group, p.tokens - first);
+        few_tokens(p, first, count, h);
+        __syncthreads();
+        for (uint32_t t = wave; t < count; t += FEW_THREADS / 64) {
+            float z[C];
+            few_logits<C>(h + t * p.inner, w, p.inner, p.vocab, lane, z);
+            const int64_t label = p.labels[first + t];
+            const float l = lse[first + t], by = label < 0 || label >= (int64_t)p.vocab ? __builtin_nanf("") : dloss[first + t];
+#pragma unroll
+            for (int v = 0; v < C; v++)
+                if ((uint32_t)v < p.vocab) {
+                    z[v] = label == p.ignore ? 0.0f : (expf(z[v] - l) - (label == v ? 1.0f : 0.0f)) * by;
+                    if (lane == 0) g[t * p.vocab + v] = z[v];
+                }
+            for (uint32_t d = lane; d < p.inner; d += 64) {
+                float x = 0.0f;
+#pragma unroll
+                for (int v = 0; v < C; v++)
+                    if ((uint32_t)v < p.vocab) x = __builtin_fmaf(z[v], w[v * p.inner + d], x);
+                slz_put(dh, p.type, (size_t)(first + t) * ld_dh + d, x);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < OWN; i++)
+            if ((uint32_t)i * FEW_THREADS < weights)
+                for (uint32_t t = 0; t < count; t++) sum[i] = __builtin_fmaf(g[t * p.vocab + own_v[i]], h[t * p.inner + own_d[i]], sum[i]);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < OWN; i++) {
+        const uint32_t e = i * FEW_THREADS + threadIdx.x;
+        if (e >= weights) continue;
+        if (part) part[(size_t)blockIdx.x * weights + e] = sum[i];
+        else slz_put(dw, p.type, (size_t)own_v[i] * ld_dw + own_d[i], sum[i]);
+    }
+}
+__global__ void __launch_bounds__(256)
+k_few_join(const float *__restrict__ part, uint32_t blocks, uint32_t vocab, uint32_t inner, void *__restrict__ dw, int type, int64_t ld_dw) {
+    const uint32_t e = blockIdx.x * 256 + threadIdx.x, weights = vocab * inner;
+    if (e >= weights) return;
+    float sum = 0.0f;
+    for (uint32_t b = 0; b < blocks; b++) sum += part[(size_t)b * weights + e];
+    slz_put(dw, type, (size_t)(e / inner) * ld_dw + e % inner, sum);
+}
+
+static bool few_takes(const slz_ce_shape *sh) { return sh->vocab <= FEW_CLASSES && (uint64_t)sh->vocab * sh->inner <= FEW_WEIGHTS; }
+static uint32_t few_group(const slz_ce_shape *sh) {
+    const uint32_t fit = FEW_TOKENS_LDS / sh->inner;
+    return fit < 1 ? 1 : fit > 32 ? 32 : fit;
+}
+static uint32_t few_blocks(const slz_ce_shape *sh) {
+    const uint32_t n = (sh->tokens + few_group(sh) - 1) / few_group(sh);
+    return n < 1 ? 1 : n > FEW_BLOCKS ? FEW_BLOCKS : n;
+}
+static size_t few_workspace(const slz_ce_shape *sh) { return few_blocks(sh) == 1 ? 0 : up256((size_t)few_blocks(sh) * sh->vocab * sh->inner * 4); }
+static few_args few_of(const slz_ce_shape *sh, const void *h, const void *w, const int64_t *labels) {
+    return {h, w, sh->type, sh->ld_h, sh->ld_w, labels, sh->ignore_index, sh->tokens, sh->inner, sh->vocab};
+}
+static int few_loss(const slz_ce_shape *sh, const void *h, const void *w, const int64_t *labels, float *loss, float *lse, hipStream_t s) {
+    const uint32_t group = few_group(sh);
+    const auto k = sh->vocab <= 4 ? k_few_loss<4> : sh->vocab <= 16 ? k_few_loss<16> : k_few_loss<32>;
+    hipLaunchKernelGGL(k, dim3(few_blocks(sh)), dim3(FEW_THREADS), (sh->vocab + group) * sh->inner * 4, s, few_of(sh, h, w, labels), group, loss, lse);
+    return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
+}
+static int few_grad(const slz_ce_shape *sh, const void *h, const void *w, const int64_t *labels, const float *lse, const float *dloss, void *dh, void *dw,
+                    float *part, hipStream_t s) {
+    const uint32_t group = few_group(sh), blocks = few_blocks(sh);
+    const auto k = sh->vocab <= 4 ? k_few_grad<4> : sh->vocab <= 16 ? k_few_grad<16> : k_few_grad<32>;
+    hipLaunchKernelGGL(k, dim3(blocks), dim3(FEW_THREADS), ((sh->vocab + group) * sh->inner + group * sh->vocab) * 4, s, few_of(sh, h, w, labels), group, lse,
+                       dloss, dh, sh->ld_dh, dw, sh->ld_dw, blocks > 1 ? part : nullptr);
+    if (blocks > 1)
+        hipLaunchKernelGGL(k_few_join, dim3((sh->vocab * sh->inner + 255) / 256), dim3(256), 0, s, part, blocks, sh->vocab, sh->inner, dw, sh->type, sh->ld_dw);
+    return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
+}
+
 struct ce_plan {
     uint32_t words;                  // of a piece
     size_t h, w, pairs, label_z, g, dh, unit, total;
@@ -186,7 +357,7 @@ static int ce_check(const slz_ce_shape *sh, const void *h, const void *w, const 
 static int ce_workspace(const slz_ce_shape *sh, const void *h, const void *w, bool grad, size_t *bytes) {
     if (!sh || !bytes || !slz_type_ok(sh->type) || sh->inner == 0 || sh->vocab == 0) return SLZ_E_INVALID_ARG;
     if (sh->tokens > SLZ_CLEAR_MAX_LEN || sh->vocab > SLZ_CLEAR_MAX_LEN || sh->inner > SLZ_CLEAR_MAX_LD) return SLZ_E_TOO_LARGE;
-    *bytes = plan_ce(sh, h, w, grad).total;
+    *bytes = few_takes(sh) ? (grad ? few_workspace(sh) : 0) : plan_ce(sh, h, w, grad).total;
     return SLZ_OK;
 }
 extern "C" int slz_linear_ce_workspace(const slz_ce_shape *sh, const void *h, const void *w, size_t *bytes) { return ce_workspace(sh, h, w, false, bytes); }
@@ -207,16 +378,20 @@ extern "C" int slz_linear_ce(const slz_ce_shape *sh, const void *h, const void *
     if (rc == SLZ_OK) rc = slz_matrix_check(loss, sh->tokens, 1, 1, 4);
     if (rc == SLZ_OK) rc = slz_matrix_check(lse, sh->tokens, 1, 1, 4);
     if (rc != SLZ_OK || sh->tokens == 0) return rc;
+    if (few_takes(sh)) return few_loss(sh, h, w, labels, loss, lse, (hipStream_t)stream);
     const ce_plan P = plan_ce(sh, h, w, false);
     if (!slz_ws_ok(ws, ws_bytes, P.total)) return SLZ_E_INVALID_ARG;
     hipStream_t s = (hipStream_t)stream;
     char *base = (char *)ws;
     float2 *pairs = (float2 *)(base + P.pairs);
     float *label_z = (float *)(base + P.label_z);
-    const slz_operand oh = slz_operand_of(h, sh->type, sh->tokens, sh->inner, sh->ld_h, base + P.h, s);
+    slz_layouts jobs = {};
+    const slz_operand oh = slz_operand_of(h, sh->type, sh->tokens, sh->inner, sh->ld_h, base + P.h, jobs);
     for (uint32_t v = 0; v < sh->vocab; v += P.words) {
         const uint32_t words = sh->vocab - v < P.words ? sh->vocab - v : P.words;
-        const slz_operand ow = slz_operand_of(rows_of(w, sh, v), sh->type, words, sh->inner, sh->ld_w, base + P.w, s);
+        const slz_operand ow = slz_operand_of(rows_of(w, sh, v), sh->type, words, sh->inner, sh->ld_w, base + P.w, jobs);
+        slz_layout_run(jobs, s);                       // with h before the first piece
+        jobs.count = 0;
         const ce_lse_epi epi{pairs, label_z, labels, v};
         rc = ce_logits(sh->type, slz_gemm_of(oh, ow, sh->tokens, words, sh->inner), epi, P.side, s);
         if (rc != SLZ_OK) return rc;
@@ -246,6 +421,10 @@ extern "C" int slz_linear_ce_grad(const slz_ce_shape *sh, const void *h, const v
     if (rc == SLZ_OK) rc = slz_matrix_check(dh, sh->tokens, sh->inner, sh->ld_dh, slz_type_bytes(sh->type));
     if (rc == SLZ_OK) rc = slz_matrix_check(dw, sh->vocab, sh->inner, sh->ld_dw, slz_type_bytes(sh->type));
     if (rc != SLZ_OK) return rc;
+    if (few_takes(sh)) {
+        if (!slz_ws_ok(ws, ws_bytes, few_workspace(sh))) return SLZ_E_INVALID_ARG;
+        return few_grad(sh, h, w, labels, lse, dloss, dh, dw, (float *)ws, (hipStream_t)stream);
+    }
     const ce_plan P = plan_ce(sh, h, w, true);
     if (!slz_ws_ok(ws, ws_bytes, P.total)) return SLZ_E_INVALID_ARG;
     hipStream_t s = (hipStream_t)stream;
@@ -253,11 +432,14 @@ extern "C" int slz_linear_ce_grad(const slz_ce_shape *sh, const void *h, const v
     float *dh_sum = (float *)(base + P.dh), *unit = (float *)(base + P.unit);
     if (sh->type == SLZ_F16) slz_unit_of(dloss, sh->tokens, unit, s);
     const slz_times_unit f{sh->type == SLZ_F16 ? unit : nullptr, 1.0f / CE_F16_UP};
-    const slz_operand oh = slz_operand_of(h, sh->type, sh->tokens, sh->inner, sh->ld_h, base + P.h, s);
+    slz_layouts jobs = {};
+    const slz_operand oh = slz_operand_of(h, sh->type, sh->tokens, sh->inner, sh->ld_h, base + P.h, jobs);
     const slz_operand g{base + P.g, (int64_t)P.g_row, (int64_t)up256((size_t)sh->tokens * P.g_row), oh.pieces, oh.element};
     for (uint32_t v = 0; v < sh->vocab; v += P.words) {
         const uint32_t words = sh->vocab - v < P.words ? sh->vocab - v : P.words;
-        const slz_operand ow = slz_operand_of(rows_of(w, sh, v), sh->type, words, sh->inner, sh->ld_w, base + P.w, s);
+        const slz_operand ow = slz_operand_of(rows_of(w, sh, v), sh->type, words, sh->inner, sh->ld_w, base + P.w, jobs);
+        slz_layout_run(jobs, s);                       // with h before the first piece
+        jobs.count = 0;
         const ce_grad_epi epi{base + P.g, g.ld, g.piece, sh->type, lse, dloss, unit, labels, sh->ignore_index, v, sh->vocab};
         rc = ce_logits(sh->type, slz_gemm_of(oh, ow, sh->tokens, words, sh->inner), epi, P.side, s);
         if (rc == SLZ_OK)

@@ -71,8 +71,8 @@ def test_products_of_8_bit_integers_refuse():
     assert L.slz_linear_i8(None, P, P, P, P, P, 1 << 30, None) == INVALID
     assert L.slz_matmul_i8_workspace(None, P, P, ref(need)) == INVALID
     assert L.slz_matmul_i8_workspace(ref(sh), P, P, None) == INVALID
-    # a workspace that is missing, too small or misaligned, where one is needed (rows of 31 entries)
-    odd = SlzI8Shape(**{**ok, "k": 31})
+    # a workspace that is missing, too small or misaligned, where one is needed (many rows, of 31 entries)
+    odd = SlzI8Shape(**{**ok, "m": 64, "k": 31})
     odd.ld_a = odd.ld_b = 31
     assert L.slz_matmul_i8_workspace(ref(odd), P, P, ref(need)) == 0 and need.value > 0
     for ws, size in ((None, 1 << 30), (P, need.value - 1), (P + 128, need.value)):
