@@ -36,8 +36,8 @@ extern "C" {
 
 /* ---- products of 8-bit integers ------------------------------------------------------------------------------------------ */
 
-/* Row i of x [rows][cols] to 8 bits: top = max_k |x_ik|, scale_i = top / 127, q_ik = rint(x_ik (127 / top)) (ties to even), in
- * 32-bit floating point; a row of zeros has scale 0 and zeros, a row with an infinity or NaN has scale NaN and zeros. */
+/* Row i of x [rows][cols] to 8 bits: top = max_k |x_ik|, scale_i = top / 127, q_ik = rint(x_ik ((1 / top) 127)) (ties to
+ * even), each operation in 32-bit floating point; a row of zeros has scale 0 and zeros, a row with an infinity or NaN has scale NaN and zeros. */
 int slz_quantize_i8(const void *x_dev, int type, uint32_t rows, uint32_t cols, int64_t ld_x, int8_t *q_dev, int64_t ld_q,
                     float *scale_dev, void *hip_stream);
 

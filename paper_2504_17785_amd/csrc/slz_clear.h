@@ -56,6 +56,50 @@ __device__ __forceinline__ void slz_split3(float x, uint16_t (&q)[3]) {
     q[1] = (uint16_t)(__builtin_bit_cast(uint32_t, l) >> 16);
     q[2] = (uint16_t)(__builtin_bit_cast(uint32_t, r - l) >> 16);
 }
+typedef int v4i32 __attribute__((ext_vector_type(4)));
+// Eight elements of a row of `cols` at c (a multiple of 8), zeros past its end; the row may begin at any address.  Where the row ends inside,
+// its last eight are read and moved down.  In two parts, so that several loads are under way before the first is looked at.
+typedef v4i32 v4i32_any __attribute__((aligned(1)));
+template <int TYPE> struct row8 { v4i32 w[TYPE == SLZ_F32 ? 2 : 1]; };
+template <int TYPE> __device__ __forceinline__ row8<TYPE> row8_load(const void *x, size_t row, uint32_t c, uint32_t cols) {
+    row8<TYPE> q;
+    if (cols < 8u) {                                   // all of it, in the first threads
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = c + i < cols ? slz_get(x, TYPE, row + c + i) : 0.0f;
+        if constexpr (TYPE == SLZ_F32) {
+            q.w[0] = v4i32{__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
+            q.w[1] = v4i32{__float_as_int(v[4]), __float_as_int(v[5]), __float_as_int(v[6]), __float_as_int(v[7])};
+        } else {
+            uint32_t h[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) h[i] = slz_half(v[2 * i], TYPE) | ((uint32_t)slz_half(v[2 * i + 1], TYPE) << 16);
+            q.w[0] = v4i32{(int)h[0], (int)h[1], (int)h[2], (int)h[3]};
+        }
+        return q;
+    }
+    const uint32_t from = min(c, cols - 8u);
+    const v4i32_any *p = (const v4i32_any *)((const char *)x + (row + from) * slz_type_bytes(TYPE));
+    q.w[0] = p[0];
+    if constexpr (TYPE == SLZ_F32) q.w[1] = p[1];
+    return q;
+}
+template <int TYPE> __device__ __forceinline__ void row8_values(const row8<TYPE> &q, uint32_t c, uint32_t cols, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        if constexpr (TYPE == SLZ_F32) v[i] = __int_as_float(q.w[i / 4][i % 4]);
+        else {
+            const uint16_t h = (uint16_t)((uint32_t)q.w[0][i / 2] >> (16 * (i & 1)));
+            v[i] = TYPE == SLZ_BF16 ? slz_bf16_to_f32(h) : slz_f16_to_f32(h);
+        }
+    }
+    if (c + 8u <= cols) return;
+    const uint32_t gone = c >= cols ? 8u : cols < 8u ? 0u : c + 8u - cols;
+#pragma unroll
+    for (uint32_t b = 1; b < 16; b <<= 1)
+#pragma unroll
+        for (uint32_t i = 0; i < 8; i++) v[i] = gone & b ? (i + b < 8 ? v[(i + b) % 8] : 0.0f) : v[i];
+}
 // C consecutive values v of one row at p[0 .. C), of which `valid` exist; aligned: p is a multiple of C elements
 template <int C> __device__ __forceinline__ void slz_put_run(void *p, int type, const float (&v)[C], uint32_t valid, bool aligned) {
     static_assert(C % 4 == 0, "");
@@ -80,6 +124,17 @@ template <int C> __device__ __forceinline__ void slz_put_run(void *p, int type, 
 #pragma unroll
     for (int i = 0; i < C; i++)
         if ((uint32_t)i < valid) slz_put(p, type, i, v[i]);
+}
+// i / by and the rest; in 32 bits where that holds i
+__device__ __forceinline__ size_t slz_divide(size_t i, uint32_t by, bool narrow, uint32_t &rest) {
+    if (narrow) {
+        const uint32_t q = (uint32_t)i / by;
+        rest = (uint32_t)i - q * by;
+        return q;
+    }
+    const size_t q = i / by;
+    rest = (uint32_t)(i - q * by);
+    return q;
 }
 // maximum over a wave, in every lane: over 16 lanes by lane permutations within the row, then over the four rows
 template <int CONTROL> __device__ __forceinline__ float slz_dpp_max(float x) {

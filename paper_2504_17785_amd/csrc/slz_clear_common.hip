@@ -20,8 +20,9 @@ __global__ void __launch_bounds__(256) k_layout(const slz_layouts jobs) {
     const uint32_t per_row = j.ld_out / 16u;
     const size_t total = (size_t)j.rows * per_row;
     for (size_t g = (size_t)blockIdx.x * 256 + threadIdx.x; g < total; g += (size_t)gridDim.x * 256) {
-        const size_t r = g / per_row;
-        const uint32_t at = (uint32_t)(g % per_row) * 16u;
+        uint32_t at;
+        const size_t r = slz_divide(g, per_row, total <= 0xffffffffu, at);
+        at *= 16u;
         char *to = j.out + r * j.ld_out + at;
         if (j.bytes == 1) align_16<1>(j, r, at, to);
         else if (j.bytes == 2) align_16<2>(j, r, at / 2, to);

@@ -19,7 +19,6 @@
 #include <utility>
 
 typedef float v4f __attribute__((ext_vector_type(4)));
-typedef int v4i32 __attribute__((ext_vector_type(4)));
 typedef short v4s16 __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
@@ -122,11 +121,16 @@ template <bool ROWS_ARE_K, int T, int WAVES, int SPREAD> struct slz_tile {
     }
 };
 
-// Tile of a workgroup: the eight XCDs take workgroups in turn and each has an L2 of its own, so each gets a run of
-// consecutive tiles; within the order, eight tile rows go along the columns together.
-__device__ __forceinline__ void slz_tile_of(uint32_t x, uint32_t tiles_m, uint32_t tiles_n, uint32_t symmetric, uint32_t &tm, uint32_t &tn) {
-    const uint32_t total = gridDim.x, even = total & ~7u;
+// Tile, range of k and matrix of a workgroup.  The eight XCDs take workgroups in turn and each has an L2 of its own, so each gets a run of consecutive
+// tiles, all of a range and of a matrix before the next; within the order, eight tile rows go along the columns together.
+__device__ __forceinline__ void slz_tile_of(uint32_t tiles_m, uint32_t tiles_n, uint32_t symmetric, uint32_t &tm, uint32_t &tn, uint32_t &range, uint32_t &batch) {
+    uint32_t x = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z);
+    const uint32_t total = gridDim.x * gridDim.y * gridDim.z, even = total & ~7u;
     if (x < even) x = (x & 7u) * (even >> 3) + (x >> 3);
+    const uint32_t which = x / gridDim.x;
+    x -= which * gridDim.x;
+    batch = which / gridDim.y;
+    range = which - batch * gridDim.y;
     if (symmetric) {                                   // row tm has tm + 1 tiles
         uint32_t t = (uint32_t)((__builtin_sqrtf(8.0f * (float)x + 1.0f) - 1.0f) * 0.5f);
         while (t * (t + 1u) / 2u > x) t--;
@@ -159,9 +163,8 @@ __global__ void __launch_bounds__(WM *WN * 64) k_gemm(const slz_gemm p, const EP
     __shared__ __attribute__((aligned(1024))) char lds[2][tile_a::BYTES + tile_b::BYTES];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wave_m = wave / WN, wave_n = wave % WN;
-    uint32_t tm, tn;
-    slz_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, p.symmetric, tm, tn);
-    const uint32_t batch = blockIdx.z, range = blockIdx.y;
+    uint32_t tm, tn, range, batch;
+    slz_tile_of(p.tiles_m, p.tiles_n, p.symmetric, tm, tn, range, batch);
     const uint32_t steps_k = (p.K + KS - 1) / KS, steps = steps_k * p.pairs;
     const uint32_t begin = range * p.range, end = min(steps, begin + p.range);
 
@@ -237,6 +240,7 @@ template <class F> struct slz_store_epi {
     int64_t ld, batch_stride;        // elements
     uint32_t aligned;                // rows begin at multiples of 16 bytes
     F f;
+    static constexpr bool any_side = true;
     template <int MI, int NI, bool RUN, int WM, int WN, class ACC>
     __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *) const {
         constexpr int C = RUN ? NI * 4 : 4, PARTS = RUN ? 1 : NI;
@@ -269,6 +273,7 @@ struct slz_times_unit {
 template <class T> struct slz_partial_epi {
     T *ws;
     uint32_t ld, batches, add;
+    static constexpr bool any_side = true;
     template <int MI, int NI, bool RUN, int WM, int WN, class ACC>
     __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *) const {
 #pragma unroll
@@ -303,25 +308,33 @@ __global__ void __launch_bounds__(256) k_join(const T *ws, uint32_t ranges, uint
 // ---- launches ----------------------------------------------------------------------------------------------------------------
 template <int TM_, int TN_, int WM_, int WN_> struct slz_tiling { static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_; };
 using slz_tiles_256 = slz_tiling<256, 256, 2, 4>;
+using slz_tiles_192 = slz_tiling<192, 192, 2, 4>;
 using slz_tiles_128 = slz_tiling<128, 128, 2, 2>;
 using slz_tiles_64 = slz_tiling<64, 64, 2, 2>;
 
-// Which tiling and how many ranges of k.  A step of 128 bytes of k takes a workgroup that has its compute unit to itself 1.6 (256 x 256), 0.7 (128)
-// and 0.33 us (64), and a full compute unit gives one every 1.6, 0.46 and 0.18 us: large tiles do 1.1 and 2.5 times the work of smaller
-// ones in the same time, small ones end sooner where there are few.  (8192^3 bf16: 1100, 1086, 645 TFLOP/s; 1024^3: 29, 14, 8 us.)  Ranges of k
-// cost a second launch that reads their sums.
+// Which tiling and how many ranges of k.  A step of 128 bytes of k takes a compute unit 1.5 us with a tile of 256 a side, 0.95 with one of 192, 0.62
+// with one of 128 and 0.88 with two at once, 0.33 with one of 64 and 0.18 for each of several (measured at 4096 deep: 3840^2 with 256: 99 us;
+// 2688^2 with 192: 63, with 128: 57; 768^2 with 256, 192, 128: 85, 58, 43).  Large tiles read less for each product, small ones fill the chip with less
+// and leave less of it idle at the end.  Ranges of k cost a second launch that reads their sums.
 struct slz_choice { uint32_t side, split; };
-static inline slz_choice slz_choose(uint32_t M, uint32_t N, uint32_t steps, uint32_t batches, bool symmetric, uint32_t most_ranges) {
-    static const struct { uint32_t side; double alone, full; } kinds[3] = {{256, 1.6, 1.6}, {128, 0.7, 0.46}, {64, 0.33, 0.18}};
+static inline double slz_step_us(uint32_t side, double tiles) {
+    const auto rounds = [&](double at_once) { return (double)(uint64_t)((tiles + at_once - 1) / at_once); };
+    if (side == 256) return rounds(256) * 1.5;
+    if (side == 192) return rounds(256) * 0.95;
+    if (side == 64) return rounds(256) * 0.18 > 0.33 ? rounds(256) * 0.18 : 0.33;
+    const double pairs = (double)(uint64_t)(tiles / 512), rest = tiles - pairs * 512;
+    return pairs * 0.88 + (rest > 256 ? 0.88 : rest > 0 ? 0.62 : 0.0);
+}
+static inline slz_choice slz_choose(uint32_t M, uint32_t N, uint32_t steps, uint32_t batches, bool symmetric, uint32_t most_ranges, bool any_side = true) {
     slz_choice best = {64, 1};
     double least = 1e30;
-    for (const auto &k : kinds) {
-        const double tm = (M + k.side - 1) / k.side, tn = (N + k.side - 1) / k.side, tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batches;
+    for (const uint32_t side : {256u, 192u, 128u, 64u}) {
+        if (side == 192 && !any_side) continue;
+        const double tm = (M + side - 1) / side, tn = (N + side - 1) / side, tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batches;
         for (uint32_t split = 1; split <= most_ranges && (split == 1 || steps >= 4 * split); split *= 2) {
-            const double rounds = (double)(uint64_t)((tiles * split + 255) / 256), step = rounds * k.full > k.alone ? rounds * k.full : k.alone;
-            double us = ((steps + split - 1) / split) * step;
+            double us = ((steps + split - 1) / split) * slz_step_us(side, tiles * split);
             if (split > 1) us += 4.0 + (double)M * N * batches * 4.0 * (split + 1) / 3e6;
-            if (us < least) { least = us; best = {k.side, split}; }
+            if (us < least) { least = us; best = {side, split}; }
         }
     }
     return best;
@@ -356,7 +369,7 @@ static int slz_gemm_launch(slz_gemm p, const EPI &epi, uint32_t batches, hipStre
     p.range = (slz_gemm_steps(p, slz_el<EL>::bytes) + p.split - 1) / p.split;
     const uint64_t tiles = p.symmetric ? (uint64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (uint64_t)p.tiles_m * p.tiles_n;
     if (tiles == 0 || batches == 0) return SLZ_OK;
-    if (tiles > 0x7fffffffu) return SLZ_E_TOO_LARGE;
+    if (tiles * p.split * batches > 0x7fffffffu) return SLZ_E_TOO_LARGE;
     hipLaunchKernelGGL((k_gemm<EL, A_ROWS_K, B_ROWS_K, T::TM, T::TN, T::WM, T::WN, EPI>), dim3((uint32_t)tiles, p.split, batches),
                        dim3(T::WM * T::WN * 64), 0, s, p, epi);
     return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
@@ -364,6 +377,8 @@ static int slz_gemm_launch(slz_gemm p, const EPI &epi, uint32_t batches, hipStre
 template <int EL, bool A_ROWS_K, bool B_ROWS_K, class EPI>
 static int slz_gemm_run(const slz_gemm &p, const EPI &epi, uint32_t side, uint32_t batches, hipStream_t s) {
     if (side == 256) return slz_gemm_launch<slz_tiles_256, EL, A_ROWS_K, B_ROWS_K>(p, epi, batches, s);
+    if constexpr (EPI::any_side)
+        if (side == 192) return slz_gemm_launch<slz_tiles_192, EL, A_ROWS_K, B_ROWS_K>(p, epi, batches, s);
     if (side == 128) return slz_gemm_launch<slz_tiles_128, EL, A_ROWS_K, B_ROWS_K>(p, epi, batches, s);
     return slz_gemm_launch<slz_tiles_64, EL, A_ROWS_K, B_ROWS_K>(p, epi, batches, s);
 }

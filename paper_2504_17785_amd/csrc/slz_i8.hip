@@ -2,60 +2,17 @@
 #include "slz_gemm.h"
 
 // ---- quantisation ------------------------------------------------------------------------------------------------------------------
-// A row whose largest entry is below 2^-100 is moved up by 2^100 first, so that 127 / top stays finite.
+// A row whose largest entry is below 2^-100 is moved up by 2^100 first, so that 1 / top stays finite.
 __device__ __forceinline__ float quantize_scale(float top, bool finite, float &up, float &inv) {
     up = top < 0x1p-100f ? 0x1p100f : 1.0f;
     const float t = top * up;
-    inv = finite && t > 0.0f ? 127.0f / t : 0.0f;
+    inv = finite && t > 0.0f ? 1.0f / t * 127.0f : 0.0f;
     return finite ? t / 127.0f / up : __builtin_nanf("");
 }
 __device__ __forceinline__ int8_t quantize_one(float x, float up, float inv) {
     return (int8_t)(int)fminf(fmaxf(rintf(x * up * inv), -127.0f), 127.0f);
 }
 
-// Eight elements of a row of `cols` at c (a multiple of 8), zeros past its end; the row may begin at any address.  Where the row ends inside,
-// its last eight are read and moved down.  In two parts, so that several loads are under way before the first is looked at.
-typedef v4i32 v4i32_any __attribute__((aligned(1)));
-template <int TYPE> struct row8 { v4i32 w[TYPE == SLZ_F32 ? 2 : 1]; };
-template <int TYPE> __device__ __forceinline__ row8<TYPE> row8_load(const void *x, size_t row, uint32_t c, uint32_t cols) {
-    row8<TYPE> q;
-    if (cols < 8u) {                                   // all of it, in the first threads
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = c + i < cols ? slz_get(x, TYPE, row + c + i) : 0.0f;
-        if constexpr (TYPE == SLZ_F32) {
-            q.w[0] = v4i32{__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
-            q.w[1] = v4i32{__float_as_int(v[4]), __float_as_int(v[5]), __float_as_int(v[6]), __float_as_int(v[7])};
-        } else {
-            uint32_t h[4];
-#pragma unroll
-            for (int i = 0; i < 4; i++) h[i] = slz_half(v[2 * i], TYPE) | ((uint32_t)slz_half(v[2 * i + 1], TYPE) << 16);
-            q.w[0] = v4i32{(int)h[0], (int)h[1], (int)h[2], (int)h[3]};
-        }
-        return q;
-    }
-    const uint32_t from = min(c, cols - 8u);
-    const v4i32_any *p = (const v4i32_any *)((const char *)x + (row + from) * slz_type_bytes(TYPE));
-    q.w[0] = p[0];
-    if constexpr (TYPE == SLZ_F32) q.w[1] = p[1];
-    return q;
-}
-template <int TYPE> __device__ __forceinline__ void row8_values(const row8<TYPE> &q, uint32_t c, uint32_t cols, float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        if constexpr (TYPE == SLZ_F32) v[i] = __int_as_float(q.w[i / 4][i % 4]);
-        else {
-            const uint16_t h = (uint16_t)((uint32_t)q.w[0][i / 2] >> (16 * (i & 1)));
-            v[i] = TYPE == SLZ_BF16 ? slz_bf16_to_f32(h) : slz_f16_to_f32(h);
-        }
-    }
-    if (c + 8u <= cols) return;
-    const uint32_t gone = c >= cols ? 8u : cols < 8u ? 0u : c + 8u - cols;
-#pragma unroll
-    for (uint32_t b = 1; b < 16; b <<= 1)
-#pragma unroll
-        for (uint32_t i = 0; i < 8; i++) v[i] = gone & b ? (i + b < 8 ? v[(i + b) % 8] : 0.0f) : v[i];
-}
 __device__ __forceinline__ float top_of(const float (&v)[8]) {
     float top = 0.0f;
 #pragma unroll
@@ -453,6 +410,7 @@ extern "C" int slz_linear_i8(const slz_i8_shape *sh, const void *x, const int8_t
 // ---- gradient ------------------------------------------------------------------------------------------------------------------------------
 // dy times the values scale_r q_rc: these are laid out as an operand once (bf16, or three bf16 for f32), then two ordinary products.  f16 could
 // not hold small scales, so its values are divided by `unit`, the power of two at or above the largest scale, and the sums multiplied by it.
+typedef uint64_t u64_any __attribute__((aligned(1)));
 // eight values of a row per thread
 __global__ void __launch_bounds__(256)
 k_values(const int8_t *__restrict__ q, const float *__restrict__ scale, const float *__restrict__ unit, int type, uint32_t rows, uint32_t cols, int64_t ld_q,
@@ -460,12 +418,18 @@ k_values(const int8_t *__restrict__ q, const float *__restrict__ scale, const fl
     const uint32_t per_row = ld_out / 16u;
     const size_t total = (size_t)rows * per_row;
     for (size_t g = (size_t)blockIdx.x * 256 + threadIdx.x; g < total; g += (size_t)gridDim.x * 256) {
-        const size_t r = g / per_row;
-        const uint32_t c = (uint32_t)(g % per_row) * 8;
+        uint32_t c;
+        const size_t r = slz_divide(g, per_row, total <= 0xffffffffu, c);
+        c *= 8;
         const float sc = type == SLZ_F16 ? scale[r] / *unit : scale[r];
+        uint64_t bytes = 0;
+        if (c + 8u <= cols) bytes = *(const u64_any *)(q + r * ld_q + c);
+        else
+            for (uint32_t i = 0; i < 8 && c + i < cols; i++) bytes |= (uint64_t)(uint8_t)q[r * ld_q + c + i] << (8 * i);
         uint16_t t[3][8];
+#pragma unroll
         for (int i = 0; i < 8; i++) {
-            const float v = c + i < cols ? (float)q[r * ld_q + c + i] * sc : 0.0f;
+            const float v = (float)(int8_t)(bytes >> (8 * i)) * sc;
             if (type == SLZ_F32) {
                 uint16_t u[3];
                 slz_split3(v, u);

@@ -15,12 +15,13 @@
 // (maximum, sum of exp(z - maximum)) of two sets of z; a set whose z are all -inf has (-inf, 0) and adds nothing
 __device__ __forceinline__ float2 ce_both(float2 p, float2 q) {
     const float top = fmaxf(p.x, q.x), from = top == -__builtin_inff() ? 0.0f : top;
-    return make_float2(top, p.y * expf(p.x - from) + q.y * expf(q.x - from));
+    return make_float2(top, p.y * __expf(p.x - from) + q.y * __expf(q.x - from));
 }
 
 // One pair for every 32 words, whatever the tiling: sums of eight, then of four such.  A token's loss so has the same bits alone and among others.
 #define CE_BLOCK 32
 struct ce_lse_epi {
+    static constexpr bool any_side = false;            // blocks of 32 words lie within a wave's columns
     float2 *pairs;                   // [block of words][tokens]
     float *label_z;
     const int64_t *labels;
@@ -70,11 +71,18 @@ k_ce_join(const float2 *__restrict__ pairs, const float *__restrict__ label_z, c
     const uint32_t r = threadIdx.x & 15u, slice = threadIdx.x >> 4, t = blockIdx.x * 16 + r;
     float2 all = make_float2(-__builtin_inff(), 0.0f);
     if (t < tokens)
-        for (uint32_t i = slice; i < blocks; i += 256) {
-            float2 four[4];
+        for (uint32_t i = slice; i < blocks; i += 64 * 8) {
+            float2 some[8];
 #pragma unroll
-            for (int q = 0; q < 4; q++) four[q] = i + q * 64 < blocks ? pairs[(size_t)(i + q * 64) * tokens + t] : make_float2(-__builtin_inff(), 0.0f);
-            all = ce_both(all, ce_both(ce_both(four[0], four[1]), ce_both(four[2], four[3])));
+            for (int q = 0; q < 8; q++) some[q] = i + q * 64 < blocks ? pairs[(size_t)(i + q * 64) * tokens + t] : make_float2(-__builtin_inff(), 0.0f);
+            float top = all.x;
+#pragma unroll
+            for (int q = 0; q < 8; q++) top = fmaxf(top, some[q].x);
+            const float from = top == -__builtin_inff() ? 0.0f : top;
+            all.y *= __expf(all.x - from);
+            all.x = top;
+#pragma unroll
+            for (int q = 0; q < 8; q++) all.y += some[q].y * __expf(some[q].x - from);
         }
     part[slice][r] = all;
     for (uint32_t half = 32; half > 0; half >>= 1) {
@@ -90,6 +98,7 @@ k_ce_join(const float2 *__restrict__ pairs, const float *__restrict__ label_z, c
 
 // g of a piece: [pieces][tokens][ld], columns from N to the next multiple of 8 zero
 struct ce_grad_epi {
+    static constexpr bool any_side = false;            // eight columns of a lane at a time
     char *g;
     int64_t ld, piece;               // bytes
     int type;
@@ -142,7 +151,7 @@ struct ce_grad_epi {
 // gradient of many tokens: two), where the tiled products would be four to eight.  Taken by the sizes of w alone, so that a token's loss does not
 // depend on how many there are.
 #define FEW_CLASSES 32
-#define FEW_WEIGHTS 8192
+#define FEW_WEIGHTS 16384
 #define FEW_THREADS 1024
 #define FEW_TOKENS_LDS 16384         // entries of h that a workgroup holds
 #define FEW_BLOCKS 256
@@ -154,8 +163,27 @@ struct few_args {
     int64_t ignore;
     uint32_t tokens, inner, vocab;
 };
-// z of a token in every lane; h: its entries in shared memory
-template <int C> __device__ __forceinline__ void few_logits(const float *h, const float *w, uint32_t inner, uint32_t vocab, uint32_t lane, float (&z)[C]) {
+// rows of w or h to shared memory in 32 bits, a wave a row, four loads under way
+template <int TYPE> __device__ __forceinline__ void few_rows_of(const void *x, int64_t ld, uint32_t rows, uint32_t inner, float *to) {
+    const uint32_t lane = threadIdx.x & 63u;
+    for (uint32_t r = threadIdx.x >> 6; r < rows; r += FEW_THREADS / 64)
+        for (uint32_t d0 = lane; d0 < inner; d0 += 256) {
+            float v[4];
+#pragma unroll
+            for (uint32_t q = 0; q < 4; q++) v[q] = slz_get(x, TYPE, (size_t)r * ld + min(d0 + q * 64, inner - 1));
+#pragma unroll
+            for (uint32_t q = 0; q < 4; q++)
+                if (d0 + q * 64 < inner) to[r * inner + d0 + q * 64] = v[q];
+        }
+}
+__device__ __forceinline__ void few_rows(const void *x, int type, int64_t ld, uint32_t rows, uint32_t inner, float *to) {
+    if (type == SLZ_F32) few_rows_of<SLZ_F32>(x, ld, rows, inner, to);
+    else if (type == SLZ_BF16) few_rows_of<SLZ_BF16>(x, ld, rows, inner, to);
+    else few_rows_of<SLZ_F16>(x, ld, rows, inner, to);
+}
+// Softmax of a token by a wave: lane v has z of class v (-inf behind the last), and gets the logarithm of the sum of exp.
+template <int C> __device__ __forceinline__ float few_logits(const float *h, const float *w, uint32_t inner, uint32_t vocab, uint32_t lane) {
+    float z[C];
 #pragma unroll
     for (int v = 0; v < C; v++) z[v] = 0.0f;
     for (uint32_t d = lane; d < inner; d += 64) {
@@ -164,24 +192,18 @@ template <int C> __device__ __forceinline__ void few_logits(const float *h, cons
         for (int v = 0; v < C; v++)
             if ((uint32_t)v < vocab) z[v] = __builtin_fmaf(x, w[v * inner + d], z[v]);
     }
+    float own = -__builtin_inff();
 #pragma unroll
     for (int v = 0; v < C; v++)
-        if ((uint32_t)v < vocab) z[v] = slz_wave_sum(z[v]);
+        if ((uint32_t)v < vocab) {
+            const float sum = slz_wave_sum(z[v]);
+            own = lane == (uint32_t)v ? sum : own;
+        }
+    return own;
 }
-template <int C> __device__ __forceinline__ float few_lse(const float (&z)[C], uint32_t vocab) {
-    float top = -__builtin_inff(), sum = 0.0f;
-#pragma unroll
-    for (int v = 0; v < C; v++) top = (uint32_t)v < vocab ? fmaxf(top, z[v]) : top;
-    const float from = top == -__builtin_inff() ? 0.0f : top;
-#pragma unroll
-    for (int v = 0; v < C; v++) sum += (uint32_t)v < vocab ? expf(z[v] - from) : 0.0f;
-    return top + logf(sum);
-}
-__device__ __forceinline__ void few_weights(const few_args &p, float *w) {
-    for (uint32_t i = threadIdx.x; i < p.vocab * p.inner; i += FEW_THREADS) w[i] = slz_get(p.w, p.type, (size_t)(i / p.inner) * p.ld_w + i % p.inner);
-}
-__device__ __forceinline__ void few_tokens(const few_args &p, uint32_t first, uint32_t count, float *h) {
-    for (uint32_t i = threadIdx.x; i < count * p.inner; i += FEW_THREADS) h[i] = slz_get(p.h, p.type, (size_t)(first + i / p.inner) * p.ld_h + i % p.inner);
+__device__ __forceinline__ float few_lse(float own, bool real) {
+    const float top = slz_wave_max(own), from = top == -__builtin_inff() ? 0.0f : top;
+    return top + logf(slz_wave_sum(real ? expf(own - from) : 0.0f));
 }
 
 // `group` tokens at a time
@@ -190,21 +212,20 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few_loss(const few_args p, uint
     extern __shared__ __attribute__((aligned(16))) float few[];
     float *w = few, *h = few + p.vocab * p.inner;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    few_weights(p, w);
+    few_rows(p.w, p.type, p.ld_w, p.vocab, p.inner, w);
     for (uint32_t first = blockIdx.x * group; first < p.tokens; first += gridDim.x * group) {
         const uint32_t count = min(group, p.tokens - first);
-        few_tokens(p, first, count, h);
+        const int64_t own_label = lane < count ? p.labels[first + lane] : 0;            // group is 32 at most
+        few_rows((const char *)p.h + (size_t)first * p.ld_h * slz_type_bytes(p.type), p.type, p.ld_h, count, p.inner, h);
         __syncthreads();
         for (uint32_t t = wave; t < count; t += FEW_THREADS / 64) {
-            float z[C], at_label = 0.0f;
-            few_logits<C>(h + t * p.inner, w, p.inner, p.vocab, lane, z);
-            const float l = few_lse<C>(z, p.vocab);
-            const int64_t label = p.labels[first + t];
-#pragma unroll
-            for (int v = 0; v < C; v++) at_label = label == v ? z[v] : at_label;
+            const float z = few_logits<C>(h + t * p.inner, w, p.inner, p.vocab, lane), l = few_lse(z, lane < p.vocab);
+            const int64_t label = __shfl(own_label, (int)t, 64);
+            const bool inside = label >= 0 && label < (int64_t)p.vocab;
+            const float at_label = __shfl(z, inside ? (int)label : 0, 64);
             if (lane == 0) {
                 lse[first + t] = l;
-                loss[first + t] = label == p.ignore ? 0.0f : label < 0 || label >= (int64_t)p.vocab ? __builtin_nanf("") : l - at_label;
+                loss[first + t] = label == p.ignore ? 0.0f : inside ? l - at_label : __builtin_nanf("");
             }
         }
         __syncthreads();
@@ -212,7 +233,8 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few_loss(const few_args p, uint
 }
 
 // dw: the sums of each workgroup's tokens go to `part` [workgroup][vocab][inner], or with one workgroup to dw
-template <int C>
+// OWN: entries of dw of a thread
+template <int C, int OWN>
 __global__ void __launch_bounds__(FEW_THREADS)
 k_few_grad(const few_args p, uint32_t group, const float *__restrict__ lse, const float *__restrict__ dloss, void *__restrict__ dh, int64_t ld_dh,
            void *__restrict__ dw, int64_t ld_dw, float *__restrict__ part) {
@@ -220,45 +242,43 @@ k_few_grad(const few_args p, uint32_t group, const float *__restrict__ lse, cons
     const uint32_t weights = p.vocab * p.inner;
     float *w = few, *g = w + weights, *h = g + group * p.vocab;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    constexpr int OWN = FEW_WEIGHTS / FEW_THREADS;                  // entries of dw of a thread
     float sum[OWN];
-    uint32_t own_v[OWN], own_d[OWN];
+    uint32_t own_at[OWN];                              // class and place in the row
 #pragma unroll
     for (int i = 0; i < OWN; i++) {
         const uint32_t e = i * FEW_THREADS + threadIdx.x;
         sum[i] = 0.0f;
-        own_v[i] = e < weights ? e / p.inner : 0u;
-        own_d[i] = e < weights ? e % p.inner : 0u;
+        own_at[i] = e < weights ? (e / p.inner) << 16 | e % p.inner : 0u;
     }
-    few_weights(p, w);
+    few_rows(p.w, p.type, p.ld_w, p.vocab, p.inner, w);
     for (uint32_t first = blockIdx.x * group; first < p.tokens; first += gridDim.x * group) {
         const uint32_t count = min(group, p.tokens - first);
-        few_tokens(p, first, count, h);
+        const int64_t own_label = lane < count ? p.labels[first + lane] : 0;            // group is 32 at most
+        const float own_lse = lane < count ? lse[first + lane] : 0.0f, own_dloss = lane < count ? dloss[first + lane] : 0.0f;
+        few_rows((const char *)p.h + (size_t)first * p.ld_h * slz_type_bytes(p.type), p.type, p.ld_h, count, p.inner, h);
         __syncthreads();
         for (uint32_t t = wave; t < count; t += FEW_THREADS / 64) {
-            float z[C];
-            few_logits<C>(h + t * p.inner, w, p.inner, p.vocab, lane, z);
-            const int64_t label = p.labels[first + t];
-            const float l = lse[first + t], by = label < 0 || label >= (int64_t)p.vocab ? __builtin_nanf("") : dloss[first + t];
-#pragma unroll
-            for (int v = 0; v < C; v++)
-                if ((uint32_t)v < p.vocab) {
-                    z[v] = label == p.ignore ? 0.0f : (expf(z[v] - l) - (label == v ? 1.0f : 0.0f)) * by;
-                    if (lane == 0) g[t * p.vocab + v] = z[v];
-                }
+            const float z = few_logits<C>(h + t * p.inner, w, p.inner, p.vocab, lane), l = __shfl(own_lse, (int)t, 64);
+            const int64_t label = __shfl(own_label, (int)t, 64);
+            const float by = label < 0 || label >= (int64_t)p.vocab ? __builtin_nanf("") : __shfl(own_dloss, (int)t, 64);
+            const float own = label == p.ignore ? 0.0f : (expf(z - l) - (label == (int64_t)lane ? 1.0f : 0.0f)) * by;
+            if (lane < p.vocab) g[t * p.vocab + lane] = own;
             for (uint32_t d = lane; d < p.inner; d += 64) {
                 float x = 0.0f;
 #pragma unroll
                 for (int v = 0; v < C; v++)
-                    if ((uint32_t)v < p.vocab) x = __builtin_fmaf(z[v], w[v * p.inner + d], x);
+                    if ((uint32_t)v < p.vocab) x = __builtin_fmaf(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, own), v)), w[v * p.inner + d], x);
                 slz_put(dh, p.type, (size_t)(first + t) * ld_dh + d, x);
             }
         }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < OWN; i++)
-            if ((uint32_t)i * FEW_THREADS < weights)
-                for (uint32_t t = 0; t < count; t++) sum[i] = __builtin_fmaf(g[t * p.vocab + own_v[i]], h[t * p.inner + own_d[i]], sum[i]);
+            if ((uint32_t)i * FEW_THREADS < weights) {
+                const float *gi = g + (own_at[i] >> 16), *hi = h + (own_at[i] & 0xffffu);
+#pragma unroll 2
+                for (uint32_t t = 0; t < count; t++) sum[i] = __builtin_fmaf(gi[t * p.vocab], hi[t * p.inner], sum[i]);
+            }
         __syncthreads();
     }
 #pragma unroll
@@ -266,7 +286,7 @@ k_few_grad(const few_args p, uint32_t group, const float *__restrict__ lse, cons
         const uint32_t e = i * FEW_THREADS + threadIdx.x;
         if (e >= weights) continue;
         if (part) part[(size_t)blockIdx.x * weights + e] = sum[i];
-        else slz_put(dw, p.type, (size_t)own_v[i] * ld_dw + own_d[i], sum[i]);
+        else slz_put(dw, p.type, (size_t)(own_at[i] >> 16) * ld_dw + (own_at[i] & 0xffffu), sum[i]);
     }
 }
 __global__ void __launch_bounds__(256)
@@ -279,28 +299,35 @@ k_few_join(const float *__restrict__ part, uint32_t blocks, uint32_t vocab, uint
 }
 
 static bool few_takes(const slz_ce_shape *sh) { return sh->vocab <= FEW_CLASSES && (uint64_t)sh->vocab * sh->inner <= FEW_WEIGHTS; }
-static uint32_t few_group(const slz_ce_shape *sh) {
+// tokens a workgroup takes at a time, `most` or what its shared memory holds, and workgroups.  Loss: a token for each of its waves; gradient: two, since
+// the second launch costs more
+static uint32_t few_group(const slz_ce_shape *sh, uint32_t most) {
     const uint32_t fit = FEW_TOKENS_LDS / sh->inner;
-    return fit < 1 ? 1 : fit > 32 ? 32 : fit;
+    return fit < 1 ? 1 : fit > most ? most : fit;
 }
-static uint32_t few_blocks(const slz_ce_shape *sh) {
-    const uint32_t n = (sh->tokens + few_group(sh) - 1) / few_group(sh);
+static uint32_t few_blocks(const slz_ce_shape *sh, uint32_t group) {
+    const uint32_t n = (sh->tokens + group - 1) / group;
     return n < 1 ? 1 : n > FEW_BLOCKS ? FEW_BLOCKS : n;
 }
-static size_t few_workspace(const slz_ce_shape *sh) { return few_blocks(sh) == 1 ? 0 : up256((size_t)few_blocks(sh) * sh->vocab * sh->inner * 4); }
+static size_t few_workspace(const slz_ce_shape *sh) {
+    const uint32_t blocks = few_blocks(sh, few_group(sh, 32));
+    return blocks == 1 ? 0 : up256((size_t)blocks * sh->vocab * sh->inner * 4);
+}
 static few_args few_of(const slz_ce_shape *sh, const void *h, const void *w, const int64_t *labels) {
     return {h, w, sh->type, sh->ld_h, sh->ld_w, labels, sh->ignore_index, sh->tokens, sh->inner, sh->vocab};
 }
 static int few_loss(const slz_ce_shape *sh, const void *h, const void *w, const int64_t *labels, float *loss, float *lse, hipStream_t s) {
-    const uint32_t group = few_group(sh);
-    const auto k = sh->vocab <= 4 ? k_few_loss<4> : sh->vocab <= 16 ? k_few_loss<16> : k_few_loss<32>;
-    hipLaunchKernelGGL(k, dim3(few_blocks(sh)), dim3(FEW_THREADS), (sh->vocab + group) * sh->inner * 4, s, few_of(sh, h, w, labels), group, loss, lse);
+    const uint32_t group = few_group(sh, 16);
+    const auto k = sh->vocab <= 8 ? k_few_loss<8> : sh->vocab <= 16 ? k_few_loss<16> : k_few_loss<32>;
+    hipLaunchKernelGGL(k, dim3(few_blocks(sh, group)), dim3(FEW_THREADS), (sh->vocab + group) * sh->inner * 4, s, few_of(sh, h, w, labels), group, loss, lse);
     return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
 }
 static int few_grad(const slz_ce_shape *sh, const void *h, const void *w, const int64_t *labels, const float *lse, const float *dloss, void *dh, void *dw,
                     float *part, hipStream_t s) {
-    const uint32_t group = few_group(sh), blocks = few_blocks(sh);
-    const auto k = sh->vocab <= 4 ? k_few_grad<4> : sh->vocab <= 16 ? k_few_grad<16> : k_few_grad<32>;
+    const uint32_t group = few_group(sh, 32), blocks = few_blocks(sh, group);
+    const bool small = sh->vocab * sh->inner <= 2 * FEW_THREADS;
+    constexpr int all = FEW_WEIGHTS / FEW_THREADS;
+    const auto k = sh->vocab <= 16 ? (small ? k_few_grad<16, 2> : k_few_grad<16, all>) : small ? k_few_grad<32, 2> : k_few_grad<32, all>;
     hipLaunchKernelGGL(k, dim3(blocks), dim3(FEW_THREADS), ((sh->vocab + group) * sh->inner + group * sh->vocab) * 4, s, few_of(sh, h, w, labels), group, lse,
                        dloss, dh, sh->ld_dh, dw, sh->ld_dw, blocks > 1 ? part : nullptr);
     if (blocks > 1)
@@ -325,7 +352,7 @@ static ce_plan plan_ce(const slz_ce_shape *sh, const void *h, const void *w, boo
     if (words < sh->vocab) words = words < 1024 ? 1024 : words & ~(size_t)255;
     P.words = (uint32_t)(words < sh->vocab ? words : sh->vocab);
     const uint32_t pairs = sh->type == SLZ_F32 ? 6 : 1;
-    P.side = slz_choose(sh->tokens, P.words, (sh->inner + 63) / 64 * pairs, 1, false, 1).side;
+    P.side = slz_choose(sh->tokens, P.words, (sh->inner + 63) / 64 * pairs, 1, false, 1, false).side;
     size_t o = 0;
     P.h = o; o += slz_operand_bytes(h, sh->type, sh->tokens, sh->inner, sh->ld_h);
     P.w = o; o += slz_operand_bytes(w, sh->type, P.words, sh->inner, sh->ld_w);

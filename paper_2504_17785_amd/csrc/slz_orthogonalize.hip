@@ -12,7 +12,7 @@
 #include "slz_gemm.h"
 
 #define ORTH_UP 64.0f                // operands are held times this: the second halves stay out of the subnormal numbers
-#define ORTH_NORM_BLOCKS 64
+#define ORTH_NORM_BLOCKS 1024
 
 struct orth_view {                   // a batch of matrices of two f16 each; rows of a multiple of 64 elements
     uint16_t *hi, *lo;               // lo may be null
@@ -49,14 +49,30 @@ __device__ __forceinline__ float orth_get(const orth_view &v, size_t at) {
 }
 
 // ---- norm and first X -------------------------------------------------------------------------------------------------------------------
+// Sums of squares of a matrix, in ORTH_NORM_BLOCKS parts at most; eight elements of a row at a time, four such under way in a thread
+template <int TYPE>
 __global__ void __launch_bounds__(256)
-k_orth_norm(const void *__restrict__ g, int type, uint32_t rows, uint32_t cols, int64_t ld, int64_t stride, double *__restrict__ part) {
-    const size_t base = (size_t)blockIdx.y * stride;
+k_orth_norm(const void *__restrict__ g, uint32_t rows, uint32_t cols, int64_t ld, int64_t stride, double *__restrict__ part) {
+    const uint32_t per_row = (cols + 7u) / 8u;
+    const size_t base = (size_t)blockIdx.y * stride, total = (size_t)rows * per_row, each = (total + gridDim.x - 1) / gridDim.x;
+    const size_t first = blockIdx.x * each, last = first + each < total ? first + each : total;
     double sum = 0.0;
-    for (uint32_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        for (uint32_t c = threadIdx.x; c < cols; c += 256) {
-            const double x = slz_get(g, type, base + (size_t)r * ld + c);
-            sum += x * x;
+    for (size_t i0 = first + threadIdx.x; i0 < last; i0 += 256 * 4) {
+        row8<TYPE> x[4];
+        uint32_t c[4];
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const size_t r = slz_divide(i0 + q * 256 < last ? i0 + q * 256 : i0, per_row, total <= 0xffffffffu, c[q]);
+            c[q] *= 8u;
+            x[q] = row8_load<TYPE>(g, base + r * ld, c[q], cols);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            if (i0 + q * 256 >= last) continue;
+            float v[8];
+            row8_values<TYPE>(x[q], c[q], cols, v);
+#pragma unroll
+            for (int k = 0; k < 8; k++) sum += (double)v[k] * (double)v[k];
         }
     }
 #pragma unroll
@@ -71,23 +87,24 @@ __global__ void __launch_bounds__(256)
 k_orth_load(const void *__restrict__ g, int type, uint32_t rows, uint32_t cols, int64_t ld, int64_t stride, int tall, const double *__restrict__ part,
             uint32_t parts, float eps, orth_view x, float *__restrict__ factor) {
     __shared__ float tile[64][65];
-    __shared__ double total;
-    if (threadIdx.x == 0) {
-        double s = 0.0;
-        for (uint32_t i = 0; i < parts; i++) s += part[blockIdx.z * ORTH_NORM_BLOCKS + i];
-        total = sqrt(s) + (double)eps;
+    const uint32_t r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, t = threadIdx.x;
+    const size_t base = (size_t)blockIdx.z * stride;
+    float own[16];
+#pragma unroll
+    for (int q = 0; q < 16; q++) {
+        const uint32_t i = t + q * 256, r = r0 + i / 64, c = c0 + i % 64;
+        own[q] = r < rows && c < cols ? slz_get(g, type, base + (size_t)r * ld + c) : 0.0f;
     }
-    __syncthreads();
-    const double norm = total;
+    double sum = 0.0;
+    for (uint32_t i = t & 63u; i < parts; i += 64) sum += part[blockIdx.z * ORTH_NORM_BLOCKS + i];
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
+    const double norm = sqrt(sum) + (double)eps;
     int e = 0;
     if (norm > 0.0 && norm < 1e300) frexp(norm, &e);
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) factor[blockIdx.z] = (float)(ldexp(1.0, e) / norm);
-    const uint32_t r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, t = threadIdx.x;
-    const size_t base = (size_t)blockIdx.z * stride;
-    for (uint32_t i = t; i < 4096; i += 256) {
-        const uint32_t r = r0 + i / 64, c = c0 + i % 64;
-        tile[i / 64][i % 64] = r < rows && c < cols ? ldexpf(slz_get(g, type, base + (size_t)r * ld + c), -e) : 0.0f;
-    }
+#pragma unroll
+    for (int q = 0; q < 16; q++) tile[(t + q * 256) / 64][t % 64] = ldexpf(own[q], -e);
     __syncthreads();
     const uint32_t m = tall ? cols : rows, wide = ((tall ? rows : cols) + 7u) & ~7u;
     for (uint32_t i = t; i < 1024; i += 256) {
@@ -110,6 +127,7 @@ k_orth_store(orth_view x, const float *__restrict__ factor, void *__restrict__ o
 // A symmetric product's result: the diagonal apart, the rest to `out` with zeros on the diagonal and in the columns up to the next multiple of 8.
 // A tile below the diagonal is stored a second time, transposed through shared memory, half by half.
 template <class F> struct orth_symmetric_epi {
+    static constexpr bool any_side = true;
     orth_view out;
     float *diagonal;                 // [batch][m]
     F f;
@@ -185,6 +203,7 @@ struct orth_polynomial {
     __device__ __forceinline__ float finish(float v) const { return a + v; }
 };
 struct orth_apply_epi {
+    static constexpr bool any_side = true;
     orth_view x, next;               // this step's X and the next one's
     const float *diagonal;           // a + B_ii
     const float *factor;             // or null
@@ -304,8 +323,10 @@ extern "C" int slz_orthogonalize(const slz_orth_shape *sh, const void *g, void *
     float *da = (float *)(w + P.da), *db = (float *)(w + P.db), *factor = (float *)(w + P.factor);
     double *part = (double *)(w + P.part);
     const uint32_t aligned = slz_in_place(out, 16, sh->ld_out, eb) && (sh->batch == 1 || sh->stride_out * eb % 16 == 0);
-    const uint32_t parts = sh->rows < ORTH_NORM_BLOCKS ? sh->rows : ORTH_NORM_BLOCKS;
-    hipLaunchKernelGGL(k_orth_norm, dim3(parts, sh->batch), dim3(256), 0, s, g, sh->type, sh->rows, sh->cols, sh->ld_g, sh->stride_g, part);
+    const uint64_t needed = ((uint64_t)sh->rows * sh->cols + 8191) / 8192;
+    const uint32_t parts = needed < ORTH_NORM_BLOCKS ? (uint32_t)needed : ORTH_NORM_BLOCKS;
+    const auto norm = sh->type == SLZ_F32 ? k_orth_norm<SLZ_F32> : sh->type == SLZ_BF16 ? k_orth_norm<SLZ_BF16> : k_orth_norm<SLZ_F16>;
+    hipLaunchKernelGGL(norm, dim3(parts, sh->batch), dim3(256), 0, s, g, sh->rows, sh->cols, sh->ld_g, sh->stride_g, part);
     hipLaunchKernelGGL(k_orth_load, dim3((sh->cols + 63) / 64, (sh->rows + 63) / 64, sh->batch), dim3(256), 0, s, g, sh->type, sh->rows, sh->cols, sh->ld_g,
                        sh->stride_g, tall, part, parts, sh->eps, x[0], factor);
     if (sh->steps == 0)

@@ -59,7 +59,7 @@ def quantised(x):
     x = x.float().cpu().numpy()
     top = np.abs(x).max(axis=1, initial=0).astype(np.float32)
     with np.errstate(all="ignore"):
-        inv = np.where(top > 0, np.float32(127) / top, np.float32(0)).astype(np.float32)
+        inv = np.where(top > 0, np.float32(1) / top * np.float32(127), np.float32(0)).astype(np.float32)
         q = np.rint(x * inv[:, None])
     return q.astype(np.int8), (top / np.float32(127)).astype(np.float32)
 
