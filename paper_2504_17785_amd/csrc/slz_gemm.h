@@ -316,7 +316,7 @@ using slz_tiles_64 = slz_tiling<64, 64, 2, 2>;
 // with one of 128 and 0.88 with two at once, 0.33 with one of 64 and 0.18 for each of several (measured at 4096 deep: 3840^2 with 256: 99 us;
 // 2688^2 with 192: 63, with 128: 57; 768^2 with 256, 192, 128: 85, 58, 43).  Large tiles read less for each product, small ones fill the chip with less
 // and leave less of it idle at the end.  Ranges of k cost a second launch that reads their sums.
-struct slz_choice { uint32_t side, split; };
+struct slz_choice { uint32_t side, split; double us; };
 static inline double slz_step_us(uint32_t side, double tiles) {
     const auto rounds = [&](double at_once) { return (double)(uint64_t)((tiles + at_once - 1) / at_once); };
     if (side == 256) return rounds(256) * 1.5;
@@ -326,15 +326,14 @@ static inline double slz_step_us(uint32_t side, double tiles) {
     return pairs * 0.88 + (rest > 256 ? 0.88 : rest > 0 ? 0.62 : 0.0);
 }
 static inline slz_choice slz_choose(uint32_t M, uint32_t N, uint32_t steps, uint32_t batches, bool symmetric, uint32_t most_ranges, bool any_side = true) {
-    slz_choice best = {64, 1};
-    double least = 1e30;
+    slz_choice best = {64, 1, 1e30};
     for (const uint32_t side : {256u, 192u, 128u, 64u}) {
         if (side == 192 && !any_side) continue;
         const double tm = (M + side - 1) / side, tn = (N + side - 1) / side, tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batches;
         for (uint32_t split = 1; split <= most_ranges && (split == 1 || steps >= 4 * split); split *= 2) {
             double us = ((steps + split - 1) / split) * slz_step_us(side, tiles * split);
             if (split > 1) us += 4.0 + (double)M * N * batches * 4.0 * (split + 1) / 3e6;
-            if (us < least) { least = us; best = {side, split}; }
+            if (us < best.us) best = {side, split, us};
         }
     }
     return best;

@@ -135,12 +135,12 @@ def test_cross_entropy_workspace_does_not_hold_the_logits():
 def test_orthogonalize_refuses():
     L = slz.lib()
     need = ctypes.c_size_t(0)
-    ok = dict(batch=2, rows=4, cols=8, type=1, ld_g=8, stride_g=32, ld_out=8, stride_out=32, steps=5, a=3.4, b=-4.8, c=2.0, eps=1e-7)
+    ok = dict(batch=2, rows=200, cols=300, type=1, ld_g=300, stride_g=60000, ld_out=300, stride_out=60000, steps=5, a=3.4, b=-4.8, c=2.0, eps=1e-7)
 
     def each(code, g=P, out=P, ws=P, size=1 << 40, **kw):
         assert L.slz_orthogonalize(ref(SlzOrthShape(**{**ok, **kw})), g, out, ws, size, None) == code
 
-    for kw in (dict(type=4), dict(steps=65), dict(ld_g=7), dict(ld_out=7), dict(g=None), dict(out=None), dict(g=P + 1), dict(out=P + 1), dict(ws=None),
+    for kw in (dict(type=4), dict(steps=65), dict(ld_g=299), dict(ld_out=299), dict(g=None), dict(out=None), dict(g=P + 1), dict(out=P + 1), dict(ws=None),
                dict(ws=P + 64), dict(size=1000)):
         each(INVALID, **kw)
     for kw in (dict(batch=65536), dict(rows=1 << 22), dict(cols=(1 << 22) + 1, ld_g=1 << 23, ld_out=1 << 23)):

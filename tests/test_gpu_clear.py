@@ -243,7 +243,8 @@ def ce_inputs(tokens, inner, vocab, dtype, seed, slack=0, skip=0):
 
 
 LOSSES = [(1, 1, 1), (1, 64, 2), (8, 8, 3), (5, 128, 10), (32, 128, 10), (1, 512, 5000), (16, 256, 1000), (33, 40, 129), (128, 64, 128), (130, 72, 257), (200, 264, 1025),
-          (515, 128, 3001), (3, 1000, 40), (129, 17, 130)]
+          (515, 128, 3001), (3, 1000, 40), (129, 17, 130),
+          (33, 128, 10), (300, 100, 16), (9000, 20, 7), (100, 500, 32), (100, 513, 32), (5, 8192, 2), (70, 2047, 8), (1100, 3000, 40)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -426,7 +427,8 @@ def check_update(slz, g, **kw):
     return got
 
 
-UPDATES = [(1, 1), (1, 9), (7, 1), (2, 3), (8, 8), (16, 100), (65, 33), (128, 784), (784, 128), (128, 128), (130, 131), (257, 300), (300, 256), (512, 512), (40, 2000)]
+UPDATES = [(1, 1), (1, 9), (7, 1), (2, 3), (8, 8), (16, 100), (65, 33), (128, 784), (784, 128), (128, 128), (130, 131), (257, 300), (300, 256), (512, 512), (40, 2000),
+           (128, 129), (100, 257), (33, 1100), (5000, 30), (64, 513), (3, 20000), (129, 3000), (2500, 200)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -442,6 +444,8 @@ def test_orthogonalize_batches_and_arguments(slz, dtype):
     for i in range(5):
         assert torch.equal(slz.orthogonalize(g[i]), all_of[i])
     assert torch.equal(slz.orthogonalize(g[::2]), all_of[::2])
+    for rows, cols in ((100, 700), (20, 5000), (140, 2000)):         # slices and ranges of several matrices
+        check_update(slz, randn((3, rows, cols), 3, dtype, slack=1))
     check_update(slz, g[0], steps=0)
     check_update(slz, g[0], steps=1)
     check_update(slz, g[1], steps=3, coefficients=(2.0, -1.5, 0.5))
