@@ -8,7 +8,7 @@
 #include "slz_gemm.h"
 
 // a piece's g takes this much at most (at least 1024 words of the vocabulary)
-#define CE_PIECE_BYTES ((size_t)256 << 20)
+#define CE_PIECE_BYTES ((size_t)128 << 20)
 // f16: g is held times this; |g| <= |dloss|, so that the largest stay finite and those from 2^-28 of the largest keep 11 bits
 #define CE_F16_UP 16384.0f
 
@@ -150,8 +150,9 @@ struct ce_grad_epi {
 // A classifier's head: w fits a workgroup's shared memory in 32 bits, a wave computes all of a token's z, and the whole call is one launch (the
 // gradient of many tokens: two), where the tiled products would be four to eight.  Taken by the sizes of w alone, so that a token's loss does not
 // depend on how many there are.
-#define FEW_CLASSES 32
-#define FEW_WEIGHTS 16384
+#define FEW_CLASSES 16
+#define FEW_INNER 512                // longer rows leave too few tokens of a workgroup at a time
+#define FEW_WEIGHTS (FEW_CLASSES * FEW_INNER)
 #define FEW_THREADS 1024
 #define FEW_TOKENS_LDS 16384         // entries of h that a workgroup holds
 #define FEW_BLOCKS 256
@@ -298,7 +299,7 @@ k_few_join(const float *__restrict__ part, uint32_t blocks, uint32_t vocab, uint
     slz_put(dw, type, (size_t)(e / inner) * ld_dw + e % inner, sum);
 }
 
-static bool few_takes(const slz_ce_shape *sh) { return sh->vocab <= FEW_CLASSES && (uint64_t)sh->vocab * sh->inner <= FEW_WEIGHTS; }
+static bool few_takes(const slz_ce_shape *sh) { return sh->vocab <= FEW_CLASSES && sh->inner <= FEW_INNER; }
 // tokens a workgroup takes at a time, `most` or what its shared memory holds, and workgroups.  Loss: a token for each of its waves; gradient: two, since
 // the second launch costs more
 static uint32_t few_group(const slz_ce_shape *sh, uint32_t most) {
@@ -318,7 +319,7 @@ static few_args few_of(const slz_ce_shape *sh, const void *h, const void *w, con
 }
 static int few_loss(const slz_ce_shape *sh, const void *h, const void *w, const int64_t *labels, float *loss, float *lse, hipStream_t s) {
     const uint32_t group = few_group(sh, 16);
-    const auto k = sh->vocab <= 8 ? k_few_loss<8> : sh->vocab <= 16 ? k_few_loss<16> : k_few_loss<32>;
+    const auto k = sh->vocab <= 8 ? k_few_loss<8> : k_few_loss<16>;
     hipLaunchKernelGGL(k, dim3(few_blocks(sh, group)), dim3(FEW_THREADS), (sh->vocab + group) * sh->inner * 4, s, few_of(sh, h, w, labels), group, loss, lse);
     return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
 }
@@ -327,7 +328,7 @@ static int few_grad(const slz_ce_shape *sh, const void *h, const void *w, const 
     const uint32_t group = few_group(sh, 32), blocks = few_blocks(sh, group);
     const bool small = sh->vocab * sh->inner <= 2 * FEW_THREADS;
     constexpr int all = FEW_WEIGHTS / FEW_THREADS;
-    const auto k = sh->vocab <= 16 ? (small ? k_few_grad<16, 2> : k_few_grad<16, all>) : small ? k_few_grad<32, 2> : k_few_grad<32, all>;
+    const auto k = small ? k_few_grad<16, 2> : k_few_grad<16, all>;
     hipLaunchKernelGGL(k, dim3(blocks), dim3(FEW_THREADS), ((sh->vocab + group) * sh->inner + group * sh->vocab) * 4, s, few_of(sh, h, w, labels), group, lse,
                        dloss, dh, sh->ld_dh, dw, sh->ld_dw, blocks > 1 ? part : nullptr);
     if (blocks > 1)
@@ -337,7 +338,7 @@ static int few_grad(const slz_ce_shape *sh, const void *h, const void *w, const 
 
 struct ce_plan {
     uint32_t words;                  // of a piece
-    size_t h, w, pairs, label_z, g, dh, unit, total;
+    size_t h, w, pairs, label_z, g, dh, dw, unit, total;
     uint32_t g_row, dh_ld;
     uint32_t side;                   // of the tiles of z
     slz_choice dh_choice, dw_choice;
@@ -346,10 +347,17 @@ static ce_plan plan_ce(const slz_ce_shape *sh, const void *h, const void *w, boo
     ce_plan P = {};
     const size_t pieces = sh->type == SLZ_F32 ? 3 : 1;
     const bool w_there = slz_operand_bytes(w, sh->type, 1, sh->inner, sh->ld_w) == 0;
+    // words of a piece, and of them a multiple that gives whole rounds of tiles on 256 compute units where it fits (4096 tokens: 4096; 4096 x 4096
+    // x 131072 takes 15.2 ms in pieces of 8192, 16384 or 131072 words and 15.9 in five of 26368)
     size_t words = sh->vocab;
-    if (grad) words = words < CE_PIECE_BYTES / (2 * pieces * (sh->tokens + 1)) ? words : CE_PIECE_BYTES / (2 * pieces * (sh->tokens + 1));
-    if (!w_there) words = words < CE_PIECE_BYTES / (2 * pieces * sh->inner) ? words : CE_PIECE_BYTES / (2 * pieces * sh->inner);
-    if (words < sh->vocab) words = words < 1024 ? 1024 : words & ~(size_t)255;
+    const size_t for_g = CE_PIECE_BYTES / (2 * pieces * (sh->tokens ? sh->tokens : 1)), for_w = CE_PIECE_BYTES / (2 * pieces * sh->inner);
+    if (grad && words > for_g) words = for_g;
+    if (!w_there && words > for_w) words = for_w;
+    if (words < sh->vocab) {
+        uint32_t unit = 65536, rows = (sh->tokens + 255) / 256;
+        for (; unit > 256 && rows && rows % 2 == 0; rows /= 2) unit /= 2;
+        words = words >= unit ? words / unit * unit : words >= 1024 ? words & ~(size_t)255 : 1024;
+    }
     P.words = (uint32_t)(words < sh->vocab ? words : sh->vocab);
     const uint32_t pairs = sh->type == SLZ_F32 ? 6 : 1;
     P.side = slz_choose(sh->tokens, P.words, (sh->inner + 63) / 64 * pairs, 1, false, 1, false).side;
@@ -365,7 +373,8 @@ static ce_plan plan_ce(const slz_ce_shape *sh, const void *h, const void *w, boo
         P.dh_ld = slz_ranges_ld(sh->inner);
         // dh: one launch over a piece, or its sums kept in ranges of the piece's words, to which each piece adds
         P.dh_choice = slz_choose(sh->tokens, sh->inner, (P.words + 63) / 64 * pairs, 1, false, 64);
-        P.dw_choice = slz_choose(P.words, sh->inner, (sh->tokens + 63) / 64 * pairs, 1, false, 1);
+        P.dw_choice = slz_choose(P.words, sh->inner, (sh->tokens + 63) / 64 * pairs, 1, false, 32);
+        P.dw = o; o += slz_ranges_bytes(P.dw_choice, P.words, sh->inner);
         P.dh = o; o += P.words < sh->vocab || P.dh_choice.split > 1 ? up256((size_t)P.dh_choice.split * sh->tokens * P.dh_ld * 4) : 0;
         P.unit = o; o += 256;
     }
@@ -430,9 +439,9 @@ extern "C" int slz_linear_ce(const slz_ce_shape *sh, const void *h, const void *
 }
 
 template <int EL> static int ce_products(const slz_ce_shape *sh, const ce_plan &P, const slz_operand &g, const slz_operand &oh, const slz_operand &ow,
-                                         uint32_t first, uint32_t words, void *dh, void *dw, float *dh_sum, const slz_times_unit &f, hipStream_t s) {
+                                         uint32_t first, uint32_t words, void *dh, void *dw, float *dh_sum, char *dw_ranges, const slz_times_unit &f, hipStream_t s) {
     char *dw_rows = (char *)dw + (int64_t)first * sh->ld_dw * slz_type_bytes(sh->type);
-    int rc = slz_gemm_to<EL, true, true>(slz_gemm_of(g, oh, words, sh->inner, sh->tokens), P.dw_choice, f, dw_rows, sh->type, sh->ld_dw, nullptr, s);
+    int rc = slz_gemm_to<EL, true, true>(slz_gemm_of(g, oh, words, sh->inner, sh->tokens), P.dw_choice, f, dw_rows, sh->type, sh->ld_dw, dw_ranges, s);
     if (rc != SLZ_OK) return rc;
     slz_gemm p = slz_gemm_of(g, ow, sh->tokens, sh->inner, words);
     if (P.words == sh->vocab) return slz_gemm_to<EL, false, true>(p, P.dh_choice, f, dh, sh->type, sh->ld_dh, (char *)dh_sum, s);
@@ -470,8 +479,8 @@ extern "C" int slz_linear_ce_grad(const slz_ce_shape *sh, const void *h, const v
         const ce_grad_epi epi{base + P.g, g.ld, g.piece, sh->type, lse, dloss, unit, labels, sh->ignore_index, v, sh->vocab};
         rc = ce_logits(sh->type, slz_gemm_of(oh, ow, sh->tokens, words, sh->inner), epi, P.side, s);
         if (rc == SLZ_OK)
-            rc = sh->type == SLZ_F16 ? ce_products<SLZ_EL_F16>(sh, P, g, oh, ow, v, words, dh, dw, dh_sum, f, s)
-                                     : ce_products<SLZ_EL_BF16>(sh, P, g, oh, ow, v, words, dh, dw, dh_sum, f, s);
+            rc = sh->type == SLZ_F16 ? ce_products<SLZ_EL_F16>(sh, P, g, oh, ow, v, words, dh, dw, dh_sum, base + P.dw, f, s)
+                                     : ce_products<SLZ_EL_BF16>(sh, P, g, oh, ow, v, words, dh, dw, dh_sum, base + P.dw, f, s);
         if (rc != SLZ_OK) return rc;
     }
     if (P.words < sh->vocab && sh->tokens)

@@ -134,45 +134,62 @@ template <class F> struct orth_symmetric_epi {
     F f;
     template <int MI, int NI, bool RUN, int WM, int WN, class ACC>
     __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *lds) const {
-        // 2-byte words; the pitch keeps 16-byte alignment, and without the 8 the tile of 256 x 256 fills the shared memory of its operands
-        constexpr uint32_t TM = WM * MI * 16, TN = WN * NI * 16, PITCH = TM + (TM < 256 ? 8 : 0);
-        static_assert(TN * PITCH * 2 <= 2 * (TM + TN) * 128, "fits the operands' buffers");
+        // Transposed 2-byte words of one half, or of both where the operands' buffers hold them.  The pitch keeps 16-byte alignment; without the 8 a tile of
+        // 256 x 256 fills the buffers, as do both halves of one of 128.
+        constexpr uint32_t TM = WM * MI * 16, TN = WN * NI * 16, ROOM = 2 * (TM + TN) * 128, PITCH = TM + (TM == 256 || TM == 128 ? 0 : 8), HALF = TN * PITCH;
+        constexpr int AT_ONCE = 2 * HALF * 2 <= ROOM ? 2 : 1;
+        static_assert(HALF * 2 <= ROOM, "fits the operands' buffers");
         const uint32_t wide = (p.M + 7u) & ~7u, m0 = at.tile_m * TM, n0 = at.tile_n * TN;
         const size_t base = at.batch * out.stride;
         uint16_t *turned = (uint16_t *)lds;
-        const int halves = out.lo && at.tile_m != at.tile_n ? 2 : 1;
-        for (int half = 0; half < halves; half++) {
+        // all that is read before anything is written: the compiler may not move one past the other
+        float u[MI][NI][4];
 #pragma unroll
-            for (int i = 0; i < MI; i++) {
-                const uint32_t m = slz_row(at, i);
+        for (int i = 0; i < MI; i++)
 #pragma unroll
-                for (int j = 0; j < NI; j++) {
-                    const uint32_t n = slz_col<NI, RUN>(at, j);
-                    float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    if (m < p.M && n < p.M) f(at.batch, m, n, acc[i][j], u);
-                    if (at.tile_m == at.tile_n)
-#pragma unroll
-                        for (int c = 0; c < 4; c++)
-                            if (m == n + c && m < p.M) {
-                                diagonal[at.batch * p.M + m] = f.on_diagonal(at.batch, m, u[c]);
-                                u[c] = 0.0f;
-                            }
-#pragma unroll
-                    for (int c = 0; c < 4; c++) {
-                        if (n + c >= p.M) u[c] = 0.0f;
-                        _Float16 hi, lo;
-                        orth_halves(u[c], hi, lo);
-                        turned[(n - n0 + c) * PITCH + m - m0] = __builtin_bit_cast(uint16_t, half ? lo : hi);
-                    }
-                    if (half == 0 && m < p.M && n < wide) orth_put4(out, base + (size_t)m * out.ld + n, u);
-                }
+            for (int j = 0; j < NI; j++) {
+                const uint32_t m = slz_row(at, i), n = slz_col<NI, RUN>(at, j);
+                u[i][j][0] = u[i][j][1] = u[i][j][2] = u[i][j][3] = 0.0f;
+                if (m < p.M && n < p.M) f(at.batch, m, n, acc[i][j], u[i][j]);
             }
-            if (at.tile_m == at.tile_n) return;
+#pragma unroll
+        for (int i = 0; i < MI; i++)
+#pragma unroll
+            for (int j = 0; j < NI; j++) {
+                const uint32_t m = slz_row(at, i), n = slz_col<NI, RUN>(at, j);
+                if (at.tile_m == at.tile_n)
+#pragma unroll
+                    for (int c = 0; c < 4; c++)
+                        if (m == n + c && m < p.M) {
+                            diagonal[at.batch * p.M + m] = f.on_diagonal(at.batch, m, u[i][j][c]);
+                            u[i][j][c] = 0.0f;
+                        }
+#pragma unroll
+                for (int c = 0; c < 4; c++) u[i][j][c] = n + c < p.M ? u[i][j][c] : 0.0f;
+                if (m < p.M && n < wide) orth_put4(out, base + (size_t)m * out.ld + n, u[i][j]);
+            }
+        if (at.tile_m == at.tile_n) return;
+        const int halves = out.lo ? 2 : 1;
+        for (int first = 0; first < halves; first += AT_ONCE) {
+            const int last = min(halves, first + AT_ONCE);
+            for (int half = first; half < last; half++)
+#pragma unroll
+                for (int i = 0; i < MI; i++)
+#pragma unroll
+                    for (int j = 0; j < NI; j++)
+#pragma unroll
+                        for (int c = 0; c < 4; c++) {
+                            _Float16 hi, lo;
+                            orth_halves(u[i][j][c], hi, lo);
+                            turned[(half - first) * HALF + (slz_col<NI, RUN>(at, j) - n0 + c) * PITCH + slz_row(at, i) - m0] = __builtin_bit_cast(uint16_t, half ? lo : hi);
+                        }
             __syncthreads();
-            uint16_t *to = (half ? out.lo : out.hi) + base;
-            for (uint32_t g = threadIdx.x; g < TN * (TM / 8); g += WM * WN * 64) {
-                const uint32_t n = g / (TM / 8), m = g % (TM / 8) * 8;
-                if (n0 + n < p.M && m0 + m < wide) *(uint4 *)(to + (size_t)(n0 + n) * out.ld + m0 + m) = *(const uint4 *)(turned + n * PITCH + m);
+            for (int half = first; half < last; half++) {
+                uint16_t *to = (half ? out.lo : out.hi) + base;
+                for (uint32_t g = threadIdx.x; g < TN * (TM / 8); g += WM * WN * 64) {
+                    const uint32_t n = g / (TM / 8), m = g % (TM / 8) * 8;
+                    if (n0 + n < p.M && m0 + m < wide) *(uint4 *)(to + (size_t)(n0 + n) * out.ld + m0 + m) = *(const uint4 *)(turned + (half - first) * HALF + n * PITCH + m);
+                }
             }
             __syncthreads();
         }
@@ -237,21 +254,28 @@ struct orth_apply_epi {
     __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *) const {
         const uint32_t wide = (p.N + 7u) & ~7u;
         const float f = factor ? factor[at.batch] : 1.0f;
+        // a row's X is read before the row before it is written
+        float old[2][NI][4], d[2];
+        const auto load = [&](int i) {
+            const uint32_t m = min(slz_row(at, i), p.M - 1);
+            d[i & 1] = f * diagonal[at.batch * p.M + m];
+#pragma unroll
+            for (int j = 0; j < NI; j++) orth_get4(x, at.batch * x.stride + (size_t)m * x.ld + min(slz_col<NI, RUN>(at, j), wide - 4), old[i & 1][j]);
+        };
+        load(0);
 #pragma unroll
         for (int i = 0; i < MI; i++) {
+            if (i + 1 < MI) load(i + 1);
             const uint32_t m = slz_row(at, i);
             if (m >= p.M) continue;
-            const float d = f * diagonal[at.batch * p.M + m];
 #pragma unroll
             for (int j = 0; j < NI; j++) {
                 const uint32_t n = slz_col<NI, RUN>(at, j);
                 if (n >= wide) continue;
-                const size_t here = at.batch * x.stride + (size_t)m * x.ld + n;
-                float old[4], v[4];
-                orth_get4(x, here, old);
+                float v[4];
 #pragma unroll
-                for (int c = 0; c < 4; c++) v[c] = n + c < p.N ? d * old[c] + acc[i][j][c] * (f / ORTH_UP) : 0.0f;
-                if (!out) orth_put4(next, here, v);
+                for (int c = 0; c < 4; c++) v[c] = n + c < p.N ? d[i & 1] * old[i & 1][j][c] + acc[i][j][c] * (f / ORTH_UP) : 0.0f;
+                if (!out) orth_put4(next, at.batch * x.stride + (size_t)m * x.ld + n, v);
                 else if (n < p.N) {
 #pragma unroll
                     for (int c = 0; c < 4; c++) v[c] *= 1.0f / ORTH_UP;
