@@ -4,16 +4,21 @@
 
 // A thread makes 16 bytes of each piece of a job's result; jobs by grid y.
 template <int SRC> __device__ __forceinline__ void align_16(const slz_layout &j, size_t r, uint32_t c, char *to) {
-    constexpr int C = 16 / SRC;
-    union { uint8_t b[16]; uint16_t h[8]; uint4 v; } u;
-    u.v = make_uint4(0, 0, 0, 0);
+    constexpr uint32_t C = 16 / SRC;
+    const char *from = j.x + ((int64_t)r * j.ld + c) * SRC;
+    if (c + C <= j.cols) {
+        *(v4i32 *)to = *(const v4i32_any *)from;
+        return;
+    }
+    union { uint8_t b[16]; uint16_t h[8]; v4i32 v; } u;
+    u.v = v4i32{0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < C; i++)
+    for (uint32_t i = 0; i < C; i++)
         if (c + i < j.cols) {
-            if (SRC == 1) u.b[i] = ((const uint8_t *)j.x)[r * j.ld + c + i];
-            else u.h[i % 8] = ((const uint16_t *)j.x)[r * j.ld + c + i];
+            if (SRC == 1) u.b[i] = ((const uint8_t *)from)[i];
+            else u.h[i % 8] = ((const uint16_t *)from)[i];
         }
-    *(uint4 *)to = u.v;
+    *(v4i32 *)to = u.v;
 }
 __global__ void __launch_bounds__(256) k_layout(const slz_layouts jobs) {
     const slz_layout j = jobs.job[blockIdx.y];
@@ -29,9 +34,11 @@ __global__ void __launch_bounds__(256) k_layout(const slz_layouts jobs) {
         else {
             uint32_t w[3][4];
             uint16_t t[2][3];
+            float v[8];
+            row8_values<SLZ_F32>(row8_load<SLZ_F32>(j.x, r * j.ld, at / 2, j.cols), at / 2, j.cols, v);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                slz_split3(at / 2 + i < j.cols ? ((const float *)j.x)[r * j.ld + at / 2 + i] : 0.0f, t[i & 1]);
+                slz_split3(v[i], t[i & 1]);
                 if (i & 1)
                     for (int k = 0; k < 3; k++) w[k][i / 2] = t[0][k] | ((uint32_t)t[1][k] << 16);
             }

@@ -153,14 +153,14 @@ template <int MI, int NI, int A_LDS, int B_LDS, int... G> __device__ __forceinli
     (slz_order<(G + 2 < 2 * MI ? A_LDS : 0) + (G < MI ? B_LDS * ((G + 1) * NI / MI - G * NI / MI) : 0), NI>(), ...);
 }
 
-template <int EL, bool A_ROWS_K, bool B_ROWS_K, int TM, int TN, int WM, int WN, class EPI>
+template <int EL, bool A_ROWS_K, bool B_ROWS_K, int TM, int TN, int WM, int WN, int PIECES, class EPI>
 __global__ void __launch_bounds__(WM *WN * 64) k_gemm(const slz_gemm p, const EPI epi) {
     constexpr int WAVES = WM * WN, MI = TM / WM / 16, NI = TN / WN / 16, ES = slz_el<EL>::bytes, KS = 128 / ES;
     constexpr int A_LDS = A_ROWS_K ? 2 : 1, B_LDS = B_ROWS_K ? 2 : 1;           // instructions per operand
     using acc_t = typename slz_el<EL>::acc;
     using tile_a = slz_tile<A_ROWS_K, TM, WAVES, 0>;
     using tile_b = slz_tile<B_ROWS_K, TN, WAVES, B_ROWS_K ? 0 : NI * 4>;
-    __shared__ __attribute__((aligned(1024))) char lds[2][tile_a::BYTES + tile_b::BYTES];
+    __shared__ __attribute__((aligned(1024))) char lds[2][PIECES * (tile_a::BYTES + tile_b::BYTES)];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wave_m = wave / WN, wave_n = wave % WN;
     uint32_t tm, tn, range, batch;
@@ -185,6 +185,7 @@ __global__ void __launch_bounds__(WM *WN * 64) k_gemm(const slz_gemm p, const EP
         for (int j = 0; j < NI; j++) acc[i][j] = acc_t{0, 0, 0, 0};
 
     uint32_t pair = steps_k ? begin / steps_k : 0u, kt = begin - pair * steps_k;
+    constexpr int SECOND = tile_a::BYTES + tile_b::BYTES;           // second pieces' place
     const auto load_step = [&](int buffer) {
         const uint32_t k0 = kt * KS, left = p.K - k0;
         const uint32_t pieces = min((left * ES + 15u) / 16u, 8u), rows_k = min(left, (uint32_t)KS);
@@ -194,14 +195,41 @@ __global__ void __launch_bounds__(WM *WN * 64) k_gemm(const slz_gemm p, const EP
         const uint32_t bytes_b = B_ROWS_K ? (rows_k - 1) * ldb + ((p.N - n0) * ES + 15u) / 16u * 16u : (min(p.N - n0, (uint32_t)TN) - 1) * ldb + (left * ES + 15u) / 16u * 16u;
         ta.load(a, bytes_a, pieces, lds[buffer], wave);
         tb.load(b, bytes_b, pieces, lds[buffer] + tile_a::BYTES, wave);
+        if constexpr (PIECES == 2) {
+            ta.load(a + p.a_piece[1], bytes_a, pieces, lds[buffer] + SECOND, wave);
+            tb.load(b + p.b_piece[1], bytes_b, pieces, lds[buffer] + SECOND + tile_a::BYTES, wave);
+        }
         if (++kt == steps_k) { kt = 0; pair++; }
     };
     if (begin < end) load_step(0);
     for (uint32_t s = begin; s < end; s++) {
         const int buffer = (s - begin) & 1;
         __syncthreads();                               // this step's pieces are there; everyone is done with the other buffer
-        if (A_ROWS_K && s + 1 < end) load_step(buffer ^ 1);
+        if ((A_ROWS_K || PIECES == 2) && s + 1 < end) load_step(buffer ^ 1);
         const char *la = lds[buffer], *lb = la + tile_a::BYTES;
+        if constexpr (PIECES == 2) {
+            // numbers in two pieces, both loaded at once: three products of what is read once, the small ones first
+#pragma unroll
+            for (int kk = 0; kk < 2; kk++) {
+                v4i32 fb[2][NI], fa[2];
+#pragma unroll
+                for (int j = 0; j < NI; j++)
+#pragma unroll
+                    for (int q = 0; q < 2; q++) fb[q][j] = tb.template read<NI>(lb + q * SECOND, wave_n * (NI * 16), j, kk, lane);
+#pragma unroll
+                for (int i = 0; i < MI; i++) {
+#pragma unroll
+                    for (int q = 0; q < 2; q++) fa[q] = ta.template read<MI>(la + q * SECOND, wave_m * (MI * 16), i, kk, lane);
+#pragma unroll
+                    for (int j = 0; j < NI; j++) {
+                        acc[i][j] = slz_mma<EL>(fb[0][j], fa[1], acc[i][j]);
+                        acc[i][j] = slz_mma<EL>(fb[1][j], fa[0], acc[i][j]);
+                        acc[i][j] = slz_mma<EL>(fb[0][j], fa[0], acc[i][j]);
+                    }
+                }
+            }
+            continue;
+        }
         // 2 MI groups of NI matrix instructions, each with one operand of A; A's operands are read two groups ahead, B's for the
         // second half during the first: shared memory and the matrix cores are busy for about as long, and so at the same time
         v4i32 fa[3], fb[2][NI];
@@ -246,6 +274,7 @@ template <class F> struct slz_store_epi {
     uint32_t aligned;                // rows begin at multiples of 16 bytes
     F f;
     static constexpr bool any_side = true;
+    static constexpr int widest = 256;
     template <int MI, int NI, bool RUN, int WM, int WN, class ACC>
     __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *) const {
         constexpr int C = RUN ? NI * 4 : 4, PARTS = RUN ? 1 : NI;
@@ -279,6 +308,7 @@ template <class T> struct slz_partial_epi {
     T *ws;
     uint32_t ld, batches, add;
     static constexpr bool any_side = true;
+    static constexpr int widest = 256;
     template <int MI, int NI, bool RUN, int WM, int WN, class ACC>
     __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *) const {
 #pragma unroll
@@ -321,24 +351,25 @@ using slz_tiles_64 = slz_tiling<64, 64, 2, 2>;
 // with one of 128 and 0.88 with two at once, 0.33 with one of 64 and 0.18 for each of several (measured at 4096 deep: 3840^2 with 256: 99 us;
 // 2688^2 with 192: 63, with 128: 57; 768^2 with 256, 192, 128: 85, 58, 43).  Large tiles read less for each product, small ones fill the chip with less
 // and leave less of it idle at the end.  Ranges of k cost a second launch that reads their sums.
-struct slz_choice { uint32_t side, split; double us; };
-static inline double slz_step_us(uint32_t side, double tiles) {
+struct slz_choice { uint32_t side, split; double us; uint32_t pieces = 1; };     // pieces: of a number that are loaded together
+static inline double slz_step_us(uint32_t side, double tiles, uint32_t pieces) {
     const auto rounds = [&](double at_once) { return (double)(uint64_t)((tiles + at_once - 1) / at_once); };
+    if (pieces == 2) return side == 128 ? rounds(256) * 1.9 : rounds(256) * 0.42 > 0.5 ? rounds(256) * 0.42 : 0.5;
     if (side == 256) return rounds(256) * 1.5;
     if (side == 192) return rounds(256) * 0.95;
     if (side == 64) return rounds(256) * 0.18 > 0.33 ? rounds(256) * 0.18 : 0.33;
     const double pairs = (double)(uint64_t)(tiles / 512), rest = tiles - pairs * 512;
     return pairs * 0.88 + (rest > 256 ? 0.88 : rest > 0 ? 0.62 : 0.0);
 }
-static inline slz_choice slz_choose(uint32_t M, uint32_t N, uint32_t steps, uint32_t batches, bool symmetric, uint32_t most_ranges, bool any_side = true) {
+static inline slz_choice slz_choose(uint32_t M, uint32_t N, uint32_t steps, uint32_t batches, bool symmetric, uint32_t most_ranges, bool any_side = true, uint32_t pieces = 1) {
     slz_choice best = {64, 1, 1e30};
     for (const uint32_t side : {256u, 192u, 128u, 64u}) {
-        if (side == 192 && !any_side) continue;
+        if ((side == 192 && !any_side) || (side == 256 && symmetric) || (side > 128 && pieces == 2)) continue;
         const double tm = (M + side - 1) / side, tn = (N + side - 1) / side, tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batches;
         for (uint32_t split = 1; split <= most_ranges && (split == 1 || steps >= 4 * split); split *= 2) {
-            double us = ((steps + split - 1) / split) * slz_step_us(side, tiles * split);
+            double us = ((steps + split - 1) / split) * slz_step_us(side, tiles * split, pieces);
             if (split > 1) us += 4.0 + (double)M * N * batches * 4.0 * (split + 1) / 3e6;
-            if (us < best.us) best = {side, split, us};
+            if (us < best.us) best = {side, split, us, pieces};
         }
     }
     return best;
@@ -366,7 +397,7 @@ static inline uint32_t slz_gemm_steps(const slz_gemm &p, int element_bytes) {
     return (p.K + ks - 1) / ks * p.pairs;
 }
 
-template <class T, int EL, bool A_ROWS_K, bool B_ROWS_K, class EPI>
+template <class T, int EL, bool A_ROWS_K, bool B_ROWS_K, int PIECES = 1, class EPI>
 static int slz_gemm_launch(slz_gemm p, const EPI &epi, uint32_t batches, hipStream_t s) {
     p.tiles_m = (p.M + T::TM - 1) / T::TM;
     p.tiles_n = (p.N + T::TN - 1) / T::TN;
@@ -374,13 +405,20 @@ static int slz_gemm_launch(slz_gemm p, const EPI &epi, uint32_t batches, hipStre
     const uint64_t tiles = p.symmetric ? (uint64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (uint64_t)p.tiles_m * p.tiles_n;
     if (tiles == 0 || batches == 0) return SLZ_OK;
     if (tiles * p.split * batches > 0x7fffffffu) return SLZ_E_TOO_LARGE;
-    hipLaunchKernelGGL((k_gemm<EL, A_ROWS_K, B_ROWS_K, T::TM, T::TN, T::WM, T::WN, EPI>), dim3((uint32_t)tiles, p.split, batches),
+    hipLaunchKernelGGL((k_gemm<EL, A_ROWS_K, B_ROWS_K, T::TM, T::TN, T::WM, T::WN, PIECES, EPI>), dim3((uint32_t)tiles, p.split, batches),
                        dim3(T::WM * T::WN * 64), 0, s, p, epi);
     return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
 }
+// operands of two pieces (a_piece[1] and b_piece[1]: the second ones), tiles of 128 or 64
+template <int EL, bool A_ROWS_K, bool B_ROWS_K, class EPI>
+static int slz_gemm_run2(const slz_gemm &p, const EPI &epi, uint32_t side, uint32_t batches, hipStream_t s) {
+    if (side == 128) return slz_gemm_launch<slz_tiling<128, 128, 2, 4>, EL, A_ROWS_K, B_ROWS_K, 2>(p, epi, batches, s);
+    return slz_gemm_launch<slz_tiles_64, EL, A_ROWS_K, B_ROWS_K, 2>(p, epi, batches, s);
+}
 template <int EL, bool A_ROWS_K, bool B_ROWS_K, class EPI>
 static int slz_gemm_run(const slz_gemm &p, const EPI &epi, uint32_t side, uint32_t batches, hipStream_t s) {
-    if (side == 256) return slz_gemm_launch<slz_tiles_256, EL, A_ROWS_K, B_ROWS_K>(p, epi, batches, s);
+    if constexpr (EPI::widest == 256)
+        if (side == 256) return slz_gemm_launch<slz_tiles_256, EL, A_ROWS_K, B_ROWS_K>(p, epi, batches, s);
     if constexpr (EPI::any_side)
         if (side == 192) return slz_gemm_launch<slz_tiles_192, EL, A_ROWS_K, B_ROWS_K>(p, epi, batches, s);
     // eight waves where an operand's rows are k: 768^2 by 4096 deep 58 us, with four 67; 43 and 45 where k is contiguous, but 4096^3 141 and 133

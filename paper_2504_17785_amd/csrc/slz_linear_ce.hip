@@ -21,6 +21,7 @@ __device__ __forceinline__ float2 ce_both(float2 p, float2 q) {
 // One pair for every 32 words, whatever the tiling: sums of eight, then of four such.  A token's loss so has the same bits alone and among others.
 #define CE_BLOCK 32
 struct ce_lse_epi {
+    static constexpr int widest = 256;
     static constexpr bool any_side = false;            // blocks of 32 words lie within a wave's columns
     float2 *pairs;                   // [block of words][tokens]
     float *label_z;
@@ -98,6 +99,7 @@ k_ce_join(const float2 *__restrict__ pairs, const float *__restrict__ label_z, c
 
 // g of a piece: [pieces][tokens][ld], columns from N to the next multiple of 8 zero
 struct ce_grad_epi {
+    static constexpr int widest = 256;
     static constexpr bool any_side = false;            // eight columns of a lane at a time
     char *g;
     int64_t ld, piece;               // bytes

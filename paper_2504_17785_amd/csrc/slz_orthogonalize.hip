@@ -129,14 +129,15 @@ k_orth_store(orth_view x, const float *__restrict__ factor, void *__restrict__ o
 // A tile below the diagonal is stored a second time, transposed through shared memory, half by half.
 template <class F> struct orth_symmetric_epi {
     static constexpr bool any_side = true;
+    static constexpr int widest = 192;
     orth_view out;
     float *diagonal;                 // [batch][m]
     F f;
     template <int MI, int NI, bool RUN, int WM, int WN, class ACC>
     __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *lds) const {
-        // Transposed 2-byte words of one half, or of both where the operands' buffers hold them.  The pitch keeps 16-byte alignment; without the 8 a tile of
-        // 256 x 256 fills the buffers, as do both halves of one of 128.
-        constexpr uint32_t TM = WM * MI * 16, TN = WN * NI * 16, ROOM = 2 * (TM + TN) * 128, PITCH = TM + (TM == 256 || TM == 128 ? 0 : 8), HALF = TN * PITCH;
+        // Transposed 2-byte words of one half, or of both where the operands' buffers hold them.  The pitch keeps 16-byte alignment; without the 8 both
+        // halves of a tile of 128 x 128 fill the buffers.
+        constexpr uint32_t TM = WM * MI * 16, TN = WN * NI * 16, ROOM = 2 * (TM + TN) * 128, PITCH = TM + (TM == 128 ? 0 : 8), HALF = TN * PITCH;
         constexpr int AT_ONCE = 2 * HALF * 2 <= ROOM ? 2 : 1;
         static_assert(HALF * 2 <= ROOM, "fits the operands' buffers");
         const uint32_t wide = (p.M + 7u) & ~7u, m0 = at.tile_m * TM, n0 = at.tile_n * TN;
@@ -243,6 +244,7 @@ struct orth_polynomial {
 };
 struct orth_apply_epi {
     static constexpr bool any_side = true;
+    static constexpr int widest = 256;
     orth_view x, next;               // this step's X and the next one's
     const float *diagonal;           // a + B_ii
     const float *factor;             // or null
@@ -620,8 +622,7 @@ struct orth_plan {
     uint32_t ld_x, ld_a;
     size_t one_x, one_a;             // bytes of a piece of X, of A or B
     size_t x[2], a, b, da, db, factor, part, total;
-    slz_choice gram;
-    uint32_t polynomial, apply;                      // sides of their tiles
+    slz_choice gram, polynomial, apply;
     size_t ranges;
     uint32_t padded, slice, slices;                  // up to 128 rows: rows padded, columns of a workgroup, workgroups of a matrix
     size_t sums[2];
@@ -633,6 +634,13 @@ static void small_slices(orth_plan &P) {
     if (all <= 8192 && small_lds(P.padded, P.pieces, all) <= SMALL_LDS) { P.slice = all; P.slices = 1; return; }
     P.slice = 16384 / P.padded;
     P.slices = (P.n + P.slice - 1) / P.slice;
+}
+// Two pieces: three products one after the other in any tiling, or tiles of 128 or 64 that load both pieces at once.  These read a third less, but large
+// tiles read less still: f32, 6 x 500 x 1000 277 us together and 345 in turn, 1024^2 279 and 431, 4096 x 8192 9532 and 6889
+static slz_choice orth_choose(const orth_plan &P, uint32_t N, uint32_t steps, uint32_t batch, bool symmetric, uint32_t most_ranges) {
+    if (P.pieces == 1) return slz_choose(P.m, N, steps, batch, symmetric, most_ranges);
+    const slz_choice in_turn = slz_choose(P.m, N, steps * 3, batch, symmetric, most_ranges), together = slz_choose(P.m, N, steps, batch, symmetric, most_ranges, true, 2);
+    return together.us < in_turn.us ? together : in_turn;
 }
 static orth_plan plan_orth(const slz_orth_shape *sh) {
     orth_plan P = {};
@@ -665,14 +673,14 @@ static orth_plan plan_orth(const slz_orth_shape *sh) {
     P.db = o; o += up256((size_t)sh->batch * P.m * 4);
     P.factor = o; o += up256((size_t)sh->batch * 4);
     P.part = o; o += up256((size_t)sh->batch * ORTH_NORM_BLOCKS * 8);
-    const uint32_t pairs = P.pieces == 2 ? 3 : 1, steps = (P.n + 63) / 64 * pairs;
-    P.gram = slz_choose(P.m, P.m, steps, sh->batch, true, 1);
-    const slz_choice cut = slz_choose(P.m, P.m, steps, sh->batch, false, 32);
+    const uint32_t steps = (P.n + 63) / 64;
+    P.gram = orth_choose(P, P.m, steps, sh->batch, true, 1);
+    const slz_choice cut = orth_choose(P, P.m, steps, sh->batch, false, 32);
     if (cut.us < P.gram.us && P.m <= 65535) P.gram = cut;
     P.ranges = o; o += P.gram.split > 1 ? up256((size_t)P.gram.split * sh->batch * P.m * slz_ranges_ld(P.m) * 4) : 0;
     P.total = o;
-    P.polynomial = slz_choose(P.m, P.m, (P.m + 63) / 64 * pairs, sh->batch, true, 1).side;
-    P.apply = slz_choose(P.m, P.n, (P.m + 63) / 64 * pairs, sh->batch, false, 1).side;
+    P.polynomial = orth_choose(P, P.m, (P.m + 63) / 64, sh->batch, true, 1);
+    P.apply = orth_choose(P, P.n, (P.m + 63) / 64, sh->batch, false, 1);
     return P;
 }
 static int orth_check(const slz_orth_shape *sh) {
@@ -689,17 +697,16 @@ extern "C" int slz_orthogonalize_workspace(const slz_orth_shape *sh, size_t *byt
     return SLZ_OK;
 }
 
-// operands of one or two pieces; the pairs whose share of the sum is 2^-11 and more, the small ones first
-static slz_gemm orth_product(const orth_view &a, const orth_view &b, uint32_t pieces, uint32_t M, uint32_t N, uint32_t K) {
+static slz_gemm orth_product(const orth_view &a, const orth_view &b, uint32_t pieces, const slz_choice &c, uint32_t M, uint32_t N, uint32_t K) {
     slz_gemm p = {};
     p.a = (const char *)a.hi; p.b = (const char *)b.hi;
     p.lda = (int64_t)a.ld * 2; p.ldb = (int64_t)b.ld * 2;
     p.a_batch = (int64_t)a.stride * 2; p.b_batch = (int64_t)b.stride * 2;
     p.M = M; p.N = N; p.K = K;
     p.split = 1;
-    p.pairs = pieces == 2 ? 3 : 1;
+    p.pairs = pieces == 2 && c.pieces == 1 ? 3 : 1;    // in turn, the small products first
     if (pieces == 2) {
-        p.a_piece[0] = (const char *)a.lo - (const char *)a.hi;
+        p.a_piece[c.pieces == 2 ? 1 : 0] = (const char *)a.lo - (const char *)a.hi;
         p.b_piece[1] = (const char *)b.lo - (const char *)b.hi;
     }
     return p;
@@ -770,6 +777,9 @@ static int orth_small(const slz_orth_shape *sh, const orth_plan &P, const void *
     return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
 }
 
+template <bool B_ROWS_K, class EPI> static int orth_run(const slz_gemm &p, const EPI &epi, const slz_choice &c, uint32_t batches, hipStream_t s) {
+    return c.pieces == 2 ? slz_gemm_run2<SLZ_EL_F16, false, B_ROWS_K>(p, epi, c.side, batches, s) : slz_gemm_run<SLZ_EL_F16, false, B_ROWS_K>(p, epi, c.side, batches, s);
+}
 extern "C" int slz_orthogonalize(const slz_orth_shape *sh, const void *g, void *out, void *ws, size_t ws_bytes, void *stream) {
     const int rc0 = orth_check(sh);
     if (rc0 != SLZ_OK) return rc0;
@@ -798,26 +808,26 @@ extern "C" int slz_orthogonalize(const slz_orth_shape *sh, const void *g, void *
     for (uint32_t i = 0; i < sh->steps; i++) {
         const orth_view &now = x[i & 1], &next = x[(i & 1) ^ 1];
         const float *f = i == 0 ? factor : nullptr;
-        slz_gemm p = orth_product(now, now, P.pieces, P.m, P.m, P.n);
+        slz_gemm p = orth_product(now, now, P.pieces, P.gram, P.m, P.m, P.n);
         int rc;
         if (P.gram.split == 1) {
             p.symmetric = 1;
-            rc = slz_gemm_run<SLZ_EL_F16, false, false>(p, orth_symmetric_epi<orth_gram>{a, da, {f}}, P.gram.side, sh->batch, s);
+            rc = orth_run<false>(p, orth_symmetric_epi<orth_gram>{a, da, {f}}, P.gram, sh->batch, s);
         } else {
             const uint32_t ld = slz_ranges_ld(P.m);
             p.split = P.gram.split;
-            rc = slz_gemm_run<SLZ_EL_F16, false, false>(p, slz_partial_epi<float>{(float *)(w + P.ranges), ld, sh->batch, 0}, P.gram.side, sh->batch, s);
+            rc = orth_run<false>(p, slz_partial_epi<float>{(float *)(w + P.ranges), ld, sh->batch, 0}, P.gram, sh->batch, s);
             hipLaunchKernelGGL(k_orth_gram_join, dim3((P.m + 1030) / 1024, P.m, sh->batch), dim3(256), 0, s, (const float *)(w + P.ranges), P.gram.split, sh->batch,
                                P.m, ld, orth_gram{f}, a, da);
         }
         if (rc != SLZ_OK) return rc;
-        p = orth_product(a, a, P.pieces, P.m, P.m, P.m);
+        p = orth_product(a, a, P.pieces, P.polynomial, P.m, P.m, P.m);
         p.symmetric = 1;
-        rc = slz_gemm_run<SLZ_EL_F16, false, false>(p, orth_symmetric_epi<orth_polynomial>{b, db, {a, da, P.m, sh->a, sh->b, sh->c}}, P.polynomial, sh->batch, s);
+        rc = orth_run<false>(p, orth_symmetric_epi<orth_polynomial>{b, db, {a, da, P.m, sh->a, sh->b, sh->c}}, P.polynomial, sh->batch, s);
         if (rc != SLZ_OK) return rc;
-        p = orth_product(b, now, P.pieces, P.m, P.n, P.m);
+        p = orth_product(b, now, P.pieces, P.apply, P.m, P.n, P.m);
         const orth_apply_epi epi{now, next, db, f, i + 1 == sh->steps ? out : nullptr, sh->type, tall, aligned, sh->ld_out, sh->stride_out};
-        rc = slz_gemm_run<SLZ_EL_F16, false, true>(p, epi, P.apply, sh->batch, s);
+        rc = orth_run<true>(p, epi, P.apply, sh->batch, s);
         if (rc != SLZ_OK) return rc;
     }
     SLZ_HIP(hipGetLastError());
