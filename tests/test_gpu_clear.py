@@ -563,3 +563,12 @@ def test_the_binding_refuses(slz):
         slz.orthogonalize(x[0])
     with pytest.raises(slz.SlzError):
         slz.linear_ce(h, v[:0], labels)
+
+
+def test_the_example_learns_and_answers_in_8_bits():
+    import examples.clear_step as example
+    losses, right, one, among = example.train(steps=40)
+    # ten classes: the loss begins near log 10 and the classes are far apart (0.3 sqrt(784) = 8 deviations)
+    assert losses[0] > 1.5 and sum(losses[-5:]) / 5 < 0.5 * losses[0]
+    assert right > 0.9
+    assert torch.equal(one, among)                     # an input answered alone and among others
