@@ -77,7 +77,8 @@ typedef struct {
 
 /* z_tv = sum_d h_td w_vd, lse_t = log sum_v exp z_tv, loss_t = lse_t - z_t,label.  loss is 0 where the label is ignore_index and NaN
  * where another label lies outside [0, vocab).  The z are summed and kept in 32 bits, a tile of the vocabulary at a time; none
- * is written to memory.  labels int64 [tokens], loss and lse [tokens] 32-bit floating point. */
+ * is written to memory.  A z of NaN or +inf makes its token's results NaN; one of -inf adds nothing (f32: an infinity in h or w
+ * counts as NaN).  A token's results have the same bits whatever the other tokens are.  labels int64 [tokens], loss and lse [tokens] 32-bit floating point. */
 int slz_linear_ce_workspace(const slz_ce_shape *shape, const void *h_dev, const void *w_dev, size_t *bytes);
 int slz_linear_ce(const slz_ce_shape *shape, const void *h_dev, const void *w_dev, const int64_t *labels_dev, float *loss_dev,
                   float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream);

@@ -81,10 +81,13 @@ slz_operand slz_operand_i8_of(const int8_t *p, uint32_t rows, uint32_t cols, int
     return o;
 }
 
-// One workgroup: the power of two at or above the largest of the magnitudes (1 where there is none that is finite)
+// One workgroup: the power of two above the largest of the finite magnitudes (1 where there is none)
 __global__ void __launch_bounds__(256) k_scale_unit(const float *__restrict__ scale, uint32_t count, float *__restrict__ unit) {
     float top = 0.0f;
-    for (uint32_t i = threadIdx.x; i < count; i += 256) top = fmaxf(top, fabsf(scale[i]));
+    for (uint32_t i = threadIdx.x; i < count; i += 256) {
+        const float a = fabsf(scale[i]);
+        if (a < __builtin_inff()) top = fmaxf(top, a);
+    }
     top = slz_wave_max(top);
     __shared__ float tops[4];
     if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
@@ -92,8 +95,8 @@ __global__ void __launch_bounds__(256) k_scale_unit(const float *__restrict__ sc
     if (threadIdx.x == 0) {
         top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
         int e = 0;
-        if (top > 0.0f && top < __builtin_inff()) frexpf(top, &e);
-        *unit = ldexpf(1.0f, e < -120 ? -120 : e > 120 ? 120 : e);
+        if (top > 0.0f) frexpf(top, &e);
+        *unit = ldexpf(1.0f, e < -100 ? -100 : e > 100 ? 100 : e);
     }
 }
 

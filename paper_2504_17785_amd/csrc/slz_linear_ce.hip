@@ -9,6 +9,7 @@
 
 // a piece's g takes this much at most (at least 1024 words of the vocabulary)
 #define CE_PIECE_BYTES ((size_t)128 << 20)
+#define CE_PIECE_WORDS ((size_t)1 << 21)     // rows of g stay as short as any operand's
 // f16: g is held times this; |g| <= |dloss|, so that the largest stay finite and those from 2^-28 of the largest keep 11 bits
 #define CE_F16_UP 16384.0f
 
@@ -16,6 +17,12 @@
 __device__ __forceinline__ float2 ce_both(float2 p, float2 q) {
     const float top = fmaxf(p.x, q.x), from = top == -__builtin_inff() ? 0.0f : top;
     return make_float2(top, p.y * __expf(p.x - from) + q.y * __expf(q.x - from));
+}
+
+// which of `count` words from `first` on the label is, or -1
+__device__ __forceinline__ int ce_word(int64_t label, uint32_t first, uint32_t count) {
+    const uint64_t d = (uint64_t)label - first;
+    return d < count ? (int)d : -1;
 }
 
 // One pair for every 32 words, whatever the tiling: sums of eight, then of four such.  A token's loss so has the same bits alone and among others.
@@ -30,13 +37,19 @@ struct ce_lse_epi {
     template <int MI, int NI, bool RUN, int WM, int WN, class ACC>
     __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *) const {
         static_assert(RUN && (NI == 2 || NI == 4), "a lane has 8 or 16 columns, four or two lanes a block");
+        if (at.n0 + NI * 16u <= p.N) part<MI, NI, RUN, true>(acc, at, p);
+        else part<MI, NI, RUN, false>(acc, at, p);
+    }
+    // WHOLE: all the wave's columns are words
+    template <int MI, int NI, bool RUN, bool WHOLE, class ACC>
+    __device__ __forceinline__ void part(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p) const {
         const uint32_t n0 = slz_col<NI, RUN>(at, 0);
 #pragma unroll
         for (int i = 0; i < MI; i++) {
             const uint32_t m = slz_row(at, i);
             float top = -__builtin_inff();
 #pragma unroll
-            for (int c = 0; c < NI * 4; c++) top = n0 + c < p.N ? fmaxf(top, acc[i][c / 4][c % 4]) : top;
+            for (int c = 0; c < NI * 4; c++) top = WHOLE || n0 + c < p.N ? fmaxf(top, acc[i][c / 4][c % 4]) : top;
             top = fmaxf(top, __shfl_xor(top, 16, 64));
             if (NI == 2) top = fmaxf(top, __shfl_xor(top, 32, 64));
             const float from = top == -__builtin_inff() ? 0.0f : top;
@@ -45,15 +58,15 @@ struct ce_lse_epi {
             for (int h = 0; h < NI / 2; h++) {
                 sums[h] = 0.0f;
 #pragma unroll
-                for (int c = h * 8; c < h * 8 + 8; c++) sums[h] += n0 + c < p.N ? __expf(acc[i][c / 4][c % 4] - from) : 0.0f;
+                for (int c = h * 8; c < h * 8 + 8; c++) sums[h] += WHOLE || n0 + c < p.N ? __expf(acc[i][c / 4][c % 4] - from) : 0.0f;
             }
             float sum = sums[0];
             if (NI == 4) sum += sums[NI / 2 - 1];
             sum += __shfl_xor(sum, 16, 64);
             if (NI == 2) sum += __shfl_xor(sum, 32, 64);
             if (m >= p.M || n0 >= p.N) continue;
-            const int64_t word = labels[m] - first_word - n0;
-            if (word >= 0 && word < NI * 4 && n0 + word < p.N) {
+            const int word = ce_word(labels[m], first_word + n0, min(NI * 4u, p.N - n0));
+            if (word >= 0) {
                 float z = 0.0f;
 #pragma unroll
                 for (int c = 0; c < NI * 4; c++) z = word == c ? acc[i][c / 4][c % 4] : z;
@@ -111,6 +124,11 @@ struct ce_grad_epi {
     template <int MI, int NI, bool RUN, int WM, int WN, class ACC>
     __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *) const {
         static_assert(RUN && NI % 2 == 0, "");
+        if (at.n0 + NI * 16u <= p.N) part<MI, NI, RUN, true>(acc, at, p);
+        else part<MI, NI, RUN, false>(acc, at, p);
+    }
+    template <int MI, int NI, bool RUN, bool WHOLE, class ACC>
+    __device__ __forceinline__ void part(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p) const {
         const uint32_t n0 = slz_col<NI, RUN>(at, 0), wide = (p.N + 7u) & ~7u;
         const float up = type == SLZ_F16 ? CE_F16_UP / *unit : 1.0f;
 #pragma unroll
@@ -120,16 +138,16 @@ struct ce_grad_epi {
             const int64_t label = labels[m];
             const bool counts = label != ignore;
             const float by = label < 0 || label >= (int64_t)vocab ? __builtin_nanf("") : dloss[m] * up, l = lse[m];
-            const int64_t word = label - first_word - n0;
+            const int word = ce_word(label, first_word + n0, NI * 4);
 #pragma unroll
             for (int q = 0; q < NI / 2; q++) {
                 const uint32_t n = n0 + q * 8u;
-                if (n >= wide) continue;
+                if (!WHOLE && n >= wide) continue;
                 float v[8];
 #pragma unroll
                 for (int c = 0; c < 8; c++) {
                     const float z = acc[i][q * 2 + c / 4][c % 4], e = type == SLZ_F32 ? expf(z - l) : __expf(z - l);
-                    v[c] = counts && n + c < p.N ? (e - (word == q * 8 + c ? 1.0f : 0.0f)) * by : 0.0f;
+                    v[c] = counts && (WHOLE || n + c < p.N) ? (e - (word == q * 8 + c ? 1.0f : 0.0f)) * by : 0.0f;
                 }
                 char *to = g + (int64_t)m * ld + (int64_t)n * 2;
                 if (type == SLZ_F32) {
@@ -354,6 +372,7 @@ static ce_plan plan_ce(const slz_ce_shape *sh, const void *h, const void *w, boo
     size_t words = sh->vocab;
     const size_t for_g = CE_PIECE_BYTES / (2 * pieces * (sh->tokens ? sh->tokens : 1)), for_w = CE_PIECE_BYTES / (2 * pieces * sh->inner);
     if (grad && words > for_g) words = for_g;
+    if (grad && words > CE_PIECE_WORDS) words = CE_PIECE_WORDS;
     if (!w_there && words > for_w) words = for_w;
     if (words < sh->vocab) {
         uint32_t unit = 65536, rows = (sh->tokens + 255) / 256;

@@ -244,7 +244,7 @@ def ce_inputs(tokens, inner, vocab, dtype, seed, slack=0, skip=0):
 
 LOSSES = [(1, 1, 1), (1, 64, 2), (8, 8, 3), (5, 128, 10), (32, 128, 10), (1, 512, 5000), (16, 256, 1000), (33, 40, 129), (128, 64, 128), (130, 72, 257), (200, 264, 1025),
           (515, 128, 3001), (3, 1000, 40), (129, 17, 130),
-          (33, 128, 10), (300, 100, 16), (9000, 20, 7), (100, 500, 32), (100, 513, 32), (5, 8192, 2), (70, 2047, 8), (1100, 3000, 40)]
+          (33, 128, 10), (300, 100, 16), (100, 512, 16), (9000, 20, 7), (100, 500, 32), (100, 513, 32), (5, 8192, 2), (70, 2047, 8), (1100, 3000, 40)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -326,6 +326,37 @@ def test_linear_ce_in_several_pieces_of_the_vocabulary(slz):
     z *= dloss[:, None]
     want = z.t().contiguous() @ h.float()
     assert ((dw.float() - want).norm() <= 3 * U[torch.bfloat16] * want.norm()), sums
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradients_of_any_scale(slz, dtype):
+    # f16 holds what is relative to the largest: gradients of 1e-30 or 1e4, and an ignored token's that is not a number
+    h, w, labels, dloss = ce_inputs(40, 64, 300, dtype, 42)
+    labels[7] = IGNORED
+    for scale in (1e-3, 1e3):
+        by = dloss * scale
+        check_ce(slz, h, w, labels, by)
+        by[7] = float("inf")
+        lse = slz.linear_ce(h, w, labels)[1]
+        first = slz.linear_ce_grad(h, w, labels, lse, by)
+        by[7] = 0
+        second = slz.linear_ce_grad(h, w, labels, lse, by)
+        assert torch.equal(first[0], second[0]) and torch.equal(first[1], second[1])
+    if dtype == torch.float32:
+        dh, dw = slz.linear_ce_grad(h, w, labels, lse, dloss * 1e-30)
+        one, two = slz.linear_ce_grad(h, w, labels, lse, dloss)
+        for got, want in ((dh, one), (dw, two)):
+            assert ((got.to(WIDE) * 1e30 - want.to(WIDE)).norm() <= 2.0 ** -20 * want.to(WIDE).norm())
+
+
+def test_a_loss_has_the_same_bits_alone_and_among_others(slz):
+    for dtype in TYPES:
+        for inner, vocab in ((64, 10), (72, 700), (520, 5000)):
+            h, w, labels, _ = ce_inputs(900, inner, vocab, dtype, 43)
+            loss, lse = slz.linear_ce(h, w, labels)
+            for part in (slice(0, 1), slice(5, 12), slice(100, 250), slice(3, 900, 7)):
+                a, b = slz.linear_ce(h[part].contiguous(), w, labels[part].contiguous())
+                assert torch.equal(a, loss[part]) and torch.equal(b, lse[part])
 
 
 def test_linear_ce_past_four_gib(slz):
