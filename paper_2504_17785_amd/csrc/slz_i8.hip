@@ -29,7 +29,8 @@ __device__ __forceinline__ uint2 quantize8(const float (&v)[8], bool finite, flo
         for (int i = 0; i < 8; i++) w[i / 4] |= (uint32_t)(uint8_t)quantize_one(v[i], up, inv) << (8 * (i & 3));
     return make_uint2(w[0], w[1]);
 }
-// One workgroup per row; bound by its latency for few rows (2.5 us) and by memory for many (4096 x 4096 bf16: 11.5 us, 4.3 TB/s).  A row of up to 16 entries a thread stays in registers, of a longer one the rest is read again from the cache.
+// One workgroup per row; bound by its latency for few rows (2.5 us) and by memory for many (4096 x 4096 bf16: 12.4 us, 4.1 TB/s).  A row of up to 16
+// entries a thread stays in registers, of a longer one the rest is read again from the cache.
 #define QUANTIZE_KEPT 2
 template <int TYPE>
 __global__ void __launch_bounds__(256)
@@ -412,7 +413,7 @@ extern "C" int slz_linear_i8(const slz_i8_shape *sh, const void *x, const int8_t
 // dy times the values scale_r q_rc: these are laid out as an operand once (bf16, or three bf16 for f32), then two ordinary products.  f16 could
 // not hold small scales, so its values are divided by `unit`, the power of two above the largest scale, and the sums multiplied by it.
 typedef uint64_t u64_any __attribute__((aligned(1)));
-// eight values of a row per thread
+// eight values of a row per thread: 4096 x 4096 to bf16 23.1 us (48 MiB, 2.2 TB/s)
 __global__ void __launch_bounds__(256)
 k_values(const int8_t *__restrict__ q, const float *__restrict__ scale, const float *__restrict__ unit, int type, uint32_t rows, uint32_t cols, int64_t ld_q,
          char *__restrict__ out, uint32_t ld_out, int64_t piece) {

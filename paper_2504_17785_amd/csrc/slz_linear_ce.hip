@@ -5,6 +5,9 @@
 // the label's z; a second kernel joins a token's pairs.
 // Gradient: in pieces of the vocabulary, z again, from it g = (exp(z - lse) - [v = label]) dloss to the workspace, then the two products
 // dw = g^T h (complete for the piece's rows) and dh += g w (summed over the pieces in 32 bits).
+// Bound by the matrix cores where rows are long: 4096 tokens x 4096 x 131072 bf16: forward 3.40 ms (1.29 PFLOP/s), each 16384 words' g 496 us (1.11),
+// dw 540 (1.02), dh 514 (1.07).  Short rows leave the epilogues: 1003 x 768 x 50021 f16: forward 108 us (0.71), g 157 (0.49), dw 133, dh 108; tiles of 256 instead of
+// the 128 taken: 105, 163, 163, 106.
 #include "slz_gemm.h"
 
 // a piece's g takes this much at most (at least 1024 words of the vocabulary)
@@ -77,7 +80,8 @@ struct ce_lse_epi {
     }
 };
 
-// 16 tokens per workgroup; each token's blocks go to 64 threads in turn, whose pairs are joined in a fixed order
+// 16 tokens per workgroup; each token's blocks go to 64 threads in turn, whose pairs are joined in a fixed order.  Bound by memory (4096 tokens x 4096
+// blocks: 28.6 us, 4.7 TB/s), for few tokens by latency (8 x 2048: 6.7 us).  256 threads a token: 4.7 there, but 11.2 instead of 8.2 for 1003 x 1564.
 __global__ void __launch_bounds__(1024)
 k_ce_join(const float2 *__restrict__ pairs, const float *__restrict__ label_z, const int64_t *__restrict__ labels, float *__restrict__ loss,
           float *__restrict__ lse, uint32_t tokens, uint32_t blocks, uint32_t vocab, int64_t ignore) {
@@ -169,7 +173,7 @@ struct ce_grad_epi {
 // ---- few classes ---------------------------------------------------------------------------------------------------------------------------
 // A classifier's head: w fits a workgroup's shared memory in 32 bits, a wave computes all of a token's z, and the whole call is one launch (the
 // gradient of many tokens: two), where the tiled products would be four to eight.  Taken by the sizes of w alone, so that a token's loss does not
-// depend on how many there are.
+// depend on how many there are.  32 tokens x 128 x 10: loss 6.1 us, gradient 14.8 in its one workgroup, both less than the host's time for a call.
 #define FEW_CLASSES 16
 #define FEW_INNER 512                // longer rows leave too few tokens of a workgroup at a time
 #define FEW_WEIGHTS (FEW_CLASSES * FEW_INNER)
