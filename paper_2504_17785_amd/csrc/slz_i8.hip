@@ -413,33 +413,37 @@ extern "C" int slz_linear_i8(const slz_i8_shape *sh, const void *x, const int8_t
 // dy times the values scale_r q_rc: these are laid out as an operand once (bf16, or three bf16 for f32), then two ordinary products.  f16 could
 // not hold small scales, so its values are divided by `unit`, the power of two above the largest scale, and the sums multiplied by it.
 typedef uint64_t u64_any __attribute__((aligned(1)));
-// eight values of a row per thread: 4096 x 4096 to bf16 23.1 us (48 MiB, 2.2 TB/s)
+// eight values of a row per thread; bound by memory: 4096 x 4096 to bf16 10.5 us (48 MiB, 4.8 TB/s)
+template <int TYPE>
 __global__ void __launch_bounds__(256)
-k_values(const int8_t *__restrict__ q, const float *__restrict__ scale, const float *__restrict__ unit, int type, uint32_t rows, uint32_t cols, int64_t ld_q,
+k_values(const int8_t *__restrict__ q, const float *__restrict__ scale, const float *__restrict__ unit, uint32_t rows, uint32_t cols, int64_t ld_q,
          char *__restrict__ out, uint32_t ld_out, int64_t piece) {
     const uint32_t per_row = ld_out / 16u;
     const size_t total = (size_t)rows * per_row;
+    constexpr int PIECES = TYPE == SLZ_F32 ? 3 : 1;
     for (size_t g = (size_t)blockIdx.x * 256 + threadIdx.x; g < total; g += (size_t)gridDim.x * 256) {
         uint32_t c;
         const size_t r = slz_divide(g, per_row, total <= 0xffffffffu, c);
         c *= 8;
-        const float sc = type == SLZ_F16 ? scale[r] / *unit : scale[r];
+        const float sc = TYPE == SLZ_F16 ? scale[r] / *unit : scale[r];
         uint64_t bytes = 0;
         if (c + 8u <= cols) bytes = *(const u64_any *)(q + r * ld_q + c);
         else
             for (uint32_t i = 0; i < 8 && c + i < cols; i++) bytes |= (uint64_t)(uint8_t)q[r * ld_q + c + i] << (8 * i);
-        uint16_t t[3][8];
+        uint16_t t[PIECES][8];
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             const float v = (float)(int8_t)(bytes >> (8 * i)) * sc;
-            if (type == SLZ_F32) {
+            if constexpr (TYPE == SLZ_F32) {
                 uint16_t u[3];
                 slz_split3(v, u);
-                t[0][i] = u[0]; t[1][i] = u[1]; t[2][i] = u[2];
-            } else t[0][i] = slz_half(v, type);
+                for (int k = 0; k < 3; k++) t[k][i] = u[k];
+            } else t[0][i] = slz_half(v, TYPE);
         }
-        for (int k = 0; k < (type == SLZ_F32 ? 3 : 1); k++) {
+#pragma unroll
+        for (int k = 0; k < PIECES; k++) {
             uint32_t w[4];
+#pragma unroll
             for (int i = 0; i < 4; i++) w[i] = t[k][2 * i] | ((uint32_t)t[k][2 * i + 1] << 16);
             *(uint4 *)(out + k * piece + r * ld_out + (size_t)c * 2) = make_uint4(w[0], w[1], w[2], w[3]);
         }
@@ -477,8 +481,10 @@ static int grad_product(const slz_i8_shape *sh, const slz_operand &left, bool le
     const int type = sh->type;
     const slz_operand right{values, (int64_t)P.row, (int64_t)up256((size_t)rows * P.row), left.pieces, left.element};
     if (type == SLZ_F16) slz_unit_of(scale, rows, unit, s);
-    if (rows)
-        hipLaunchKernelGGL(k_values, ew_grid((size_t)rows * P.row / 16), dim3(256), 0, s, q, scale, unit, type, rows, sh->k, ld_q, values, P.row, right.piece);
+    if (rows) {
+        const auto k = type == SLZ_F32 ? k_values<SLZ_F32> : type == SLZ_BF16 ? k_values<SLZ_BF16> : k_values<SLZ_F16>;
+        hipLaunchKernelGGL(k, ew_grid((size_t)rows * P.row / 16), dim3(256), 0, s, q, scale, unit, rows, sh->k, ld_q, values, P.row, right.piece);
+    }
     const slz_gemm p = slz_gemm_of(left, right, M, sh->k, rows);
     const slz_times_unit f{type == SLZ_F16 ? unit : nullptr, 1.0f};
     if (type == SLZ_F16)
