@@ -5,9 +5,9 @@
 // the label's z; a second kernel joins a token's pairs.
 // Gradient: in pieces of the vocabulary, z again, from it g = (exp(z - lse) - [v = label]) dloss to the workspace, then the two products
 // dw = g^T h (complete for the piece's rows) and dh += g w (summed over the pieces in 32 bits).
-// Bound by the matrix cores where rows are long: 4096 tokens x 4096 x 131072 bf16: forward 3.40 ms (1.29 PFLOP/s), each 16384 words' g 496 us (1.11),
-// dw 540 (1.02), dh 514 (1.07).  Short rows leave the epilogues: 1003 x 768 x 50021 f16: forward 108 us (0.71), g 157 (0.49), dw 133, dh 108; tiles of 256 instead of
-// the 128 taken: 105, 163, 163, 106.
+// Bound by the matrix cores where rows are long: 4096 tokens x 4096 x 131072 bf16: forward 3.40 ms (1.29 PFLOP/s), each 16384 words' g 476 us (1.15),
+// dw 540 (1.02), dh 514 (1.07).  Short rows leave the epilogues: 1003 x 768 x 50021 f16: forward 108 us (0.71), g 143 (0.54), dw 133, dh 108; tiles of 256 instead of
+// the 128 taken were no faster for z (105 and, before labels and factors were read ahead, 163 to 160) and slower for dw (163).
 #include "slz_gemm.h"
 
 // a piece's g takes this much at most (at least 1024 words of the vocabulary)
@@ -47,6 +47,12 @@ struct ce_lse_epi {
     template <int MI, int NI, bool RUN, bool WHOLE, class ACC>
     __device__ __forceinline__ void part(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p) const {
         const uint32_t n0 = slz_col<NI, RUN>(at, 0);
+        int words[MI];                                 // read for all rows before the first is written
+#pragma unroll
+        for (int i = 0; i < MI; i++) {
+            const uint32_t m = slz_row(at, i);
+            words[i] = m < p.M && n0 < p.N ? ce_word(labels[m], first_word + n0, min(NI * 4u, p.N - n0)) : -1;
+        }
 #pragma unroll
         for (int i = 0; i < MI; i++) {
             const uint32_t m = slz_row(at, i);
@@ -68,7 +74,7 @@ struct ce_lse_epi {
             sum += __shfl_xor(sum, 16, 64);
             if (NI == 2) sum += __shfl_xor(sum, 32, 64);
             if (m >= p.M || n0 >= p.N) continue;
-            const int word = ce_word(labels[m], first_word + n0, min(NI * 4u, p.N - n0));
+            const int word = words[i];
             if (word >= 0) {
                 float z = 0.0f;
 #pragma unroll
@@ -135,14 +141,24 @@ struct ce_grad_epi {
     __device__ __forceinline__ void part(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p) const {
         const uint32_t n0 = slz_col<NI, RUN>(at, 0), wide = (p.N + 7u) & ~7u;
         const float up = type == SLZ_F16 ? CE_F16_UP / *unit : 1.0f;
+        float bys[MI], ls[MI];                         // read for all rows before the first is written
+        int words[MI];                                 // -2: not counted
+#pragma unroll
+        for (int i = 0; i < MI; i++) {
+            const uint32_t m = min(slz_row(at, i), p.M - 1u);
+            const int64_t label = labels[m];
+            const float d = dloss[m] * up;
+            ls[i] = lse[m];
+            bys[i] = label < 0 || label >= (int64_t)vocab ? __builtin_nanf("") : d;
+            words[i] = label == ignore ? -2 : ce_word(label, first_word + n0, NI * 4);
+        }
 #pragma unroll
         for (int i = 0; i < MI; i++) {
             const uint32_t m = slz_row(at, i);
             if (m >= p.M) continue;
-            const int64_t label = labels[m];
-            const bool counts = label != ignore;
-            const float by = label < 0 || label >= (int64_t)vocab ? __builtin_nanf("") : dloss[m] * up, l = lse[m];
-            const int word = ce_word(label, first_word + n0, NI * 4);
+            const bool counts = words[i] != -2;
+            const float by = bys[i], l = ls[i];
+            const int word = words[i];
 #pragma unroll
             for (int q = 0; q < NI / 2; q++) {
                 const uint32_t n = n0 + q * 8u;
