@@ -86,8 +86,9 @@ k_orth_norm(const void *__restrict__ g, uint32_t rows, uint32_t cols, int64_t ld
     if (threadIdx.x == 0) part[blockIdx.y * ORTH_NORM_BLOCKS + blockIdx.x] = waves[0] + waves[1] + waves[2] + waves[3];
 }
 // 64 x 64 elements per workgroup, through shared memory where the transpose is wanted; factor: what g / (|g| + eps) is of the X written
+template <int TYPE>
 __global__ void __launch_bounds__(256)
-k_orth_load(const void *__restrict__ g, int type, uint32_t rows, uint32_t cols, int64_t ld, int64_t stride, int tall, const double *__restrict__ part,
+k_orth_load(const void *__restrict__ g, uint32_t rows, uint32_t cols, int64_t ld, int64_t stride, int tall, const double *__restrict__ part,
             uint32_t parts, float eps, orth_view x, float *__restrict__ factor) {
     __shared__ float tile[64][65];
     const uint32_t r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, t = threadIdx.x;
@@ -96,7 +97,8 @@ k_orth_load(const void *__restrict__ g, int type, uint32_t rows, uint32_t cols, 
 #pragma unroll
     for (int q = 0; q < 16; q++) {
         const uint32_t i = t + q * 256, r = r0 + i / 64, c = c0 + i % 64;
-        own[q] = r < rows && c < cols ? slz_get(g, type, base + (size_t)r * ld + c) : 0.0f;
+        own[q] = slz_get(g, TYPE, base + (size_t)min(r, rows - 1u) * ld + min(c, cols - 1u));       // all sixteen under way
+        if (r >= rows || c >= cols) own[q] = 0.0f;
     }
     double sum = 0.0;
     for (uint32_t i = t & 63u; i < parts; i += 64) sum += part[blockIdx.z * ORTH_NORM_BLOCKS + i];
@@ -110,7 +112,8 @@ k_orth_load(const void *__restrict__ g, int type, uint32_t rows, uint32_t cols, 
     for (int q = 0; q < 16; q++) tile[(t + q * 256) / 64][t % 64] = ldexpf(own[q], -e) * ORTH_UP;
     __syncthreads();
     const uint32_t m = tall ? cols : rows, wide = ((tall ? rows : cols) + 7u) & ~7u;
-    for (uint32_t i = t; i < 1024; i += 256) {
+#pragma unroll
+    for (uint32_t i = t; i < t + 1024; i += 256) {
         const uint32_t a = i / 16, b = i % 16 * 4, r = (tall ? c0 : r0) + a, c = (tall ? r0 : c0) + b;
         float v[4];
         for (int q = 0; q < 4; q++) v[q] = tall ? tile[b + q][a] : tile[a][b + q];
@@ -804,7 +807,8 @@ extern "C" int slz_orthogonalize(const slz_orth_shape *sh, const void *g, void *
     double *part = (double *)(w + P.part);
     const uint32_t aligned = orth_aligned(sh, out);
     const uint32_t parts = orth_norm(sh, g, part, s);
-    hipLaunchKernelGGL(k_orth_load, dim3((sh->cols + 63) / 64, (sh->rows + 63) / 64, sh->batch), dim3(256), 0, s, g, sh->type, sh->rows, sh->cols, sh->ld_g,
+    const auto load = sh->type == SLZ_F32 ? k_orth_load<SLZ_F32> : sh->type == SLZ_BF16 ? k_orth_load<SLZ_BF16> : k_orth_load<SLZ_F16>;
+    hipLaunchKernelGGL(load, dim3((sh->cols + 63) / 64, (sh->rows + 63) / 64, sh->batch), dim3(256), 0, s, g, sh->rows, sh->cols, sh->ld_g,
                        sh->stride_g, tall, part, parts, sh->eps, x[0], factor);
     if (sh->steps == 0)
         hipLaunchKernelGGL(k_orth_store, dim3(1024, sh->batch), dim3(256), 0, s, x[0], factor, out, sh->type, sh->rows, sh->cols, sh->ld_out, sh->stride_out, tall);
