@@ -5,8 +5,8 @@
 // the label's z; a second kernel joins a token's pairs.
 // Gradient: in pieces of the vocabulary, z again, from it g = (exp(z - lse) - [v = label]) dloss to the workspace, then the two products
 // dw = g^T h (complete for the piece's rows) and dh += g w (summed over the pieces in 32 bits).
-// Bound by the matrix cores where rows are long: 4096 tokens x 4096 x 131072 bf16: forward 3.40 ms (1.29 PFLOP/s), each 16384 words' g 476 us (1.15),
-// dw 540 (1.02), dh 514 (1.07).  Short rows leave the epilogues: 1003 x 768 x 50021 f16: forward 108 us (0.71), g 143 (0.54), dw 133, dh 108; tiles of 256 instead of
+// Bound by the matrix cores where rows are long: 4096 tokens x 4096 x 131072 bf16: forward 3.40 ms (1.29 PFLOP/s), each 16384 words' g 482 us (1.14),
+// dw 546 (1.01), dh 518 (1.06).  Short rows leave the epilogues: 1003 x 768 x 50021 f16: forward 110 us (0.70), g 143 (0.54), dw 135, dh 106; tiles of 256 instead of
 // the 128 taken were no faster for z (105 and, before labels and factors were read ahead, 163 to 160) and slower for dw (163).
 #include "slz_gemm.h"
 
@@ -189,7 +189,7 @@ struct ce_grad_epi {
 // ---- few classes ---------------------------------------------------------------------------------------------------------------------------
 // A classifier's head: w fits a workgroup's shared memory in 32 bits, a wave computes all of a token's z, and the whole call is one launch (the
 // gradient of many tokens: two), where the tiled products would be four to eight.  Taken by the sizes of w alone, so that a token's loss does not
-// depend on how many there are.  32 tokens x 128 x 10: loss 6.1 us, gradient 14.8 in its one workgroup, both less than the host's time for a call.
+// depend on how many there are.  32 tokens x 128 x 10: loss 6.2 us, gradient 14.6 in its one workgroup, both less than the host's time for a call.
 #define FEW_CLASSES 16
 #define FEW_INNER 512                // longer rows leave too few tokens of a workgroup at a time
 #define FEW_WEIGHTS (FEW_CLASSES * FEW_INNER)
