@@ -15,6 +15,7 @@
 // k, may read the next row; they only reach sums that no one stores.
 #pragma once
 #include "slz_clear.h"
+#include "slz_tiling.h"
 #include <type_traits>
 #include <utility>
 
@@ -58,19 +59,11 @@ struct slz_place {
 
 #define SLZ_LDS(p) ((__attribute__((address_space(3))) void *)(p))
 
-// row's bits that move the 16-byte pieces of a tile row of 128 bytes (k contiguous).  spread: the lanes of a read take rows r and
-// (r >> 2) * SPREAD apart instead of consecutive ones
-template <int SPREAD> __device__ __forceinline__ uint32_t slz_swizzle_k(uint32_t row) {
-    if constexpr (SPREAD == 0) return row & 7u;
-    else return (row & 3u) | (((row / SPREAD) & 1u) << 2);
-}
-// and of a tile row of T elements (rows are k), whole 32-byte pairs of pieces
-__device__ __forceinline__ uint32_t slz_swizzle_t(uint32_t row) { return ((row & 3u) | (((row >> 3) & 1u) << 2)) << 1; }
-
 // One operand's share of a wave: which pieces it brings, and how it reads its matrix operands.
 template <bool ROWS_ARE_K, int T, int WAVES, int SPREAD> struct slz_tile {
     static constexpr int BYTES = T * 128, LOADS = BYTES / 1024 / WAVES;
     static_assert(LOADS * WAVES * 1024 == BYTES, "each wave brings whole kilobytes");
+    static_assert(ROWS_ARE_K ? slz_places_t<T>() : slz_places_k<T, SPREAD>(), "every piece has a place, and is read from it");
     uint32_t off[LOADS], piece[LOADS];
     __device__ __forceinline__ void init(uint32_t wave, uint32_t lane, uint32_t ld) {
 #pragma unroll
@@ -78,12 +71,11 @@ template <bool ROWS_ARE_K, int T, int WAVES, int SPREAD> struct slz_tile {
             const uint32_t at = (wave * LOADS + j) * 1024u + lane * 16u;
             if constexpr (!ROWS_ARE_K) {
                 const uint32_t row = at / 128u;
-                piece[j] = ((at / 16u) & 7u) ^ slz_swizzle_k<SPREAD>(row);
+                piece[j] = slz_piece_k<SPREAD>(row, at / 16u & 7u);
                 off[j] = row * ld + piece[j] * 16u;
             } else {
                 const uint32_t row = at / (T * 2u);
-                const uint32_t p = ((at / 16u) & (T / 8u - 1u)) ^ (slz_swizzle_t(row) & (T / 8u - 1u));
-                off[j] = row * ld + p * 16u;
+                off[j] = row * ld + slz_piece_t<T>(row, at / 16u % (T / 8u)) * 16u;
                 piece[j] = 0;
             }
         }
@@ -103,14 +95,14 @@ template <bool ROWS_ARE_K, int T, int WAVES, int SPREAD> struct slz_tile {
         const uint32_t r = lane & 15u, g = lane >> 4;
         if constexpr (!ROWS_ARE_K) {
             const uint32_t row = first + (SPREAD ? (r >> 2) * (COUNT * 4u) + i * 4u + (r & 3u) : i * 16u + r);
-            return *(const v4i32 *)(lds + row * 128u + (((kk * 4u + g) ^ slz_swizzle_k<SPREAD>(row)) << 4));
+            return *(const v4i32 *)(lds + row * 128u + slz_piece_k<SPREAD>(row, kk * 4u + g) * 16u);
         } else {
             v4i32 v;
 #pragma unroll
             for (int h = 0; h < 2; h++) {
                 const uint32_t row = kk * 32u + g * 8u + h * 4u + (r >> 2);
                 const uint32_t at = (first + i * 16u + (r & 3u) * 4u) * 2u;
-                const char *p = lds + row * (T * 2u) + ((((at >> 4) ^ slz_swizzle_t(row)) & (T / 8u - 1u)) << 4) + (at & 15u);
+                const char *p = lds + row * (T * 2u) + slz_piece_t<T>(row, at >> 4) * 16u + (at & 15u);
                 const v4s16 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s16 *)p);
                 const uint64_t b = __builtin_bit_cast(uint64_t, x);
                 v[2 * h] = (int)(uint32_t)b;
@@ -351,33 +343,6 @@ using slz_tiles_192 = slz_tiling<192, 192, 2, 4>;
 using slz_tiles_128 = slz_tiling<128, 128, 2, 2>;
 using slz_tiles_64 = slz_tiling<64, 64, 2, 2>;
 
-// Which tiling and how many ranges of k.  A step of 128 bytes of k takes a compute unit 1.5 us with a tile of 256 a side, 0.95 with one of 192, 0.62
-// with one of 128 and 0.88 with two at once, 0.33 with one of 64 and 0.18 for each of several (measured at 4096 deep: 3840^2 with 256: 99 us;
-// 2688^2 with 192: 63, with 128: 57; 768^2 with 256, 192, 128: 85, 58, 43).  Large tiles read less for each product, small ones fill the chip with less
-// and leave less of it idle at the end.  Ranges of k cost a second launch that reads their sums.
-struct slz_choice { uint32_t side, split; double us; uint32_t pieces = 1; };     // pieces: of a number that are loaded together
-static inline double slz_step_us(uint32_t side, double tiles, uint32_t pieces) {
-    const auto rounds = [&](double at_once) { return (double)(uint64_t)((tiles + at_once - 1) / at_once); };
-    if (pieces == 2) return side == 128 ? rounds(256) * 1.9 : rounds(256) * 0.42 > 0.5 ? rounds(256) * 0.42 : 0.5;
-    if (side == 256) return rounds(256) * 1.5;
-    if (side == 192) return rounds(256) * 0.95;
-    if (side == 64) return rounds(256) * 0.18 > 0.33 ? rounds(256) * 0.18 : 0.33;
-    const double pairs = (double)(uint64_t)(tiles / 512), rest = tiles - pairs * 512;
-    return pairs * 0.88 + (rest > 256 ? 0.88 : rest > 0 ? 0.62 : 0.0);
-}
-static inline slz_choice slz_choose(uint32_t M, uint32_t N, uint32_t steps, uint32_t batches, bool symmetric, uint32_t most_ranges, bool any_side = true, uint32_t pieces = 1) {
-    slz_choice best = {64, 1, 1e30};
-    for (const uint32_t side : {256u, 192u, 128u, 64u}) {
-        if ((side == 192 && !any_side) || (side == 256 && symmetric) || (side > 128 && pieces == 2)) continue;
-        const double tm = (M + side - 1) / side, tn = (N + side - 1) / side, tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batches;
-        for (uint32_t split = 1; split <= most_ranges && (split == 1 || steps >= 4 * split); split *= 2) {
-            double us = ((steps + split - 1) / split) * slz_step_us(side, tiles * split, pieces);
-            if (split > 1) us += 4.0 + (double)M * N * batches * 4.0 * (split + 1) / 3e6;
-            if (us < best.us) best = {side, split, us, pieces};
-        }
-    }
-    return best;
-}
 // workspace of the ranges' sums
 static inline uint32_t slz_ranges_ld(uint32_t N) { return (N + 15u) & ~15u; }
 static inline size_t slz_ranges_bytes(const slz_choice &c, uint32_t M, uint32_t N) { return c.split > 1 ? up256((size_t)c.split * M * slz_ranges_ld(N) * 4) : 0; }

@@ -461,8 +461,8 @@ static grad_plan plan_grad(const slz_i8_shape *sh, const void *dy) {
     P.unit = P.values[1] + pieces * up256((size_t)sh->n * P.row);
     P.ranges = P.unit + 256;
     const uint32_t pairs = sh->type == SLZ_F32 ? 6 : 1;
-    P.da = slz_choose(sh->m, sh->k, (sh->n + 63) / 64 * pairs, 1, false, 16);
-    P.db = slz_choose(sh->n, sh->k, (sh->m + 63) / 64 * pairs, 1, false, 16);
+    P.da = slz_choose(sh->m, sh->k, (sh->n + 63) / 64 * pairs, 1, false, 16, true);
+    P.db = slz_choose(sh->n, sh->k, (sh->m + 63) / 64 * pairs, 1, false, 16, true);
     const size_t for_a = slz_ranges_bytes(P.da, sh->m, sh->k), for_b = slz_ranges_bytes(P.db, sh->n, sh->k);
     P.total = P.ranges + (for_a > for_b ? for_a : for_b);
     return P;

@@ -401,7 +401,7 @@ static ce_plan plan_ce(const slz_ce_shape *sh, const void *h, const void *w, boo
     }
     P.words = (uint32_t)(words < sh->vocab ? words : sh->vocab);
     const uint32_t pairs = sh->type == SLZ_F32 ? 6 : 1;
-    P.side = slz_choose(sh->tokens, P.words, (sh->inner + 63) / 64 * pairs, 1, false, 1, false).side;
+    P.side = slz_choose(sh->tokens, P.words, (sh->inner + 63) / 64 * pairs, 1, false, 1, false, false).side;
     size_t o = 0;
     P.h = o; o += slz_operand_bytes(h, sh->type, sh->tokens, sh->inner, sh->ld_h);
     P.w = o; o += slz_operand_bytes(w, sh->type, P.words, sh->inner, sh->ld_w);
@@ -413,8 +413,8 @@ static ce_plan plan_ce(const slz_ce_shape *sh, const void *h, const void *w, boo
         P.g = o; o += pieces * up256((size_t)sh->tokens * P.g_row);
         P.dh_ld = slz_ranges_ld(sh->inner);
         // dh: one launch over a piece, or its sums kept in ranges of the piece's words, to which each piece adds
-        P.dh_choice = slz_choose(sh->tokens, sh->inner, (P.words + 63) / 64 * pairs, 1, false, 64);
-        P.dw_choice = slz_choose(P.words, sh->inner, (sh->tokens + 63) / 64 * pairs, 1, false, 32);
+        P.dh_choice = slz_choose(sh->tokens, sh->inner, (P.words + 63) / 64 * pairs, 1, false, 64, true);
+        P.dw_choice = slz_choose(P.words, sh->inner, (sh->tokens + 63) / 64 * pairs, 1, false, 32, true);
         P.dw = o; o += slz_ranges_bytes(P.dw_choice, P.words, sh->inner);
         P.dh = o; o += P.words < sh->vocab || P.dh_choice.split > 1 ? up256((size_t)P.dh_choice.split * sh->tokens * P.dh_ld * 4) : 0;
         P.unit = o; o += 256;

@@ -643,9 +643,10 @@ static void small_slices(orth_plan &P) {
 }
 // Two pieces: three products one after the other in any tiling, or tiles of 128 or 64 that load both pieces at once.  These read a third less, but large
 // tiles read less still: f32, 6 x 500 x 1000 277 us together and 345 in turn, 1024^2 279 and 431, 4096 x 8192 9532 and 6889
-static slz_choice orth_choose(const orth_plan &P, uint32_t N, uint32_t steps, uint32_t batch, bool symmetric, uint32_t most_ranges) {
-    if (P.pieces == 1) return slz_choose(P.m, N, steps, batch, symmetric, most_ranges);
-    const slz_choice in_turn = slz_choose(P.m, N, steps * 3, batch, symmetric, most_ranges), together = slz_choose(P.m, N, steps, batch, symmetric, most_ranges, true, 2);
+static slz_choice orth_choose(const orth_plan &P, uint32_t N, uint32_t steps, uint32_t batch, bool symmetric, uint32_t most_ranges, bool rows_k) {
+    if (P.pieces == 1) return slz_choose(P.m, N, steps, batch, symmetric, most_ranges, rows_k);
+    const slz_choice in_turn = slz_choose(P.m, N, steps * 3, batch, symmetric, most_ranges, rows_k);
+    const slz_choice together = slz_choose(P.m, N, steps, batch, symmetric, most_ranges, rows_k, true, 2);
     return together.us < in_turn.us ? together : in_turn;
 }
 static orth_plan plan_orth(const slz_orth_shape *sh) {
@@ -680,13 +681,13 @@ static orth_plan plan_orth(const slz_orth_shape *sh) {
     P.factor = o; o += up256((size_t)sh->batch * 4);
     P.part = o; o += up256((size_t)sh->batch * ORTH_NORM_BLOCKS * 8);
     const uint32_t steps = (P.n + 63) / 64;
-    P.gram = orth_choose(P, P.m, steps, sh->batch, true, 1);
-    const slz_choice cut = orth_choose(P, P.m, steps, sh->batch, false, 32);
+    P.gram = orth_choose(P, P.m, steps, sh->batch, true, 1, false);
+    const slz_choice cut = orth_choose(P, P.m, steps, sh->batch, false, 32, false);
     if (cut.us < P.gram.us && P.m <= 65535) P.gram = cut;
     P.ranges = o; o += P.gram.split > 1 ? up256((size_t)P.gram.split * sh->batch * P.m * slz_ranges_ld(P.m) * 4) : 0;
     P.total = o;
-    P.polynomial = orth_choose(P, P.m, (P.m + 63) / 64, sh->batch, true, 1);
-    P.apply = orth_choose(P, P.n, (P.m + 63) / 64, sh->batch, false, 1);
+    P.polynomial = orth_choose(P, P.m, (P.m + 63) / 64, sh->batch, true, 1, false);
+    P.apply = orth_choose(P, P.n, (P.m + 63) / 64, sh->batch, false, 1, true);
     return P;
 }
 static int orth_check(const slz_orth_shape *sh) {
