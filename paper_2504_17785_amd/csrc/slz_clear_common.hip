@@ -83,10 +83,15 @@ slz_operand slz_operand_i8_of(const int8_t *p, uint32_t rows, uint32_t cols, int
 }
 
 // One workgroup: the power of two above the largest of the finite magnitudes (1 where there is none)
-__global__ void __launch_bounds__(256) k_scale_unit(const float *__restrict__ scale, uint32_t count, float *__restrict__ unit) {
+__global__ void __launch_bounds__(256)
+k_scale_unit(const float *__restrict__ scale, uint32_t count, float *__restrict__ unit, const int64_t *__restrict__ labels, int64_t ignore, uint32_t classes) {
     float top = 0.0f;
     for (uint32_t i = threadIdx.x; i < count; i += 256) {
         const float a = fabsf(scale[i]);
+        if (labels) {
+            const int64_t label = labels[i];
+            if (label == ignore || (uint64_t)label >= classes) continue;
+        }
         if (a < __builtin_inff()) top = fmaxf(top, a);
     }
     top = slz_wave_max(top);
@@ -101,6 +106,6 @@ __global__ void __launch_bounds__(256) k_scale_unit(const float *__restrict__ sc
     }
 }
 
-void slz_unit_of(const float *values, uint32_t count, float *unit, hipStream_t s) {
-    hipLaunchKernelGGL(k_scale_unit, dim3(1), dim3(256), 0, s, values, count, unit);
+void slz_unit_of(const float *values, uint32_t count, float *unit, hipStream_t s, const int64_t *labels, int64_t ignore, uint32_t classes) {
+    hipLaunchKernelGGL(k_scale_unit, dim3(1), dim3(256), 0, s, values, count, unit, labels, ignore, classes);
 }

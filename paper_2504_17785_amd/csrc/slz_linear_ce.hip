@@ -507,7 +507,7 @@ extern "C" int slz_linear_ce_grad(const slz_ce_shape *sh, const void *h, const v
     hipStream_t s = (hipStream_t)stream;
     char *base = (char *)ws;
     float *dh_sum = (float *)(base + P.dh), *unit = (float *)(base + P.unit);
-    if (sh->type == SLZ_F16) slz_unit_of(dloss, sh->tokens, unit, s);
+    if (sh->type == SLZ_F16) slz_unit_of(dloss, sh->tokens, unit, s, labels, sh->ignore_index, sh->vocab);
     const slz_times_unit f{sh->type == SLZ_F16 ? unit : nullptr, 1.0f / CE_F16_UP};
     slz_layouts jobs = {};
     const slz_operand oh = slz_operand_of(h, sh->type, sh->tokens, sh->inner, sh->ld_h, base + P.h, jobs);
