@@ -5,7 +5,7 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
-from tests.test_gpu_clear import IGNORED, TYPES, ce_inputs, slz  # noqa: E402,F401
+from tests.test_gpu_clear import IGNORED, LEAST, TYPES, U, WIDE, ce_inputs, inside, int8, slz  # noqa: E402,F401
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -26,3 +26,18 @@ def test_dloss_of_tokens_that_do_not_count_changes_nothing(slz, dtype, inner, vo
     dh, _ = slz.linear_ce_grad(h, w, labels, lse, dloss)
     rest = [t for t in range(40) if t != 7]
     assert torch.isnan(dh[7]).all() and torch.equal(dh[rest], want[0][rest])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradients_of_rows_with_small_scales(slz, dtype):  # noqa: F811
+    # one term a sum, so that each value of scale x integer shows by itself; scales from 1 down to 2^-21
+    n, k = 64, 96
+    a, b = int8((n, k), 1), int8((n, k), 2)
+    s = 1.37 * 2.0 ** (-torch.arange(n, device="cuda") / 3)
+    dy = torch.zeros(n, n, device="cuda", dtype=dtype)
+    dy.fill_diagonal_(200.0)
+    want_a, want_b = 200 * b.to(WIDE) * s.to(WIDE)[:, None], 200 * a.to(WIDE) * s.to(WIDE)[:, None]
+    for got, want in zip(slz.matmul_i8_grad(dy, a, s, b, s), (want_a, want_b)):
+        # the value to the type (f32: 24 bits), the products in 32 bits, the result to the type
+        value = U[dtype] if dtype != torch.float32 else 2.0 ** -21
+        inside(got, want, want.abs() * 1.01 * (value + U[dtype] + 8 * 2.0 ** -24) + LEAST[dtype], "gradient")
