@@ -105,7 +105,9 @@ typedef struct {
 
 /* Each matrix: X = g / (|g| + eps), |g| the root of the sum of squares, then `steps` times  A = X X^T,  X <- a X + (b A + c A A) X
  * (for more rows than columns the same of the transpose).  Products of 11-bit numbers, summed in 32 bits, the diagonals of A and
- * of b A + c A A apart from them in 32 bits and X in 22; for f16 and f32 every operand has 22 bits.
+ * of b A + c A A apart from them in 32 bits; for f16 and f32 products of 22-bit numbers.  Between the steps X has 22 bits, or 2^-35 where that is more.
+ * It is held in a format that reaches 63, and A and b A + c A A, off their diagonals, in one that reaches 1023: coefficients and numbers of steps that lead
+ * beyond make the matrix infinite or NaN.
  * out may not overlap g. */
 int slz_orthogonalize_workspace(const slz_orth_shape *shape, size_t *bytes);
 int slz_orthogonalize(const slz_orth_shape *shape, const void *g_dev, void *out_dev, void *workspace_dev, size_t workspace_bytes,

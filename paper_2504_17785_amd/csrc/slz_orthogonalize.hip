@@ -13,7 +13,12 @@
 // other tiling is more than 6 % faster: launches of 8 or 16 steps of k, mostly fill and epilogue.
 #include "slz_gemm.h"
 
-#define ORTH_UP 64.0f                // operands are held times this: the second halves stay out of the subnormal numbers
+// A and B are held times ORTH_UP: what is lost of them below 2^-31 is nothing against a I, to which they are added.  X is held times ORTH_X_UP, since its
+// small entries grow by a each step: relative to a norm of 1 they are 1 / sqrt(mn), and their second halves have to stay out of f16's subnormal numbers.
+// f32, 4096 x 8192, error against 64 bits: 1.1e-6 (Gaussian), 1.4e-5 (four strong directions), with 64 in place of 1024 3.1e-6 and 1.4e-4, 4096 no better;
+// the same steps in 32 bits 7.1e-6 and 3.5e-5.  Entries of X up to 63 and, off the diagonal, of A and B up to 1023 stay finite.
+#define ORTH_UP 64.0f
+#define ORTH_X_UP 1024.0f
 #define ORTH_NORM_BLOCKS 1024
 
 struct orth_view {                   // a batch of matrices of two f16 each; rows of a multiple of 64 elements
@@ -23,7 +28,7 @@ struct orth_view {                   // a batch of matrices of two f16 each; row
 };
 typedef _Float16 orth_h2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t orth_pack(_Float16 a, _Float16 b) { return __builtin_bit_cast(uint32_t, orth_h2{a, b}); }
-// Values as they are held, ORTH_UP times the number: u to its two halves and back
+// Values as they are held, ORTH_UP or ORTH_X_UP times the number: u to its two halves and back
 __device__ __forceinline__ void orth_halves(float u, _Float16 &hi, _Float16 &lo) {
     hi = (_Float16)u;
     lo = (_Float16)(u - (float)hi);
@@ -48,7 +53,14 @@ __device__ __forceinline__ void orth_get4(const orth_view &v, size_t at, float (
 }
 __device__ __forceinline__ float orth_get(const orth_view &v, size_t at) {
     const float h = slz_f16_to_f32(v.hi[at]);
-    return (v.lo ? h + slz_f16_to_f32(v.lo[at]) : h) * (1.0f / ORTH_UP);
+    return (v.lo ? h + slz_f16_to_f32(v.lo[at]) : h) * (1.0f / ORTH_X_UP);
+}
+
+// The first X is g 2^-e; with 2^e the power of two at or below the norm (1 for a norm of 0 or none) what is missing to g / norm is a factor above 1/2, at most 1
+__device__ __forceinline__ int orth_exponent(double norm) {
+    int e = 1;
+    if (norm > 0.0 && norm < 1e300) frexp(norm, &e);
+    return e - 1;
 }
 
 // ---- norm and first X -------------------------------------------------------------------------------------------------------------------
@@ -105,11 +117,10 @@ k_orth_load(const void *__restrict__ g, uint32_t rows, uint32_t cols, int64_t ld
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
     const double norm = sqrt(sum) + (double)eps;
-    int e = 0;
-    if (norm > 0.0 && norm < 1e300) frexp(norm, &e);
+    const int e = orth_exponent(norm);
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) factor[blockIdx.z] = (float)(ldexp(1.0, e) / norm);
 #pragma unroll
-    for (int q = 0; q < 16; q++) tile[(t + q * 256) / 64][t % 64] = ldexpf(own[q], -e) * ORTH_UP;
+    for (int q = 0; q < 16; q++) tile[(t + q * 256) / 64][t % 64] = ldexpf(own[q], -e) * ORTH_X_UP;
     __syncthreads();
     const uint32_t m = tall ? cols : rows, wide = ((tall ? rows : cols) + 7u) & ~7u;
 #pragma unroll
@@ -204,7 +215,7 @@ template <class F> struct orth_symmetric_epi {
 struct orth_gram {
     const float *factor;             // or null
     __device__ __forceinline__ void operator()(uint32_t batch, uint32_t, uint32_t, const v4f &sum, float (&u)[4]) const {
-        const float f = factor ? factor[batch] : 1.0f, by = f * f / ORTH_UP;
+        const float f = factor ? factor[batch] : 1.0f, by = f * f * (ORTH_UP / ORTH_X_UP / ORTH_X_UP);
 #pragma unroll
         for (int c = 0; c < 4; c++) u[c] = sum[c] * by;
     }
@@ -285,7 +296,7 @@ struct orth_apply_epi {
                 if (!out) orth_put4(next, at.batch * x.stride + (size_t)m * x.ld + n, v);
                 else if (n < p.N) {
 #pragma unroll
-                    for (int c = 0; c < 4; c++) v[c] *= 1.0f / ORTH_UP;
+                    for (int c = 0; c < 4; c++) v[c] *= 1.0f / ORTH_X_UP;
                     const int64_t first = at.batch * stride_out;
                     if (!tall) slz_put_run<4>((char *)out + (first + (int64_t)m * ld_out + n) * slz_type_bytes(type), type, v, p.N - n, aligned);
                     else
@@ -414,14 +425,13 @@ __global__ void __launch_bounds__(small_shape<MP>::WAVES * 64) k_orth_small(cons
         sum = 0.0;
         for (int w = 0; w < S::WAVES; w++) sum += wave_sums[w];
         const double norm = sqrt(sum) + (double)p.eps;
-        int e = 0;
-        if (norm > 0.0 && norm < 1e300) frexp(norm, &e);
+        const int e = orth_exponent(norm);
         factor = (float)(ldexp(1.0, e) / norm);
         if (KIND == SMALL_FIRST && blockIdx.x == 0 && threadIdx.x == 0) p.factor[batch] = factor;
         small_elements<THREADS>(p, batch, c0, width, [&](uint32_t row, uint32_t col, const float (&v)[8]) {
             _Float16 hi[8], lo[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) orth_halves(ldexpf(v[i], -e) * ORTH_UP, hi[i], lo[i]);
+            for (int i = 0; i < 8; i++) orth_halves(ldexpf(v[i], -e) * ORTH_X_UP, hi[i], lo[i]);
             if (!p.tall) {
                 const uint32_t to = row * pitch + col * 2u;
                 *(uint4 *)(x_at[0] + to) = make_uint4(orth_pack(hi[0], hi[1]), orth_pack(hi[2], hi[3]), orth_pack(hi[4], hi[5]), orth_pack(hi[6], hi[7]));
@@ -512,7 +522,7 @@ __global__ void __launch_bounds__(small_shape<MP>::WAVES * 64) k_orth_small(cons
     const uint32_t steps = KIND == SMALL_ALL ? p.steps : KIND == SMALL_FIRST ? 0u : 1u;
     for (uint32_t step = 0; step < steps; step++) {
         float u[GM][GN][4];
-        const float by = factor * factor / ORTH_UP;
+        const float by = factor * factor * (ORTH_UP / ORTH_X_UP / ORTH_X_UP);
 #pragma unroll
         for (int i = 0; i < GM; i++)
 #pragma unroll
@@ -582,7 +592,7 @@ __global__ void __launch_bounds__(small_shape<MP>::WAVES * 64) k_orth_small(cons
                 else if (m < p.m && n < width) {
                     const size_t first = (size_t)batch * p.stride_out;
 #pragma unroll
-                    for (int c = 0; c < 4; c++) x[c] *= 1.0f / ORTH_UP;
+                    for (int c = 0; c < 4; c++) x[c] *= 1.0f / ORTH_X_UP;
                     if (!p.tall)
                         slz_put_run<4>((char *)p.out + (first + (size_t)m * p.ld_out + c0 + n) * slz_type_bytes(p.type), p.type, x, width - n, p.aligned);
                     else

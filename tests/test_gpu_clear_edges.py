@@ -5,7 +5,7 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
-from tests.test_gpu_clear import IGNORED, LEAST, TYPES, U, WIDE, ce_inputs, inside, int8, slz  # noqa: E402,F401
+from tests.test_gpu_clear import COEFFICIENTS, IGNORED, LEAST, TYPES, U, WIDE, ce_inputs, inside, int8, orthogonalised, randn, slz  # noqa: E402,F401
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -41,3 +41,34 @@ def test_gradients_of_rows_with_small_scales(slz, dtype):  # noqa: F811
         # the value to the type (f32: 24 bits), the products in 32 bits, the result to the type
         value = U[dtype] if dtype != torch.float32 else 2.0 ** -21
         inside(got, want, want.abs() * 1.01 * (value + U[dtype] + 8 * 2.0 ** -24) + LEAST[dtype], "gradient")
+
+
+def updates(rows, cols):
+    """Gradients with entries far apart: a few strong directions, every other row a thousandth of the rest."""
+    g = randn((rows, cols), rows + cols)
+    yield g + 30 * randn((rows, 4), 1) @ randn((4, cols), 2)
+    g[::2] *= 1e-3
+    yield g
+
+
+@pytest.mark.parametrize("rows,cols", [(64, 512), (128, 8000), (8000, 128), (200, 300), (2000, 2100), (2100, 2000)])
+def test_updates_keep_small_entries(slz, rows, cols):  # noqa: F811
+    # coefficients (1, 0, 0) only hold X: 22 bits or 2^-35 each time, and some roundings in 32 bits
+    for g in updates(rows, cols):
+        want = orthogonalised(g, steps=0)
+        for steps in (0, 1, 3):
+            got = slz.orthogonalize(g, steps=steps, coefficients=(1.0, 0.0, 0.0))
+            inside(got, want, max(steps, 1) * (want.abs() * (2.0 ** -22 + 4 * 2.0 ** -24) + 2.0 ** -35), "%d steps" % steps)
+
+
+@pytest.mark.parametrize("rows,cols", [(128, 8000), (300, 3000)])
+def test_updates_are_as_good_as_in_32_bits(slz, rows, cols):  # noqa: F811
+    a, b, c = COEFFICIENTS
+    for g in updates(rows, cols):
+        want = orthogonalised(g)
+        x = g / g.norm()
+        for _ in range(5):
+            s = x @ x.t().contiguous()
+            x = a * x + (b * s + c * (s @ s)) @ x
+        # numbers of 22 bits in place of 24
+        assert (slz.orthogonalize(g).to(WIDE) - want).norm() <= 4 * (x.to(WIDE) - want).norm()
