@@ -23,6 +23,9 @@ static inline bool slz_in_place(const void *p, uint32_t cols, int64_t ld, uint32
     return !(((uintptr_t)p | ((uint64_t)cols * bytes) | ((uint64_t)ld * bytes)) & 15u);
 }
 
+// threads of a launch along x stay below 2^32
+static inline uint32_t slz_most_blocks(uint32_t threads) { return 0xffffffffu / threads; }
+
 static inline bool slz_ws_ok(const void *ws, size_t have, size_t need) { return need == 0 || (ws && have >= need && !((uintptr_t)ws & 255u)); }
 
 #ifdef __HIPCC__

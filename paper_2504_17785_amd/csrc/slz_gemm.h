@@ -46,6 +46,7 @@ struct slz_gemm {
     uint32_t split;                  // ranges of steps, each by workgroups of its own
     uint32_t range;                  // steps of a range
     uint32_t tiles_m, tiles_n;
+    uint32_t first_tile;             // of this launch
     uint32_t symmetric;              // only tiles on and below the diagonal
 };
 
@@ -115,12 +116,12 @@ template <bool ROWS_ARE_K, int T, int WAVES, int SPREAD> struct slz_tile {
 
 // Tile, range of k and matrix of a workgroup.  The eight XCDs take workgroups in turn and each has an L2 of its own, so each gets a run of consecutive
 // tiles, all of a range and of a matrix before the next; within the order, four tile rows go along the columns together.
-__device__ __forceinline__ void slz_tile_of(uint32_t tiles_m, uint32_t tiles_n, uint32_t symmetric, uint32_t &tm, uint32_t &tn, uint32_t &range, uint32_t &batch) {
+__device__ __forceinline__ void slz_tile_of(uint32_t tiles_m, uint32_t tiles_n, uint32_t first_tile, uint32_t symmetric, uint32_t &tm, uint32_t &tn, uint32_t &range, uint32_t &batch) {
     uint32_t x = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z);
     const uint32_t total = gridDim.x * gridDim.y * gridDim.z, even = total & ~7u;
     if (x < even) x = (x & 7u) * (even >> 3) + (x >> 3);
     const uint32_t which = x / gridDim.x;
-    x -= which * gridDim.x;
+    x += first_tile - which * gridDim.x;
     batch = which / gridDim.y;
     range = which - batch * gridDim.y;
     if (symmetric) {                                   // row tm has tm + 1 tiles
@@ -160,7 +161,7 @@ __global__ void __launch_bounds__(WM *WN * 64) k_gemm(const slz_gemm p, const EP
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wave_m = wave / WN, wave_n = wave % WN;
     uint32_t tm, tn, range, batch;
-    slz_tile_of(p.tiles_m, p.tiles_n, p.symmetric, tm, tn, range, batch);
+    slz_tile_of(p.tiles_m, p.tiles_n, p.first_tile, p.symmetric, tm, tn, range, batch);
     const uint32_t steps_k = (p.K + KS - 1) / KS, steps = steps_k * p.pairs;
     const uint32_t begin = range * p.range, end = min(steps, begin + p.range);
 
@@ -374,8 +375,12 @@ static int slz_gemm_launch(slz_gemm p, const EPI &epi, uint32_t batches, hipStre
     const uint64_t tiles = p.symmetric ? (uint64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (uint64_t)p.tiles_m * p.tiles_n;
     if (tiles == 0 || batches == 0) return SLZ_OK;
     if (tiles * p.split * batches > 0x7fffffffu) return SLZ_E_TOO_LARGE;
-    hipLaunchKernelGGL((k_gemm<EL, A_ROWS_K, B_ROWS_K, T::TM, T::TN, T::WM, T::WN, PIECES, EPI>), dim3((uint32_t)tiles, p.split, batches),
-                       dim3(T::WM * T::WN * 64), 0, s, p, epi);
+    constexpr uint32_t threads = T::WM * T::WN * 64;
+    for (p.first_tile = 0; p.first_tile < tiles; p.first_tile += slz_most_blocks(threads)) {
+        const uint32_t left = (uint32_t)tiles - p.first_tile, most = slz_most_blocks(threads);
+        hipLaunchKernelGGL((k_gemm<EL, A_ROWS_K, B_ROWS_K, T::TM, T::TN, T::WM, T::WN, PIECES, EPI>), dim3(left < most ? left : most, p.split, batches),
+                           dim3(threads), 0, s, p, epi);
+    }
     return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
 }
 // operands of two pieces (a_piece[1] and b_piece[1]: the second ones), tiles of 128 or 64

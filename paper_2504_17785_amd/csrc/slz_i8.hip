@@ -75,7 +75,10 @@ k_quantize(const void *__restrict__ x, uint32_t cols, int64_t ld_x, int8_t *__re
 static int quantize_rows(const void *x, int type, uint32_t rows, uint32_t cols, int64_t ld_x, int8_t *q, int64_t ld_q, float *scale, hipStream_t s) {
     const uint32_t words = !(((uintptr_t)q | (uint64_t)ld_q) & 7u);               // rows of q begin at multiples of eight
     const auto k = type == SLZ_F32 ? k_quantize<SLZ_F32> : type == SLZ_BF16 ? k_quantize<SLZ_BF16> : k_quantize<SLZ_F16>;
-    hipLaunchKernelGGL(k, dim3(rows), dim3(256), 0, s, x, cols, ld_x, q, ld_q, words, scale);
+    for (uint32_t first = 0, most = slz_most_blocks(256); first < rows; first += most) {
+        const void *from = (const char *)x + (int64_t)first * ld_x * slz_type_bytes(type);
+        hipLaunchKernelGGL(k, dim3(rows - first < most ? rows - first : most), dim3(256), 0, s, from, cols, ld_x, q + (int64_t)first * ld_q, ld_q, words, scale + first);
+    }
     return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
 }
 

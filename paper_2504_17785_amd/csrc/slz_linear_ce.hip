@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(1024)
 k_ce_join(const float2 *__restrict__ pairs, const float *__restrict__ label_z, const int64_t *__restrict__ labels, float *__restrict__ loss,
           float *__restrict__ lse, uint32_t tokens, uint32_t blocks, uint32_t vocab, int64_t ignore) {
     __shared__ float2 part[64][16];
-    const uint32_t r = threadIdx.x & 15u, slice = threadIdx.x >> 4, t = blockIdx.x * 16 + r;
+    const uint32_t r = threadIdx.x & 15u, slice = threadIdx.x >> 4, t = (blockIdx.y * gridDim.x + blockIdx.x) * 16 + r;
     float2 all = make_float2(-__builtin_inff(), 0.0f);
     if (t < tokens)
         for (uint32_t i = slice; i < blocks; i += 64 * 8) {
@@ -473,7 +473,8 @@ extern "C" int slz_linear_ce(const slz_ce_shape *sh, const void *h, const void *
         rc = ce_logits(sh->type, slz_gemm_of(oh, ow, sh->tokens, words, sh->inner), epi, P.side, s);
         if (rc != SLZ_OK) return rc;
     }
-    hipLaunchKernelGGL(k_ce_join, dim3((sh->tokens + 15) / 16), dim3(1024), 0, s, pairs, label_z, labels, loss, lse, sh->tokens, (sh->vocab + CE_BLOCK - 1) / CE_BLOCK,
+    const uint32_t joins = (sh->tokens + 15) / 16, most = slz_most_blocks(1024), along = joins < most ? joins : most;
+    hipLaunchKernelGGL(k_ce_join, dim3(along, (joins + along - 1) / along), dim3(1024), 0, s, pairs, label_z, labels, loss, lse, sh->tokens, (sh->vocab + CE_BLOCK - 1) / CE_BLOCK,
                        sh->vocab, sh->ignore_index);
     SLZ_HIP(hipGetLastError());
     return SLZ_OK;

@@ -1,11 +1,12 @@
 """Edges of the operators of include/silenzio_clear.h: values that must have no influence, numbers far apart, lengths beyond a launch's."""
+import numpy as np
 import pytest
 
 pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
-from tests.test_gpu_clear import COEFFICIENTS, IGNORED, LEAST, TYPES, U, WIDE, ce_inputs, inside, int8, orthogonalised, randn, slz  # noqa: E402,F401
+from tests.test_gpu_clear import COEFFICIENTS, IGNORED, LEAST, TYPES, U, WIDE, ce_inputs, inside, int8, orthogonalised, quantised, randn, scales, slz  # noqa: E402,F401
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -72,3 +73,42 @@ def test_updates_are_as_good_as_in_32_bits(slz, rows, cols):  # noqa: F811
             x = a * x + (b * s + c * (s @ s)) @ x
         # numbers of 22 bits in place of 24
         assert (slz.orthogonalize(g).to(WIDE) - want).norm() <= 4 * (x.to(WIDE) - want).norm()
+
+
+def test_quantize_of_more_rows_than_a_launch_takes(slz):  # noqa: F811
+    # a workgroup of 256 a row: 2^24 rows are 2^32 threads
+    rows = 2 ** 24 + 3
+    x = randn((rows, 1), 1, torch.bfloat16)
+    q, scale = slz.quantize_i8(x)
+    want_q, want_scale = quantised(x)
+    assert np.array_equal(q.cpu().numpy(), want_q) and np.array_equal(scale.cpu().numpy(), want_scale)
+    x = randn((rows, 16), 2, torch.bfloat16)
+    w, sw = int8((3, 16), 3), scales(3, 4)
+    y = slz.linear_i8(x, w, sw)
+    for part in (slice(0, 1000), slice(2 ** 24 - 1000, rows)):
+        assert torch.equal(y[part], slz.linear_i8(x[part].contiguous(), w, sw))
+
+
+def test_product_of_more_tiles_than_a_launch_takes(slz):  # noqa: F811
+    # tiles of 64 rows, workgroups of 256: 2^30 rows are 2^32 threads
+    m, k = 2 ** 30 + 65, 16
+    a = torch.randint(-128, 128, (m, k), device="cuda", dtype=torch.int8)
+    b, sa, sb = int8((1, k), 2), torch.ones(m, device="cuda"), torch.ones(1, device="cuda")
+    y = slz.matmul_i8(a, sa, b, sb, torch.float32)
+    for first in range(0, m, 2 ** 25):
+        part = slice(first, min(m, first + 2 ** 25))
+        assert torch.equal(y[part, 0], (a[part].float() * b.float()).sum(1))          # whole numbers below 2^24
+
+
+def test_loss_of_more_tokens_than_a_launch_takes(slz):  # noqa: F811
+    # the join has 1024 threads for 16 tokens: 2^26 tokens are 2^32
+    tokens, inner, vocab = 2 ** 26 + 21, 8, 17
+    h, w = randn((tokens, inner), 1, torch.bfloat16), randn((vocab, inner), 2, torch.bfloat16)
+    labels = torch.randint(0, vocab, (tokens,), device="cuda")
+    loss, lse = slz.linear_ce(h, w, labels)
+    for first in (0, 2 ** 25 + 5, 2 ** 26 - 2 ** 20):
+        part = slice(first, min(tokens, first + 2 ** 21))
+        one, two = slz.linear_ce(h[part].contiguous(), w, labels[part].contiguous())
+        assert torch.equal(one, loss[part]) and torch.equal(two, lse[part])
+        want = torch.logsumexp(h[part].to(WIDE) @ w.to(WIDE).t().contiguous(), 1)
+        inside(lse[part], want, 2.0 ** -17, "lse")     # z of some ten, eight terms in 32 bits
