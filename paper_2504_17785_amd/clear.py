@@ -11,6 +11,7 @@ import functools
 import torch
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_E_TOO_LARGE = -5
 
 
 class SlzI8Shape(ctypes.Structure):
@@ -81,6 +82,8 @@ def _matrix(t, what: str, types, like=None, rows=None, cols=None, dims: int = 2)
     shape, stride = t.shape, t.stride()
     if (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
         raise ValueError("%s: shape %s, need (%s, %s)" % (what, tuple(shape), rows, cols))
+    if max(shape) > 0x7fffffff:                        # the library takes 32 bits of a length, and refuses what it sees of longer ones
+        _check(_E_TOO_LARGE, "%s: shape %s" % (what, tuple(shape)))
     if like is not None and t.get_device() != like.get_device():
         raise ValueError("%s: on device %d, others on %d" % (what, t.get_device(), like.get_device()))
     c, r = shape[-1], shape[-2]

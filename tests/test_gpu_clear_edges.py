@@ -112,3 +112,15 @@ def test_loss_of_more_tokens_than_a_launch_takes(slz):  # noqa: F811
         assert torch.equal(one, loss[part]) and torch.equal(two, lse[part])
         want = torch.logsumexp(h[part].to(WIDE) @ w.to(WIDE).t().contiguous(), 1)
         inside(lse[part], want, 2.0 ** -17, "lse")     # z of some ten, eight terms in 32 bits
+
+
+def test_the_binding_refuses_lengths_beyond_32_bits(slz):  # noqa: F811
+    # matrices without elements take no memory; 2^32 + 3 is not 3
+    long = 2 ** 32 + 3
+    tall, wide, three = torch.empty((long, 0), device="cuda"), torch.empty((0, long), device="cuda"), torch.empty((3, 0), device="cuda")
+    labels, one = torch.empty(0, dtype=torch.int64, device="cuda"), scales(3, 1)
+    for call in (lambda: slz.quantize_i8(wide), lambda: slz.linear_i8(tall, three.to(torch.int8)[:0], one[:0]), lambda: slz.linear_ce(wide, wide, labels),
+                 lambda: slz.matmul_i8(wide.to(torch.int8), one[:0], wide.to(torch.int8), one[:0]),
+                 lambda: slz.orthogonalize(tall), lambda: slz.orthogonalize(torch.empty((long, 0, 4), device="cuda"))):
+        with pytest.raises(slz.SlzError):
+            call()
