@@ -2,7 +2,10 @@
 
 As in the rest of the binding the functions check their arguments, hand pointers and the current stream to the library and return at once.
 Matrices are CUDA tensors on the current device with unit stride along their rows (any distance between rows).  Workspaces
-come from torch's allocator on the current stream, so that their memory is not given away before the call's work on it is done."""
+come from torch's allocator on the current stream, so that their memory is not given away before the call's work on it is done.
+
+The gradients are functions of their own (matmul_i8_grad, linear_ce_grad) and autograd does not know them: results of tensors that require
+a gradient raise an error when a backward pass comes to them."""
 from __future__ import annotations
 
 import ctypes
@@ -116,6 +119,28 @@ def _workspace(fn, where: str, like, *args):
     return ws, ws.data_ptr(), need.value
 
 
+class _NoFormula(torch.autograd.Function):
+    """Results of tensors that require a gradient: without it a backward pass would leave them out and say nothing."""
+
+    @staticmethod
+    def forward(ctx, where, count, *tensors):
+        ctx.where = where
+        ctx.mark_non_differentiable(*(t for t in tensors[:count] if t is not None and not t.is_floating_point()))
+        return tensors[:count]
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("%s: autograd has no formula for it; call it on detached tensors, and matmul_i8_grad or linear_ce_grad for gradients" % ctx.where)
+
+
+def _results(where: str, inputs, *out):
+    for t in inputs:
+        if t.requires_grad and torch.is_grad_enabled():
+            out = _NoFormula.apply(where, len(out), *out, *inputs)
+            break
+    return out if len(out) > 1 else out[0]
+
+
 def quantize_i8(x):
     """slz_quantize_i8: x [rows][cols] -> (int8 [rows][cols], scale float32 [rows])."""
     ld = _matrix(x, "x", _TYPES)
@@ -124,7 +149,7 @@ def quantize_i8(x):
     scale = torch.empty(rows, dtype=torch.float32, device=x.device)
     _check(_lib().slz_quantize_i8(x.data_ptr(), _TYPES[x.dtype], rows, cols, ld, q.data_ptr(), max(cols, 1), scale.data_ptr(), _stream(x)),
            "slz_quantize_i8")
-    return q, scale
+    return _results("quantize_i8", (x,), q, scale)
 
 
 def matmul_i8(a, a_scale, b, b_scale, dtype=torch.bfloat16):
@@ -142,7 +167,7 @@ def matmul_i8(a, a_scale, b, b_scale, dtype=torch.bfloat16):
     L = _lib()
     ws, at, need = _workspace(L.slz_matmul_i8_workspace, "slz_matmul_i8", a, ctypes.byref(sh), a.data_ptr(), b.data_ptr())
     _check(L.slz_matmul_i8(ctypes.byref(sh), a.data_ptr(), sa, b.data_ptr(), sb, y.data_ptr(), at, need, stream), "slz_matmul_i8")
-    return y
+    return _results("matmul_i8", (a_scale, b_scale), y)
 
 
 def linear_i8(x, w, w_scale):
@@ -158,7 +183,7 @@ def linear_i8(x, w, w_scale):
     L = _lib()
     ws, at, need = _workspace(L.slz_linear_i8_workspace, "slz_linear_i8", x, ctypes.byref(sh), x.data_ptr(), w.data_ptr())
     _check(L.slz_linear_i8(ctypes.byref(sh), x.data_ptr(), w.data_ptr(), sw, y.data_ptr(), at, need, stream), "slz_linear_i8")
-    return y
+    return _results("linear_i8", (x, w_scale), y)
 
 
 def matmul_i8_grad(dy, a, a_scale, b, b_scale, need_a: bool = True, need_b: bool = True):
@@ -178,7 +203,7 @@ def matmul_i8_grad(dy, a, a_scale, b, b_scale, need_a: bool = True, need_b: bool
     ws, at, need = _workspace(L.slz_matmul_i8_grad_workspace, "slz_matmul_i8_grad", dy, ctypes.byref(sh), dy.data_ptr())
     _check(L.slz_matmul_i8_grad(ctypes.byref(sh), dy.data_ptr(), a.data_ptr(), sa, b.data_ptr(), sb, da.data_ptr() if need_a else None,
                                 max(k, 1), db.data_ptr() if need_b else None, max(k, 1), at, need, stream), "slz_matmul_i8_grad")
-    return da, db
+    return _results("matmul_i8_grad", (dy, a_scale, b_scale), da, db)
 
 
 def _ce_shape(h, w, labels, ignore_index):
@@ -200,7 +225,7 @@ def linear_ce(h, w, labels, ignore_index: int = -100):
     ws, at, need = _workspace(L.slz_linear_ce_workspace, "slz_linear_ce", h, ctypes.byref(sh), h.data_ptr(), w.data_ptr())
     _check(L.slz_linear_ce(ctypes.byref(sh), h.data_ptr(), w.data_ptr(), at_labels, loss.data_ptr(), lse.data_ptr(), at, need, stream),
            "slz_linear_ce")
-    return loss, lse
+    return _results("linear_ce", (h, w), loss, lse)
 
 
 def linear_ce_grad(h, w, labels, lse, dloss, ignore_index: int = -100):
@@ -215,7 +240,7 @@ def linear_ce_grad(h, w, labels, lse, dloss, ignore_index: int = -100):
     ws, at, need = _workspace(L.slz_linear_ce_grad_workspace, "slz_linear_ce_grad", h, ctypes.byref(sh), h.data_ptr(), w.data_ptr())
     _check(L.slz_linear_ce_grad(ctypes.byref(sh), h.data_ptr(), w.data_ptr(), at_labels, at_lse, at_dloss, dh.data_ptr(), dw.data_ptr(), at,
                                 need, stream), "slz_linear_ce_grad")
-    return dh, dw
+    return _results("linear_ce_grad", (h, w, lse, dloss), dh, dw)
 
 
 def orthogonalize(g, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7):
@@ -235,4 +260,4 @@ def orthogonalize(g, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
     L = _lib()
     ws, at, need = _workspace(L.slz_orthogonalize_workspace, "slz_orthogonalize", g, ctypes.byref(sh))
     _check(L.slz_orthogonalize(ctypes.byref(sh), g.data_ptr(), out.data_ptr(), at, need, stream), "slz_orthogonalize")
-    return out
+    return _results("orthogonalize", (g,), out)

@@ -124,3 +124,22 @@ def test_the_binding_refuses_lengths_beyond_32_bits(slz):  # noqa: F811
                  lambda: slz.orthogonalize(tall), lambda: slz.orthogonalize(torch.empty((long, 0, 4), device="cuda"))):
         with pytest.raises(slz.SlzError):
             call()
+
+
+def test_a_backward_pass_does_not_skip_what_autograd_cannot_do(slz):  # noqa: F811
+    h, w, labels, dloss = ce_inputs(8, 32, 50, torch.float32, 4)
+    b, s = int8((4, 32), 2), scales(4, 3)
+    q, sq = slz.quantize_i8(h)
+    lse = slz.linear_ce(h, w, labels)[1]
+    plain = slz.linear_ce(h, w, labels)[0]
+    assert not plain.requires_grad
+    p = h.clone().requires_grad_()
+    for result in (lambda: slz.linear_ce(p, w, labels)[0], lambda: slz.linear_i8(p, b, s), lambda: slz.orthogonalize(p), lambda: slz.quantize_i8(p)[1],
+                   lambda: slz.linear_ce_grad(p, w, labels, lse, dloss)[1], lambda: slz.matmul_i8_grad(p[:, :4], q, sq, b, s, need_b=False)[0],
+                   lambda: slz.matmul_i8(q, p[:, 0].contiguous(), b, s, torch.float32)):
+        with pytest.raises(RuntimeError, match="autograd"):
+            (result().sum() + p.sum()).backward()
+        with torch.no_grad():
+            assert not result().requires_grad
+    assert torch.equal(slz.linear_ce(p, w, labels)[0].detach(), plain)
+    assert not slz.quantize_i8(p)[0].requires_grad
