@@ -383,10 +383,9 @@ static int slz_gemm_launch(slz_gemm p, const EPI &epi, uint32_t batches, hipStre
     }
     return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
 }
-// operands of two pieces (a_piece[1] and b_piece[1]: the second ones), tiles of 128 or 64
+// operands of two pieces (a_piece[1] and b_piece[1]: the second ones)
 template <int EL, bool A_ROWS_K, bool B_ROWS_K, class EPI>
-static int slz_gemm_run2(const slz_gemm &p, const EPI &epi, uint32_t side, uint32_t batches, hipStream_t s) {
-    if (side == 128) return slz_gemm_launch<slz_tiling<128, 128, 2, 4>, EL, A_ROWS_K, B_ROWS_K, 2>(p, epi, batches, s);
+static int slz_gemm_run2(const slz_gemm &p, const EPI &epi, uint32_t batches, hipStream_t s) {
     return slz_gemm_launch<slz_tiles_64, EL, A_ROWS_K, B_ROWS_K, 2>(p, epi, batches, s);
 }
 template <int EL, bool A_ROWS_K, bool B_ROWS_K, class EPI>

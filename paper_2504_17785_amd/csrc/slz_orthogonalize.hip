@@ -651,7 +651,7 @@ static void small_slices(orth_plan &P) {
     P.slice = 16384 / P.padded;
     P.slices = (P.n + P.slice - 1) / P.slice;
 }
-// Two pieces: three products one after the other in any tiling, or tiles of 128 or 64 that load both pieces at once.  These read a third less, but large
+// Two pieces: three products one after the other in any tiling, or tiles of 64 that load both pieces at once.  These read a third less, but large
 // tiles read less still: f32, 6 x 500 x 1000 277 us together and 345 in turn, 1024^2 279 and 431, 4096 x 8192 9532 and 6889
 static slz_choice orth_choose(const orth_plan &P, uint32_t N, uint32_t steps, uint32_t batch, bool symmetric, uint32_t most_ranges, bool rows_k) {
     if (P.pieces == 1) return slz_choose(P.m, N, steps, batch, symmetric, most_ranges, rows_k);
@@ -795,7 +795,7 @@ static int orth_small(const slz_orth_shape *sh, const orth_plan &P, const void *
 }
 
 template <bool B_ROWS_K, class EPI> static int orth_run(const slz_gemm &p, const EPI &epi, const slz_choice &c, uint32_t batches, hipStream_t s) {
-    return c.pieces == 2 ? slz_gemm_run2<SLZ_EL_F16, false, B_ROWS_K>(p, epi, c.side, batches, s) : slz_gemm_run<SLZ_EL_F16, false, B_ROWS_K>(p, epi, c.side, batches, s);
+    return c.pieces == 2 ? slz_gemm_run2<SLZ_EL_F16, false, B_ROWS_K>(p, epi, batches, s) : slz_gemm_run<SLZ_EL_F16, false, B_ROWS_K>(p, epi, c.side, batches, s);
 }
 extern "C" int slz_orthogonalize(const slz_orth_shape *sh, const void *g, void *out, void *ws, size_t ws_bytes, void *stream) {
     const int rc0 = orth_check(sh);

@@ -41,10 +41,11 @@ template <int T> constexpr bool slz_places_t() {
 // and leave less of it idle at the end.  Ranges of k cost a second launch that reads their sums.
 // rows_k: an operand's rows are k.  All sides then take longer, and 192 by more than the others: 2688^2 with 256, 192, 128, 64: 111, 81, 67, 93 us where
 // 92, 62, 59, 83 with k contiguous, 5184^2 by 2048 deep 121, 129, 127, 165 (98, 102, 108, 151).  The estimate compares sides, so only 192 gets another figure.
-struct slz_choice { uint32_t side, split; double us; uint32_t pieces = 1; };     // pieces: of a number that are loaded together
+// pieces: of a number that are loaded together, in tiles of 64 (0.5 us a step, 0.42 for each of several; one of 128 1.9, more than the four in its place)
+struct slz_choice { uint32_t side, split; double us; uint32_t pieces = 1; };
 static inline double slz_step_us(uint32_t side, double tiles, uint32_t pieces, bool rows_k) {
     const auto rounds = [&](double at_once) { return (double)(uint64_t)((tiles + at_once - 1) / at_once); };
-    if (pieces == 2) return side == 128 ? rounds(256) * 1.9 : rounds(256) * 0.42 > 0.5 ? rounds(256) * 0.42 : 0.5;
+    if (pieces == 2) return rounds(256) * 0.42 > 0.5 ? rounds(256) * 0.42 : 0.5;
     if (side == 256) return rounds(256) * 1.5;
     if (side == 192) return rounds(256) * (rows_k ? 1.1 : 0.95);
     if (side == 64) return rounds(256) * 0.18 > 0.33 ? rounds(256) * 0.18 : 0.33;
@@ -55,7 +56,7 @@ static inline slz_choice slz_choose(uint32_t M, uint32_t N, uint32_t steps, uint
                                     bool any_side = true, uint32_t pieces = 1) {
     slz_choice best = {64, 1, 1e30};
     for (const uint32_t side : {256u, 192u, 128u, 64u}) {
-        if ((side == 192 && !any_side) || (side == 256 && symmetric) || (side > 128 && pieces == 2)) continue;
+        if ((side == 192 && !any_side) || (side == 256 && symmetric) || (side > 64 && pieces == 2)) continue;
         const double tm = (M + side - 1) / side, tn = (N + side - 1) / side, tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batches;
         for (uint32_t split = 1; split <= most_ranges && (split == 1 || steps >= 4 * split); split *= 2) {
             double us = ((steps + split - 1) / split) * slz_step_us(side, tiles * split, pieces, rows_k);
