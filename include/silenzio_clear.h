@@ -85,8 +85,8 @@ int slz_linear_ce(const slz_ce_shape *shape, const void *h_dev, const void *w_de
 
 /* With lse of slz_linear_ce and dloss [tokens] the gradient of what the losses are used for:
  *   g_tv = (exp(z_tv - lse_t) - [v = label_t]) dloss_t (0 for ignored tokens, NaN for labels out of range),  dh = g w,  dw = g^T h.
- * The z are computed again, in pieces of the vocabulary; a piece's g is held in h's type (f16: times a power of two; f32: in
- * 24 bits), the sums in 32 bits.  dh [tokens][inner], dw [vocab][inner]. */
+ * The z are computed again, in pieces of the vocabulary; a piece's g is held in h's type (f16, bf16: relative to
+ * the largest finite |dloss| of the tokens that count; f32: in 24 bits), the sums in 32 bits.  dh [tokens][inner], dw [vocab][inner]. */
 int slz_linear_ce_grad_workspace(const slz_ce_shape *shape, const void *h_dev, const void *w_dev, size_t *bytes);
 int slz_linear_ce_grad(const slz_ce_shape *shape, const void *h_dev, const void *w_dev, const int64_t *labels_dev,
                        const float *lse_dev, const float *dloss_dev, void *dh_dev, void *dw_dev, void *workspace_dev,

@@ -187,6 +187,6 @@ size_t slz_operand_bytes(const void *p, int type, uint32_t rows, uint32_t cols, 
 slz_operand slz_operand_of(const void *p, int type, uint32_t rows, uint32_t cols, int64_t ld, char *ws, slz_layouts &jobs);
 size_t slz_operand_i8_bytes(const int8_t *p, uint32_t rows, uint32_t cols, int64_t ld);
 slz_operand slz_operand_i8_of(const int8_t *p, uint32_t rows, uint32_t cols, int64_t ld, char *ws, slz_layouts &jobs);
-// *unit: the power of two above the largest finite magnitude of `count` values, from 2^-100 to 2^100; what f16 could not hold is divided by it.
-// With labels only the values count whose label lies in [0, classes) and is not `ignore`.
+// What a type of few bits could not hold is divided by *unit, from 2^-100 to 2^100 (1 where there is nothing above 0).  Without labels the power of two above
+// the largest finite magnitude of `count` values; with labels this magnitude itself, of the values whose label lies in [0, classes) and is not `ignore`.
 void slz_unit_of(const float *values, uint32_t count, float *unit, hipStream_t s, const int64_t *labels = nullptr, int64_t ignore = 0, uint32_t classes = 0);

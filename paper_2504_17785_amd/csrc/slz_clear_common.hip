@@ -82,7 +82,7 @@ slz_operand slz_operand_i8_of(const int8_t *p, uint32_t rows, uint32_t cols, int
     return o;
 }
 
-// One workgroup: the power of two above the largest of the finite magnitudes (1 where there is none)
+// One workgroup
 __global__ void __launch_bounds__(256)
 k_scale_unit(const float *__restrict__ scale, uint32_t count, float *__restrict__ unit, const int64_t *__restrict__ labels, int64_t ignore, uint32_t classes) {
     float top = 0.0f;
@@ -102,7 +102,8 @@ k_scale_unit(const float *__restrict__ scale, uint32_t count, float *__restrict_
         top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
         int e = 0;
         if (top > 0.0f) frexpf(top, &e);
-        *unit = ldexpf(1.0f, e < -100 ? -100 : e > 100 ? 100 : e);
+        if (labels && top > 0.0f) *unit = fminf(fmaxf(top, 0x1p-100f), 0x1p100f);
+        else *unit = ldexpf(1.0f, e < -100 ? -100 : e > 100 ? 100 : e);
     }
 }
 

@@ -293,7 +293,7 @@ template <class F> struct slz_store_epi {
     }
 };
 
-// the sum times a constant and, if given, a power of two that the operand was divided by
+// the sum times a constant and, if given, a number that the operand was divided by
 struct slz_times_unit {
     const float *unit;
     float by;

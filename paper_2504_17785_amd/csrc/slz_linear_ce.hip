@@ -13,7 +13,9 @@
 // a piece's g takes this much at most (at least 1024 words of the vocabulary)
 #define CE_PIECE_BYTES ((size_t)128 << 20)
 #define CE_PIECE_WORDS ((size_t)1 << 21)     // rows of g stay as short as any operand's
-// f16: g is held times this; |g| <= |dloss|, so that the largest stay finite and those from 2^-28 of the largest keep 11 bits
+// bf16 and f16: g is held relative to the largest |dloss| that counts.  Losses are often weighted alike (a mean), and then the label's g, -1 + p, loses little,
+// where the rounding of -dloss would be the same for all tokens: an error of all of dh and dw of up to 2^-8 (bf16) or 2^-11 (f16).
+// f16: times CE_F16_UP; |g| <= |dloss|, so that the largest stay finite and those from 2^-28 of the largest keep 11 bits
 #define CE_F16_UP 16384.0f
 
 // (maximum, sum of exp(z - maximum)) of two sets of z; a set whose z are all -inf has (-inf, 0) and adds nothing
@@ -140,7 +142,7 @@ struct ce_grad_epi {
     template <int MI, int NI, bool RUN, bool WHOLE, class ACC>
     __device__ __forceinline__ void part(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p) const {
         const uint32_t n0 = slz_col<NI, RUN>(at, 0), wide = (p.N + 7u) & ~7u;
-        const float up = type == SLZ_F16 ? CE_F16_UP / *unit : 1.0f;
+        const float up = type == SLZ_F32 ? 1.0f : (type == SLZ_F16 ? CE_F16_UP : 1.0f) / *unit;
         float bys[MI], ls[MI];                         // read for all rows before the first is written
         int words[MI];                                 // -2: not counted
 #pragma unroll
@@ -508,8 +510,8 @@ extern "C" int slz_linear_ce_grad(const slz_ce_shape *sh, const void *h, const v
     hipStream_t s = (hipStream_t)stream;
     char *base = (char *)ws;
     float *dh_sum = (float *)(base + P.dh), *unit = (float *)(base + P.unit);
-    if (sh->type == SLZ_F16) slz_unit_of(dloss, sh->tokens, unit, s, labels, sh->ignore_index, sh->vocab);
-    const slz_times_unit f{sh->type == SLZ_F16 ? unit : nullptr, 1.0f / CE_F16_UP};
+    if (sh->type != SLZ_F32) slz_unit_of(dloss, sh->tokens, unit, s, labels, sh->ignore_index, sh->vocab);
+    const slz_times_unit f{sh->type != SLZ_F32 ? unit : nullptr, sh->type == SLZ_F16 ? 1.0f / CE_F16_UP : 1.0f};
     slz_layouts jobs = {};
     const slz_operand oh = slz_operand_of(h, sh->type, sh->tokens, sh->inner, sh->ld_h, base + P.h, jobs);
     const slz_operand g{base + P.g, (int64_t)P.g_row, (int64_t)up256((size_t)sh->tokens * P.g_row), oh.pieces, oh.element};

@@ -143,3 +143,22 @@ def test_a_backward_pass_does_not_skip_what_autograd_cannot_do(slz):  # noqa: F8
             assert not result().requires_grad
     assert torch.equal(slz.linear_ce(p, w, labels)[0].detach(), plain)
     assert not slz.quantize_i8(p)[0].requires_grad
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("weight", [(1 + 2.0 ** -8) / 32, (1 + 2.0 ** -11) / 32, 1 / 3584, 1 / 7])
+def test_a_common_dloss_is_not_rounded(slz, dtype, weight):  # noqa: F811
+    # all tokens alike: the rounding of dloss to the type would be one error of all of the gradient
+    h, w, labels, dloss = ce_inputs(200, 128, 3000, dtype, 70)
+    labels[::9] = IGNORED
+    dloss[:] = weight
+    lse = slz.linear_ce(h, w, labels)[1]
+    g = torch.softmax(h.to(WIDE) @ w.to(WIDE).t().contiguous(), 1)
+    counts = labels != IGNORED
+    g[counts, labels[counts]] -= 1
+    g *= torch.where(counts, dloss.to(WIDE), 0.0)[:, None]
+    for got, want in zip(slz.linear_ce_grad(h, w, labels, lse, dloss), (g @ w.to(WIDE), g.t().contiguous() @ h.to(WIDE))):
+        # root mean squares: -1 + p is off by 0.29 U (half a place below 1 at most), the result by 0.43 U, p by 0.43 U of its share of g, below a half:
+        # together less than one and a half times the result's own
+        own = (want.to(dtype).to(WIDE) - want).norm() if dtype != torch.float32 else 2.0 ** -20 * want.norm()
+        assert (got.to(WIDE) - want).norm() <= 1.5 * own
