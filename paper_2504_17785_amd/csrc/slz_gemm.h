@@ -263,6 +263,16 @@ template <int NI, bool RUN> __device__ __forceinline__ uint32_t slz_col(const sl
 }
 
 // ---- epilogues ---------------------------------------------------------------------------------------------------------------
+// What is done with a sum, with all that is the same for all of them read: a thread's stores might change it, as far as the compiler knows
+template <class F> __device__ __forceinline__ F slz_ready(const F &f) { return f; }
+// the sum times a constant and, if given, a number that the operand was divided by
+struct slz_times { float by; __device__ __forceinline__ float operator()(uint32_t, uint32_t, uint32_t, float sum) const { return sum * by; } };
+struct slz_times_unit {
+    const float *unit;
+    float by;
+};
+__device__ __forceinline__ slz_times slz_ready(const slz_times_unit &f) { return {f.unit ? *f.unit * f.by : 1.0f}; }
+
 // out[m][n] = f(m, n, sum), rounded once to the type
 template <class F> struct slz_store_epi {
     void *out;
@@ -276,6 +286,7 @@ template <class F> struct slz_store_epi {
     __device__ __forceinline__ void run(const ACC (&acc)[MI][NI], const slz_place &at, const slz_gemm &p, float *) const {
         constexpr int C = RUN ? NI * 4 : 4, PARTS = RUN ? 1 : NI;
         const uint32_t eb = slz_type_bytes(type);
+        const auto value = slz_ready(f);
 #pragma unroll
         for (int i = 0; i < MI; i++) {
             const uint32_t m = slz_row(at, i);
@@ -286,18 +297,11 @@ template <class F> struct slz_store_epi {
                 if (n >= p.N) continue;
                 float v[C];
 #pragma unroll
-                for (int c = 0; c < C; c++) v[c] = f(at.batch, m, min(n + c, p.N - 1), acc[i][q + c / 4][c % 4]);
+                for (int c = 0; c < C; c++) v[c] = value(at.batch, m, min(n + c, p.N - 1), acc[i][q + c / 4][c % 4]);
                 slz_put_run<C>((char *)out + (at.batch * batch_stride + (int64_t)m * ld + n) * eb, type, v, p.N - n, aligned);
             }
         }
     }
-};
-
-// the sum times a constant and, if given, a number that the operand was divided by
-struct slz_times_unit {
-    const float *unit;
-    float by;
-    __device__ __forceinline__ float operator()(uint32_t, uint32_t, uint32_t, float sum) const { return unit ? sum * (*unit * by) : sum; }
 };
 
 // the sums themselves, or added to what is there, of each range: ws[range][batch][M][ld], ld a multiple of 16
@@ -329,11 +333,12 @@ template <class T, class F>
 __global__ void __launch_bounds__(256) k_join(const T *ws, uint32_t ranges, uint32_t M, uint32_t N, uint32_t ld, void *out, int type, int64_t ld_out, F f) {
     const size_t total = (size_t)M * ((N + 3) / 4), stride = (size_t)M * ld;
     typedef T t4 __attribute__((ext_vector_type(4)));
+    const auto value = slz_ready(f);
     for (size_t g = (size_t)blockIdx.x * 256 + threadIdx.x; g < total; g += (size_t)gridDim.x * 256) {
         const uint32_t m = (uint32_t)(g / ((N + 3) / 4)), n = (uint32_t)(g % ((N + 3) / 4)) * 4;
         t4 sum = *(const t4 *)(ws + (size_t)m * ld + n);
         for (uint32_t r = 1; r < ranges; r++) sum += *(const t4 *)(ws + r * stride + (size_t)m * ld + n);
-        for (uint32_t c = 0; c < 4 && n + c < N; c++) slz_put(out, type, (size_t)m * ld_out + n + c, f(0, m, n + c, sum[c]));
+        for (uint32_t c = 0; c < 4 && n + c < N; c++) slz_put(out, type, (size_t)m * ld_out + n + c, value(0, m, n + c, sum[c]));
     }
 }
 
