@@ -61,7 +61,7 @@ int slz_linear_i8(const slz_i8_shape *shape, const void *x_dev, const int8_t *b_
 /* Gradients with respect to the values A_ik = a_scale_i a_ik and B_jk = b_scale_j b_jk (the rounding of a quantisation is passed
  * straight through):  da_ik = sum_j dy_ij B_jk,  db_jk = sum_i dy_ij A_ik.  dy is [m][n] with ld_y, da [m][k], db [n][k]; either
  * of the two may be null.  For bf16 and f16 the values A and B are rounded to 8 and 11 bits for the products, which are summed
- * in 32 bits (f16: to fewer in rows whose scale is below 2^-22 of the largest finite one); for f32 they are carried in 24 bits. */
+ * in 32 bits (f16: to fewer in rows whose scale is below 2^-22 of the largest finite one; a single row is not rounded); for f32 they are carried in 24 bits. */
 int slz_matmul_i8_grad_workspace(const slz_i8_shape *shape, const void *dy_dev, size_t *bytes);
 int slz_matmul_i8_grad(const slz_i8_shape *shape, const void *dy_dev, const int8_t *a_dev, const float *a_scale_dev,
                        const int8_t *b_dev, const float *b_scale_dev, void *da_dev, int64_t ld_da, void *db_dev, int64_t ld_db,

@@ -417,6 +417,8 @@ extern "C" int slz_linear_i8(const slz_i8_shape *sh, const void *x, const int8_t
 // not hold small scales, so its values are held times VALUES_F16_UP / `unit`, the power of two above the largest scale, and the sums multiplied by the inverse:
 // magnitudes of up to 128 2^8 are below f16's largest, and rows whose scale is down to 2^-22 of the largest keep 11 bits.
 #define VALUES_F16_UP 256.0f
+// One row (no scale given): the integers themselves, which every type holds exactly, and the sums are multiplied by its scale.  Rounded with the scale in them the
+// entries of one row can all be off the same way, by up to half as much again as the result's own rounding; over many rows that evens out.
 typedef uint64_t u64_any __attribute__((aligned(1)));
 // eight values of a row per thread; bound by memory: 4096 x 4096 to bf16 10.5 us (48 MiB, 4.8 TB/s)
 template <int TYPE>
@@ -430,7 +432,7 @@ k_values(const int8_t *__restrict__ q, const float *__restrict__ scale, const fl
         uint32_t c;
         const size_t r = slz_divide(g, per_row, total <= 0xffffffffu, c);
         c *= 8;
-        const float sc = TYPE == SLZ_F16 ? scale[r] / *unit * VALUES_F16_UP : scale[r];
+        const float sc = !scale ? 1.0f : TYPE == SLZ_F16 ? scale[r] / *unit * VALUES_F16_UP : scale[r];
         uint64_t bytes = 0;
         if (c + 8u <= cols) bytes = *(const u64_any *)(q + r * ld_q + c);
         else
@@ -485,13 +487,14 @@ static int grad_product(const slz_i8_shape *sh, const slz_operand &left, bool le
                         uint32_t rows, void *out, int64_t ld_out, char *values, float *unit, char *ranges, const grad_plan &P, hipStream_t s) {
     const int type = sh->type;
     const slz_operand right{values, (int64_t)P.row, (int64_t)up256((size_t)rows * P.row), left.pieces, left.element};
-    if (type == SLZ_F16) slz_unit_of(scale, rows, unit, s);
+    const bool one = rows == 1, with_unit = type == SLZ_F16 && !one;
+    if (with_unit) slz_unit_of(scale, rows, unit, s);
     if (rows) {
         const auto k = type == SLZ_F32 ? k_values<SLZ_F32> : type == SLZ_BF16 ? k_values<SLZ_BF16> : k_values<SLZ_F16>;
-        hipLaunchKernelGGL(k, ew_grid((size_t)rows * P.row / 16), dim3(256), 0, s, q, scale, unit, rows, sh->k, ld_q, values, P.row, right.piece);
+        hipLaunchKernelGGL(k, ew_grid((size_t)rows * P.row / 16), dim3(256), 0, s, q, one ? nullptr : scale, unit, rows, sh->k, ld_q, values, P.row, right.piece);
     }
     const slz_gemm p = slz_gemm_of(left, right, M, sh->k, rows);
-    const slz_times_unit f{type == SLZ_F16 ? unit : nullptr, 1.0f / VALUES_F16_UP};
+    const slz_times_unit f{one ? scale : with_unit ? unit : nullptr, one ? 1.0f : 1.0f / VALUES_F16_UP};
     if (type == SLZ_F16)
         return left_rows_k ? slz_gemm_to<SLZ_EL_F16, true, true>(p, P.db, f, out, type, ld_out, ranges, s)
                            : slz_gemm_to<SLZ_EL_F16, false, true>(p, P.da, f, out, type, ld_out, ranges, s);

@@ -162,3 +162,17 @@ def test_a_common_dloss_is_not_rounded(slz, dtype, weight):  # noqa: F811
         # together less than one and a half times the result's own
         own = (want.to(dtype).to(WIDE) - want).norm() if dtype != torch.float32 else 2.0 ** -20 * want.norm()
         assert (got.to(WIDE) - want).norm() <= 1.5 * own
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", [(1 + 2.0 ** -8) / 64, (1 + 2.0 ** -11) / 64, 0.0123, 0.0, float("nan")])
+def test_gradients_of_one_row(slz, dtype, scale):  # noqa: F811
+    # one token: integers times one scale, each gradient of it rounded once
+    n, k = 70, 300
+    a, b = int8((1, k), 1), int8((n, k), 2)
+    s, one, dy = torch.full((1,), scale, device="cuda"), scales(n, 3), randn((1, n), 4, dtype)
+    _, db = slz.matmul_i8_grad(dy, a, s, b, one, need_a=False)
+    want = dy.to(WIDE).t().contiguous() @ (a.to(WIDE) * s.to(WIDE))
+    inside(db, want, (want.abs() * (1.01 * U[dtype] + 3 * 2.0 ** -24)).nan_to_num() + LEAST[dtype], "db")
+    da, _ = slz.matmul_i8_grad(dy.t().contiguous(), b, one, a, s, need_b=False)
+    inside(da, want, (want.abs() * (1.01 * U[dtype] + 3 * 2.0 ** -24)).nan_to_num() + LEAST[dtype], "da")
