@@ -1,5 +1,5 @@
 """Training the paper's kind of network in the clear, on the card: an MLP whose hidden layers take 8-bit integers, as the encrypted
-run's do, so that its weights and scales can be the encrypted run's start and its results what that run is compared with.
+run's do, so that its results are what that run is compared with.
 
 A step, next to the gadgets that do the same on ciphertexts:
   quantize_i8 + matmul_i8      the layers' products                    Matmul^RNS, Shift2MSBs
@@ -57,7 +57,7 @@ class Mlp:
         return loss.sum() / counts.sum()
 
     def freeze(self):
-        """8-bit weights of all layers with their scales: what is answered with, and what an encrypted run starts from."""
+        """8-bit weights of all layers with their scales: what is answered with."""
         return [slz.quantize_i8(w) for w in self.weights]
 
 

@@ -1,5 +1,5 @@
-/* Training and running a network in the clear, next to the gadgets that do it on ciphertexts (silenzio_gadgets.h): what finds
- * the scales and starting weights of an encrypted run and what its results are compared against.
+/* Training and running a network in the clear, next to the gadgets that do it on ciphertexts (silenzio_gadgets.h): what an
+ * encrypted run is compared with.  Scales are any numbers here; the gadgets' block scaling is by powers of two.
  *   slz_quantize_i8, slz_matmul_i8, slz_linear_i8, slz_matmul_i8_grad   products of 8-bit integers with a scale per row
  *   slz_linear_ce, slz_linear_ce_grad     softmax cross entropy of a linear layer's outputs, without keeping them, and its gradient
  *   slz_orthogonalize                     updates orthogonalised by Newton-Schulz products
@@ -47,7 +47,8 @@ typedef struct {
     int64_t ld_a, ld_b, ld_y;            /* ld_a is x's in slz_linear_i8 */
 } slz_i8_shape;
 
-/* y_ij = a_scale_i b_scale_j sum_k a_ik b_jk: the sum exact in 32-bit integers, one rounding to 32 bits and one to y's type.
+/* y_ij = a_scale_i b_scale_j sum_k a_ik b_jk: the sum exact in 32-bit integers and then rounded to 32-bit floating point, times the
+ * product of the scales, each operation in 32 bits, and one rounding to y's type.
  * Entries may be any int8.  SLZ_E_TOO_LARGE also for k >= 2^17, where the sum could leave 32 bits. */
 int slz_matmul_i8_workspace(const slz_i8_shape *shape, const int8_t *a_dev, const int8_t *b_dev, size_t *bytes);
 int slz_matmul_i8(const slz_i8_shape *shape, const int8_t *a_dev, const float *a_scale_dev, const int8_t *b_dev,
@@ -78,7 +79,8 @@ typedef struct {
 /* z_tv = sum_d h_td w_vd, lse_t = log sum_v exp z_tv, loss_t = lse_t - z_t,label.  loss is 0 where the label is ignore_index and NaN
  * where another label lies outside [0, vocab).  The z are summed and kept in 32 bits, a tile of the vocabulary at a time; none
  * is written to memory.  A z of NaN or +inf makes its token's results NaN; one of -inf adds nothing (f32: an infinity in h or w
- * counts as NaN).  A token's results have the same bits whatever the other tokens are.  labels int64 [tokens], loss and lse [tokens] 32-bit floating point. */
+ * counts as NaN).  A token's results have the same bits whatever the other tokens are.  labels int64 [tokens], loss and lse [tokens] 32-bit floating point.
+ * The workspace has 8 bytes for every token and 32 words, an eighth of the z in 16 bits. */
 int slz_linear_ce_workspace(const slz_ce_shape *shape, const void *h_dev, const void *w_dev, size_t *bytes);
 int slz_linear_ce(const slz_ce_shape *shape, const void *h_dev, const void *w_dev, const int64_t *labels_dev, float *loss_dev,
                   float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
@@ -86,7 +88,8 @@ int slz_linear_ce(const slz_ce_shape *shape, const void *h_dev, const void *w_de
 /* With lse of slz_linear_ce and dloss [tokens] the gradient of what the losses are used for:
  *   g_tv = (exp(z_tv - lse_t) - [v = label_t]) dloss_t (0 for ignored tokens, NaN for labels out of range),  dh = g w,  dw = g^T h.
  * The z are computed again, in pieces of the vocabulary; a piece's g is held in h's type (f16, bf16: relative to
- * the largest finite |dloss| of the tokens that count; f32: in 24 bits), the sums in 32 bits.  dh [tokens][inner], dw [vocab][inner]. */
+ * the largest finite |dloss| of the tokens that count; f32: in 24 bits), the sums in 32 bits.  dh [tokens][inner],
+ * dw [vocab][inner].  A g of 0 times an infinity or NaN is NaN, as in the formula: a row of h that holds one reaches dw even where its token is ignored. */
 int slz_linear_ce_grad_workspace(const slz_ce_shape *shape, const void *h_dev, const void *w_dev, size_t *bytes);
 int slz_linear_ce_grad(const slz_ce_shape *shape, const void *h_dev, const void *w_dev, const int64_t *labels_dev,
                        const float *lse_dev, const float *dloss_dev, void *dh_dev, void *dw_dev, void *workspace_dev,

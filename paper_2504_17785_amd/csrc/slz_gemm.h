@@ -4,10 +4,11 @@
 //
 // An operand is stored with k contiguous (rows m or n) or with m / n contiguous (rows k).  A workgroup of WM x WN waves computes a
 // TM x TN tile; in steps of 128 bytes of k (64 or 128 elements) both operands' tiles go from memory straight to shared memory in
-// 16-byte pieces, double buffered: the next step's pieces are under way while the matrix instructions run on this step's.
+// 16-byte pieces, double buffered: the next step's pieces are under way while the matrix instructions run on this step's.  Where an operand's rows are k only
+// part of the step overlaps: the compiler lets all loads finish before the first transposing read after them, as it cannot tell which buffer they fill.
 // Shared memory has no padding (the direct loads write a wave's 1 KiB in a row), so a piece's place within its row is its
-// index XOR some bits of the row number, chosen so that the lanes that read together meet different banks: a matrix-instruction operand is
-// eight (int8: sixteen) consecutive k of one row.  Where rows are k it is read through the transposing ds_read_b64_tr_b16.
+// index XOR some bits of the row number, chosen so that the lanes that read together meet different banks (tiles of 192 and 64 whose rows are k: two meet; for
+// 192 other bits without that took the same time): a matrix-instruction operand is eight (int8: sixteen) consecutive k of one row.  Where rows are k it is read through the transposing ds_read_b64_tr_b16.
 // The instruction gets B's rows as its rows and A's as its columns: a lane then holds consecutive columns of C for one row.
 //
 // Bounds: each step's loads go through a buffer descriptor that begins at the tile's corner and ends with the matrix, so rows past
@@ -147,7 +148,7 @@ template <int MI, int NI, int A_LDS, int B_LDS, int... G> __device__ __forceinli
 }
 
 // Measured, 4096^3 with tiles of 256 (a large library product: 1.40 P/s bf16, 2.15 int8): bf16 1.32 P/s where k is contiguous, 1.04 where B's rows are k,
-// 0.99 where both operands' are, int8 2.07 to 2.5.  The matrix cores are busy 48 to 54 % of the time, waves wait 29 to 41 %, no bank conflicts.  Neither side
+// 0.99 where both operands' are, int8 2.07 (8192^3 2.5).  The matrix cores are busy 48 to 54 % of the time, waves wait 29 to 41 %, no bank conflicts.  Neither side
 // alone is the bound: with the loads off an earlier form ran at 1.46 instead of 1.21, with the matrix instructions off at the time of 1.74; and a loop of
 // matrix instructions alone reaches 1.6 to 2.0 on random data, where the clock falls.
 template <int EL, bool A_ROWS_K, bool B_ROWS_K, int TM, int TN, int WM, int WN, int PIECES, class EPI>

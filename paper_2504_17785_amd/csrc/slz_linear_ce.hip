@@ -5,9 +5,9 @@
 // the label's z; a second kernel joins a token's pairs.
 // Gradient: in pieces of the vocabulary, z again, from it g = (exp(z - lse) - [v = label]) dloss to the workspace, then the two products
 // dw = g^T h (complete for the piece's rows) and dh += g w (summed over the pieces in 32 bits).
-// Bound by the matrix cores where rows are long: 4096 tokens x 4096 x 131072 bf16: forward 3.40 ms (1.29 PFLOP/s), each 16384 words' g 482 us (1.14),
-// dw 546 (1.01), dh 518 (1.06).  Short rows leave the epilogues: 1003 x 768 x 50021 f16: forward 110 us (0.70), g 143 (0.54), dw 135, dh 106; tiles of 256 instead of
-// the 128 taken were no faster for z (105 and, before labels and factors were read ahead, 163 to 160) and slower for dw (163).
+// Bound by the matrix cores where rows are long: 4096 tokens x 4096 x 131072 bf16: forward 3.46 ms (1.27 PFLOP/s), each 16384 words' g 482 us (1.14),
+// dw 538 (1.02), dh 516 (1.06).  Short rows leave the epilogues: 1003 x 768 x 50021 f16: forward 110 us (0.70), g 142 (0.54), dw 118, dh 108; tiles of 256 instead of
+// the 128 taken were no faster for z (105 and, before labels and factors were read ahead, 163 to 160), and slower for dw (product alone 114, 128 with 192, 103 with 128).
 #include "slz_gemm.h"
 
 // a piece's g takes this much at most (at least 1024 words of the vocabulary)

@@ -7,7 +7,7 @@
 //     A A = O O + (d_i + d_j) O_ij + d_i^2 [i = j]  with A = O + diag d,  and  X' = (a + B_ii) X + (B - diag) X.
 // With the operands 8 times as precise as bf16's, and that, a result of 128 to 512 rows differs from the formula's by 4e-4 to 1.1e-3 of its norm (a model of the
 // roundings on the CPU; rounding to bf16 adds 1.7e-3, all operands in bf16 1e-2 to 9e-2); with 16 rows, most singular values a hundredth of the largest, by 4e-3.  For f16 and f32 results O, B and X enter the products with both their halves (three products instead of one).
-// The first X is g times a power of two, exact; what is missing to g / |g| is a factor of the first step.
+// The first X is g times a power of two; what is missing to g / |g| is a factor of the first step.
 // A and A A are symmetric: tiles on and below the diagonal are computed and stored twice.
 // Measured, a step: 4096 x 8192 bf16 A 155 us, B 93, X' 336 (0.82 PFLOP/s; matrix cores 39 % busy, waves wait 51 %); 6 x 500 x 1000 f16 15.3, 13.2, 25.6, where no
 // other tiling is more than 6 % faster: launches of 8 or 16 steps of k, mostly fill and epilogue.
