@@ -2,7 +2,9 @@
  * encrypted run is compared with.  Scales are any numbers here; the gadgets' block scaling is by powers of two.
  *   slz_quantize_i8, slz_matmul_i8, slz_linear_i8, slz_matmul_i8_grad   products of 8-bit integers with a scale per row
  *   slz_linear_ce, slz_linear_ce_grad     softmax cross entropy of a linear layer's outputs, without keeping them, and its gradient
+ *   slz_quantize_i4, slz_values_i4, slz_linear_i4, slz_linear_i4_grad   layers whose weights have 4 bits, with a scale per group of them
  *   slz_orthogonalize                     updates orthogonalised by Newton-Schulz products
+ *   slz_grad_norm, slz_clip_by_norm       the norm that many gradients have together, and all of them held to one
  *
  * Conventions as in silenzio_pbs.h: C ABI, plain device pointers, the caller owns every buffer, work is enqueued on the given
  * HIP stream of the current device and the call returns at once, return codes are the SLZ_* codes.  Nothing is allocated and
@@ -68,6 +70,42 @@ int slz_matmul_i8_grad(const slz_i8_shape *shape, const void *dy_dev, const int8
                        const int8_t *b_dev, const float *b_scale_dev, void *da_dev, int64_t ld_da, void *db_dev, int64_t ld_db,
                        void *workspace_dev, size_t workspace_bytes, void *hip_stream);
 
+/* ---- layers with 4-bit weights ------------------------------------------------------------------------------------------------- */
+/* 4-bit rows: a row of k weights in whole blocks of 128, each of 64 bytes or 16 words of 32 bits.  Word 4 j + s of a block (j, s = 0 .. 3) has the block's
+ * entries 32 s + 8 j + e, e = 0 .. 7: those with e < 4 in the low four bits of byte e, the others in the high four of byte e - 4.  Four
+ * bits are a sign (the highest) and a magnitude of 0 to 7.  Entries past the row's end count for nothing, whatever they are; slz_quantize_i4 writes zeros.
+ * Scales are 32-bit floating point, one for every `group` consecutive weights of a row (the last of a row may have fewer): group is 32, 64 or
+ * 128.  A weight's value is scale times entry.  The rows lie on 16 bytes: the address and ld_q, in bytes, are multiples of 16 (ld_q where there are
+ * several rows); a range of rows, or of columns from a multiple of 128 on, can so be given as it is.  The leading dimensions are of q in bytes and of the scales in elements. */
+
+/* w [rows][cols] to 4 bits: for each group top = max |w|, scale = top / 7 in 32-bit floating point, entry = the whole number nearest to 7 w / top (the
+ * exact quotient, ties to even); a group of zeros has scale 0 and zeros, one with an infinity or NaN scale NaN and zeros. */
+int slz_quantize_i4(const void *w_dev, int type, uint32_t rows, uint32_t cols, int64_t ld_w, uint32_t group, uint8_t *q_dev, int64_t ld_q,
+                    float *scale_dev, int64_t ld_scale, void *hip_stream);
+/* The values of 4-bit rows, out [rows][cols] of `type`: the product in 32 bits, rounded to the type. */
+int slz_values_i4(const uint8_t *q_dev, int64_t ld_q, const float *scale_dev, int64_t ld_scale, uint32_t group, uint32_t rows, uint32_t cols,
+                  void *out_dev, int type, int64_t ld_out, void *hip_stream);
+
+typedef struct {
+    uint32_t m, n, k;                    /* x is m x k, the weights n x k, y is m x n */
+    int type;                            /* of x, y and the gradients */
+    uint32_t group;
+    int64_t ld_x, ld_q, ld_scale, ld_y;  /* ld_y is dy's in slz_linear_i4_grad */
+} slz_i4_shape;
+
+/* y_ij = sum_k x_ik w_jk with the values w, summed in 32 bits and rounded to the type. */
+int slz_linear_i4_workspace(const slz_i4_shape *shape, const void *x_dev, size_t *bytes);
+int slz_linear_i4(const slz_i4_shape *shape, const void *x_dev, const uint8_t *q_dev, const float *scale_dev, void *y_dev, void *workspace_dev,
+                  size_t workspace_bytes, void *hip_stream);
+
+/* Gradients for dy [m][n] with respect to x and to the values (the rounding of a quantisation is passed straight through):
+ *   dx_ik = sum_j dy_ij w_jk,  dw_jk = sum_i dy_ij x_ik.  dx is [m][k], dw [n][k]; either of the two may be null, and then x (without dw) or q and scale (without
+ * dx) are not read.  For bf16 and f16 the values are rounded to 8 and 11 bits for dx (f16: to fewer where the scale is below 2^-26 of the largest
+ * finite one); for f32 they are carried in 24 bits. */
+int slz_linear_i4_grad_workspace(const slz_i4_shape *shape, const void *dy_dev, const void *x_dev, size_t *bytes);
+int slz_linear_i4_grad(const slz_i4_shape *shape, const void *dy_dev, const void *x_dev, const uint8_t *q_dev, const float *scale_dev, void *dx_dev,
+                       int64_t ld_dx, void *dw_dev, int64_t ld_dw, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
 /* ---- softmax cross entropy of a linear layer --------------------------------------------------------------------------------- */
 typedef struct {
     uint32_t tokens, inner, vocab;       /* h is tokens x inner, w is vocab x inner; inner and vocab at least 1 */
@@ -115,6 +153,25 @@ typedef struct {
 int slz_orthogonalize_workspace(const slz_orth_shape *shape, size_t *bytes);
 int slz_orthogonalize(const slz_orth_shape *shape, const void *g_dev, void *out_dev, void *workspace_dev, size_t workspace_bytes,
                       void *hip_stream);
+
+/* ---- gradients clipped by their norm -------------------------------------------------------------------------------------------- */
+typedef struct {
+    const void *g;                       /* a gradient [rows][cols] on the device */
+    void *out;                           /* [rows][cols] of the same type; the same place as g (with the same leading dimension) or one that overlaps no gradient */
+    uint32_t rows, cols;
+    int64_t ld_g, ld_out;                /* any distance; where it is cols the rows are one run of elements */
+    int type;
+} slz_grad_tensor;
+
+/* norm = root of the sum of the squares of all elements of all `count` tensors (an array on the host), squared and summed in 64 bits and
+ * rounded to 32-bit floating point.  0 without elements; out, ld_out are not looked at. */
+int slz_clip_workspace(const slz_grad_tensor *tensors, uint32_t count, size_t *bytes);
+int slz_grad_norm(const slz_grad_tensor *tensors, uint32_t count, float *norm_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+/* out = g f in 32 bits, rounded to the type, with f = 1 where norm + eps <= max_norm, else max_norm / (norm + eps) (in 64 bits, rounded to 32), and NaN where norm is NaN.  The norm is computed as by
+ * slz_grad_norm and left in norm_dev, or, with norm_given, taken from there (the norm of more gradients than these).  Where f is 1 the elements keep their bits.
+ * SLZ_E_INVALID_ARG also where max_norm or eps is negative or NaN, and where an output overlaps another one or another gradient. */
+int slz_clip_by_norm(const slz_grad_tensor *tensors, uint32_t count, float max_norm, float eps, int norm_given, float *norm_dev, void *workspace_dev,
+                     size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

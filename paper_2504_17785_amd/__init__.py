@@ -586,4 +586,4 @@ class Context:
         return out
 
 
-from .clear import quantize_i8, matmul_i8, linear_i8, matmul_i8_grad, linear_ce, linear_ce_grad, orthogonalize  # noqa: E402,F401
+from .clear import quantize_i8, matmul_i8, linear_i8, matmul_i8_grad, quantize_i4, values_i4, linear_i4, linear_i4_grad, linear_ce, linear_ce_grad, orthogonalize, grad_norm, clip_by_norm  # noqa: E402,F401

@@ -1,10 +1,11 @@
-"""Binding of include/silenzio_clear.h: products of 8-bit integers, softmax cross entropy of a linear layer, orthogonalised updates.
+"""Binding of include/silenzio_clear.h: products of 8-bit integers, layers with 4-bit weights, softmax cross entropy of a linear layer,
+orthogonalised updates, gradients clipped by their norm.
 
 As in the rest of the binding the functions check their arguments, hand pointers and the current stream to the library and return at once.
 Matrices are CUDA tensors on the current device with unit stride along their rows (any distance between rows).  Workspaces
 come from torch's allocator on the current stream, so that their memory is not given away before the call's work on it is done.
 
-The gradients are functions of their own (matmul_i8_grad, linear_ce_grad) and autograd does not know them: results of tensors that require
+The gradients are functions of their own (matmul_i8_grad, linear_i4_grad, linear_ce_grad) and autograd does not know them: results of tensors that require
 a gradient raise an error when a backward pass comes to them."""
 from __future__ import annotations
 
@@ -30,6 +31,18 @@ class SlzCeShape(ctypes.Structure):
                 ("ignore_index", ctypes.c_int64)]
 
 
+class SlzI4Shape(ctypes.Structure):
+    """slz_i4_shape of include/silenzio_clear.h."""
+    _fields_ = [("m", ctypes.c_uint32), ("n", ctypes.c_uint32), ("k", ctypes.c_uint32), ("type", ctypes.c_int), ("group", ctypes.c_uint32),
+                ("ld_x", ctypes.c_int64), ("ld_q", ctypes.c_int64), ("ld_scale", ctypes.c_int64), ("ld_y", ctypes.c_int64)]
+
+
+class SlzGradTensor(ctypes.Structure):
+    """slz_grad_tensor of include/silenzio_clear.h."""
+    _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_uint32), ("cols", ctypes.c_uint32),
+                ("ld_g", ctypes.c_int64), ("ld_out", ctypes.c_int64), ("type", ctypes.c_int)]
+
+
 class SlzOrthShape(ctypes.Structure):
     """slz_orth_shape of include/silenzio_clear.h."""
     _fields_ = [("batch", ctypes.c_uint32), ("rows", ctypes.c_uint32), ("cols", ctypes.c_uint32), ("type", ctypes.c_int),
@@ -38,7 +51,7 @@ class SlzOrthShape(ctypes.Structure):
 
 
 def declare(L):
-    vp, u32, sz, i64, i = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_size_t, ctypes.c_int64, ctypes.c_int
+    vp, u32, sz, i64, i, f = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_size_t, ctypes.c_int64, ctypes.c_int, ctypes.c_float
     size = ctypes.POINTER(sz)
     i8, ce, orth = ctypes.POINTER(SlzI8Shape), ctypes.POINTER(SlzCeShape), ctypes.POINTER(SlzOrthShape)
     L.slz_quantize_i8.argtypes = [vp, i, u32, u32, i64, vp, i64, vp, vp]
@@ -48,12 +61,22 @@ def declare(L):
     L.slz_linear_i8.argtypes = [i8, vp, vp, vp, vp, vp, sz, vp]
     L.slz_matmul_i8_grad_workspace.argtypes = [i8, vp, size]
     L.slz_matmul_i8_grad.argtypes = [i8, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, sz, vp]
+    i4 = ctypes.POINTER(SlzI4Shape)
+    L.slz_quantize_i4.argtypes = [vp, i, u32, u32, i64, u32, vp, i64, vp, i64, vp]
+    L.slz_values_i4.argtypes = [vp, i64, vp, i64, u32, u32, u32, vp, i, i64, vp]
+    L.slz_linear_i4_workspace.argtypes = [i4, vp, size]
+    L.slz_linear_i4.argtypes = [i4, vp, vp, vp, vp, vp, sz, vp]
+    L.slz_linear_i4_grad_workspace.argtypes = [i4, vp, vp, size]
+    L.slz_linear_i4_grad.argtypes = [i4, vp, vp, vp, vp, vp, i64, vp, i64, vp, sz, vp]
     L.slz_linear_ce_workspace.argtypes = [ce, vp, vp, size]
     L.slz_linear_ce.argtypes = [ce, vp, vp, vp, vp, vp, vp, sz, vp]
     L.slz_linear_ce_grad_workspace.argtypes = [ce, vp, vp, size]
     L.slz_linear_ce_grad.argtypes = [ce, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.slz_orthogonalize_workspace.argtypes = [orth, size]
     L.slz_orthogonalize.argtypes = [orth, vp, vp, vp, sz, vp]
+    L.slz_clip_workspace.argtypes = [vp, u32, size]
+    L.slz_grad_norm.argtypes = [vp, u32, vp, vp, sz, vp]
+    L.slz_clip_by_norm.argtypes = [vp, u32, f, f, i, vp, vp, sz, vp]
 
 
 @functools.lru_cache(maxsize=None)
@@ -130,7 +153,7 @@ class _NoFormula(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *_):
-        raise RuntimeError("%s: autograd has no formula for it; call it on detached tensors, and matmul_i8_grad or linear_ce_grad for gradients" % ctx.where)
+        raise RuntimeError("%s: autograd has no formula for it; call it on detached tensors, and matmul_i8_grad, linear_i4_grad or linear_ce_grad for gradients" % ctx.where)
 
 
 def _results(where: str, inputs, *out):
@@ -206,6 +229,76 @@ def matmul_i8_grad(dy, a, a_scale, b, b_scale, need_a: bool = True, need_b: bool
     return _results("matmul_i8_grad", (dy, a_scale, b_scale), da, db)
 
 
+def _rows_i4(q, scale, rows, cols, group, like):
+    """Checks 4-bit rows and their scales; their row distances."""
+    if group not in (32, 64, 128):
+        raise ValueError("group: %s, need 32, 64 or 128" % (group,))
+    ld_q = _matrix(q, "q", (torch.uint8,), like, rows, (cols + 127) // 128 * 64)
+    return ld_q, _matrix(scale, "scale", (torch.float32,), q, q.shape[0], (cols + group - 1) // group)
+
+
+def quantize_i4(w, group: int = 128):
+    """slz_quantize_i4: w [rows][cols] -> (4-bit rows, uint8 [rows][64 for every 128 columns], scale float32 [rows][one for every `group` columns])."""
+    ld = _matrix(w, "w", _TYPES)
+    rows, cols = w.shape
+    if group not in (32, 64, 128):
+        raise ValueError("group: %s, need 32, 64 or 128" % (group,))
+    stream = _stream(w)
+    q = torch.empty((rows, (cols + 127) // 128 * 64), dtype=torch.uint8, device=w.device)
+    scale = torch.empty((rows, (cols + group - 1) // group), dtype=torch.float32, device=w.device)
+    _check(_lib().slz_quantize_i4(w.data_ptr(), _TYPES[w.dtype], rows, cols, ld, group, q.data_ptr(), q.shape[1], scale.data_ptr(), scale.shape[1], stream),
+           "slz_quantize_i4")
+    return _results("quantize_i4", (w,), q, scale)
+
+
+def values_i4(q, scale, cols: int, group: int = 128, dtype=torch.bfloat16):
+    """slz_values_i4: 4-bit rows of `cols` entries and their scales -> the values [rows][cols] of `dtype`."""
+    if dtype not in _TYPES:
+        raise TypeError("dtype: need float32, bfloat16 or float16, got %s" % dtype)
+    if not 0 <= cols <= 0x7fffffff:
+        raise ValueError("cols: %d" % cols)
+    ld_q, ld_scale = _rows_i4(q, scale, None, cols, group, None)
+    stream = _stream(q)
+    out = torch.empty((q.shape[0], cols), dtype=dtype, device=q.device)
+    _check(_lib().slz_values_i4(q.data_ptr(), ld_q, scale.data_ptr(), ld_scale, group, q.shape[0], cols, out.data_ptr(), _TYPES[dtype], max(cols, 1), stream),
+           "slz_values_i4")
+    return _results("values_i4", (scale,), out)
+
+
+def linear_i4(x, q, scale, group: int = 128):
+    """slz_linear_i4: x [m][k] times the values of 4-bit rows q [n] with their scales -> y [m][n] of x's type."""
+    ld_x = _matrix(x, "x", _TYPES)
+    m, k = x.shape
+    ld_q, ld_scale = _rows_i4(q, scale, None, k, group, x)
+    n = q.shape[0]
+    stream = _stream(x)
+    y = torch.empty((m, n), dtype=x.dtype, device=x.device)
+    sh = SlzI4Shape(m, n, k, _TYPES[x.dtype], group, ld_x, ld_q, ld_scale, max(n, 1))
+    L = _lib()
+    ws, at, need = _workspace(L.slz_linear_i4_workspace, "slz_linear_i4", x, ctypes.byref(sh), x.data_ptr())
+    _check(L.slz_linear_i4(ctypes.byref(sh), x.data_ptr(), q.data_ptr(), scale.data_ptr(), y.data_ptr(), at, need, stream), "slz_linear_i4")
+    return _results("linear_i4", (x, scale), y)
+
+
+def linear_i4_grad(dy, x, q, scale, group: int = 128, need_x: bool = True, need_w: bool = True):
+    """slz_linear_i4_grad: dy [m][n] and what linear_i4 was called with -> (gradient of x [m][k], of the weights' values [n][k]), of dy's type; None for one
+    that is not needed."""
+    ld_y = _matrix(dy, "dy", _TYPES)
+    m, n = dy.shape
+    ld_x = _matrix(x, "x", (dy.dtype,), dy, m)
+    k = x.shape[1]
+    ld_q, ld_scale = _rows_i4(q, scale, n, k, group, dy)
+    stream = _stream(dy)
+    dx = torch.empty((m, k), dtype=dy.dtype, device=dy.device) if need_x else None
+    dw = torch.empty((n, k), dtype=dy.dtype, device=dy.device) if need_w else None
+    sh = SlzI4Shape(m, n, k, _TYPES[dy.dtype], group, ld_x, ld_q, ld_scale, ld_y)
+    L = _lib()
+    ws, at, need = _workspace(L.slz_linear_i4_grad_workspace, "slz_linear_i4_grad", dy, ctypes.byref(sh), dy.data_ptr(), x.data_ptr())
+    _check(L.slz_linear_i4_grad(ctypes.byref(sh), dy.data_ptr(), x.data_ptr(), q.data_ptr(), scale.data_ptr(), dx.data_ptr() if need_x else None, max(k, 1),
+                                dw.data_ptr() if need_w else None, max(k, 1), at, need, stream), "slz_linear_i4_grad")
+    return _results("linear_i4_grad", (dy, x, scale), dx, dw)
+
+
 def _ce_shape(h, w, labels, ignore_index):
     ld_h = _matrix(h, "h", _TYPES)
     tokens, inner = h.shape
@@ -261,3 +354,79 @@ def orthogonalize(g, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
     ws, at, need = _workspace(L.slz_orthogonalize_workspace, "slz_orthogonalize", g, ctypes.byref(sh))
     _check(L.slz_orthogonalize(ctypes.byref(sh), g.data_ptr(), out.data_ptr(), at, need, stream), "slz_orthogonalize")
     return _results("orthogonalize", (g,), out)
+
+
+def _grad_place(t, what: str, device: int):
+    """(rows, cols, row distance) of a tensor of any shape whose elements are one run, or of a matrix."""
+    if t.dtype not in _TYPES or t.get_device() != device:
+        raise TypeError("%s: need a CUDA tensor of float32, bfloat16 or float16 on device %d, got %s on %s" % (what, device, t.dtype, t.device))
+    if t.is_contiguous():
+        n = t.numel()
+        if n <= 0x7fffffff:
+            return 1, n, n
+        cols = t.shape[-1]
+        _check(_E_TOO_LARGE if max(cols, n // cols) > 0x7fffffff else 0, "%s: shape %s" % (what, tuple(t.shape)))
+        return n // cols, cols, cols
+    if t.dim() != 2:
+        raise ValueError("%s: need a contiguous tensor, or a matrix with unit stride along its rows; got strides %s" % (what, t.stride()))
+    return (*t.shape, _matrix(t, what, _TYPES))
+
+
+def _grad_table(grads, out, device: int):
+    flat = []
+    for i, g in enumerate(grads):
+        rows, cols, ld = _grad_place(g, "gradient %d" % i, device)
+        if out is None:
+            flat += (g.data_ptr(), 0, rows | cols << 32, ld, ld, _TYPES[g.dtype])
+            continue
+        o = out[i]
+        if o is g:
+            ld_o = ld
+        else:
+            if o.dtype != g.dtype or o.shape != g.shape:
+                raise ValueError("output %d: need %s %s, got %s %s" % (i, g.dtype, tuple(g.shape), o.dtype, tuple(o.shape)))
+            rows_o, cols_o, ld_o = _grad_place(o, "output %d" % i, device)
+            if (rows, cols) != (rows_o, cols_o):               # one of them is a run, the other is not
+                rows, cols = g.shape
+                ld, ld_o = _matrix(g, "gradient %d" % i, _TYPES), _matrix(o, "output %d" % i, _TYPES)
+        flat += (g.data_ptr(), o.data_ptr(), rows | cols << 32, ld, ld_o, _TYPES[g.dtype])
+    return (ctypes.c_uint64 * len(flat))(*flat)                # a slz_grad_tensor is six of 64 bits
+
+
+def _clip_norm(grads, norm):
+    """The list of gradients, and where their norm is to be or is."""
+    grads = list(grads)
+    device = torch._C._cuda_getDevice()
+    if norm is None:
+        return grads, torch.empty((), dtype=torch.float32, device="cuda:%d" % device), device
+    if norm.dtype != torch.float32 or norm.get_device() != device or norm.numel() != 1:
+        raise TypeError("norm: need one float32 on device %d" % device)
+    return grads, norm, device
+
+
+def grad_norm(grads):
+    """slz_grad_norm: the norm that all tensors of a list have together, a float32 scalar tensor."""
+    grads, norm, device = _clip_norm(grads, None)
+    table, L = _grad_table(grads, None, device), _lib()
+    ws, at, need = _workspace(L.slz_clip_workspace, "slz_clip", norm, table, len(grads))
+    _check(L.slz_grad_norm(table, len(grads), norm.data_ptr(), at, need, torch._C._cuda_getCurrentRawStream(device)), "slz_grad_norm")
+    return _results("grad_norm", grads, norm) if grads else norm
+
+
+def clip_by_norm(grads, max_norm: float, eps: float = 1e-6, norm=None, out=None):
+    """slz_clip_by_norm: all tensors of a list times max_norm / (their common norm + eps) where that is below 1, in place or into the tensors of `out`.  The norm, a float32
+    scalar tensor, is returned; one that is given is taken in its place (of gradients that are spread over several devices)."""
+    grads, at_norm, device = _clip_norm(grads, norm)
+    out = grads if out is None else list(out)
+    if len(out) != len(grads):
+        raise ValueError("out: %d tensors for %d gradients" % (len(out), len(grads)))
+    if torch.is_grad_enabled():
+        for t in (*grads, *out):
+            if t.requires_grad:
+                raise RuntimeError("clip_by_norm: autograd has no formula for it; call it on detached tensors or under torch.no_grad()")
+    table, L = _grad_table(grads, out, device), _lib()
+    ws, at, need = _workspace(L.slz_clip_workspace, "slz_clip", at_norm, table, len(grads))
+    _check(L.slz_clip_by_norm(table, len(grads), max_norm, eps, norm is not None, at_norm.data_ptr(), at, need, torch._C._cuda_getCurrentRawStream(device)),
+           "slz_clip_by_norm")
+    torch.autograd.graph.increment_version([t for t in out if not t.is_inference()])
+    return at_norm

@@ -350,6 +350,10 @@ using slz_tiles_192 = slz_tiling<192, 192, 2, 4>;
 using slz_tiles_128 = slz_tiling<128, 128, 2, 2>;
 using slz_tiles_64 = slz_tiling<64, 64, 2, 2>;
 
+// out [M][N] = left right, the sums times *unit by where a unit is given; right's rows are the sum's index, and left's where left_rows_k (slz_i8.hip)
+int slz_float_product(const slz_operand &left, bool left_rows_k, const slz_operand &right, uint32_t M, uint32_t N, uint32_t K, const slz_choice &c, const float *unit, float by,
+                      void *out, int type, int64_t ld_out, char *ranges, hipStream_t s);
+
 // workspace of the ranges' sums
 static inline uint32_t slz_ranges_ld(uint32_t N) { return (N + 15u) & ~15u; }
 static inline size_t slz_ranges_bytes(const slz_choice &c, uint32_t M, uint32_t N) { return c.split > 1 ? up256((size_t)c.split * M * slz_ranges_ld(N) * 4) : 0; }

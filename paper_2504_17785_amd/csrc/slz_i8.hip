@@ -412,6 +412,15 @@ extern "C" int slz_linear_i8(const slz_i8_shape *sh, const void *x, const int8_t
     return i8_product(sh, oa, sa, ob, sb, y, (char *)ws + P.ranges, s);
 }
 
+int slz_float_product(const slz_operand &left, bool left_rows_k, const slz_operand &right, uint32_t M, uint32_t N, uint32_t K, const slz_choice &c, const float *unit, float by,
+                      void *out, int type, int64_t ld_out, char *ranges, hipStream_t s) {
+    const slz_gemm p = slz_gemm_of(left, right, M, N, K);
+    const slz_times_unit f{unit, by};
+    if (type == SLZ_F16)
+        return left_rows_k ? slz_gemm_to<SLZ_EL_F16, true, true>(p, c, f, out, type, ld_out, ranges, s) : slz_gemm_to<SLZ_EL_F16, false, true>(p, c, f, out, type, ld_out, ranges, s);
+    return left_rows_k ? slz_gemm_to<SLZ_EL_BF16, true, true>(p, c, f, out, type, ld_out, ranges, s) : slz_gemm_to<SLZ_EL_BF16, false, true>(p, c, f, out, type, ld_out, ranges, s);
+}
+
 // ---- gradient ------------------------------------------------------------------------------------------------------------------------------
 // dy times the values scale_r q_rc: these are laid out as an operand once (bf16, or three bf16 for f32), then two ordinary products.  The scale belongs to the
 // index that is summed over, so it has to be in one of the operands, and rounding it there takes bf16 results from 1.7e-3 off (their own rounding) to 2.4e-3 and
@@ -495,13 +504,8 @@ static int grad_product(const slz_i8_shape *sh, const slz_operand &left, bool le
         const auto k = type == SLZ_F32 ? k_values<SLZ_F32> : type == SLZ_BF16 ? k_values<SLZ_BF16> : k_values<SLZ_F16>;
         hipLaunchKernelGGL(k, ew_grid((size_t)rows * P.row / 16), dim3(256), 0, s, q, one ? nullptr : scale, unit, rows, sh->k, ld_q, values, P.row, right.piece);
     }
-    const slz_gemm p = slz_gemm_of(left, right, M, sh->k, rows);
-    const slz_times_unit f{one ? scale : with_unit ? unit : nullptr, one ? 1.0f : 1.0f / VALUES_F16_UP};
-    if (type == SLZ_F16)
-        return left_rows_k ? slz_gemm_to<SLZ_EL_F16, true, true>(p, P.db, f, out, type, ld_out, ranges, s)
-                           : slz_gemm_to<SLZ_EL_F16, false, true>(p, P.da, f, out, type, ld_out, ranges, s);
-    return left_rows_k ? slz_gemm_to<SLZ_EL_BF16, true, true>(p, P.db, f, out, type, ld_out, ranges, s)
-                       : slz_gemm_to<SLZ_EL_BF16, false, true>(p, P.da, f, out, type, ld_out, ranges, s);
+    return slz_float_product(left, left_rows_k, right, M, sh->k, rows, left_rows_k ? P.db : P.da, one ? scale : with_unit ? unit : nullptr, one ? 1.0f : 1.0f / VALUES_F16_UP, out,
+                             type, ld_out, ranges, s);
 }
 
 extern "C" int slz_matmul_i8_grad(const slz_i8_shape *sh, const void *dy, const int8_t *a, const float *sa, const int8_t *b, const float *sb, void *da,
