@@ -5,7 +5,7 @@
 #include "slz_gemm.h"
 
 #define I4_BLOCK 128u                // entries of a block, 64 bytes
-static inline uint32_t i4_blocks(uint32_t cols) { return (cols + I4_BLOCK - 1) / I4_BLOCK; }
+__host__ __device__ static inline uint32_t i4_blocks(uint32_t cols) { return (cols + I4_BLOCK - 1) / I4_BLOCK; }
 static inline uint32_t i4_groups(uint32_t cols, uint32_t group) { return (cols + group - 1) / group; }
 
 // entries e of a word, in the order of k: a sign and a magnitude
@@ -129,6 +129,394 @@ extern "C" int slz_values_i4(const uint8_t *q, int64_t ld_q, const float *scale,
     return SLZ_OK;
 }
 
+// ---- few rows ------------------------------------------------------------------------------------------------------------------------
+// The entries of a word as eight numbers of a matrix operand, exact.  A number's high byte and, in bf16, its low byte depend on the three bits of the
+// magnitude: each is looked up for four entries at once by a byte permutation of the table 0 .. 7, whose selectors are the entries themselves.
+template <int EL> __device__ __forceinline__ v4i32 i4_operand(uint32_t word) {
+    constexpr uint32_t HI03 = EL == SLZ_EL_BF16 ? 0x40403f00u : 0x42403c00u, HI47 = EL == SLZ_EL_BF16 ? 0x40404040u : 0x47464544u;
+    constexpr uint32_t LO03 = 0x40008000u, LO47 = 0xe0c0a080u;                     // bf16: 0, 3f80, 4000, 4040, 4080, 40a0, 40c0, 40e0; f16: low bytes are 0
+    v4i32 o;
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        const uint32_t w = h ? word >> 4 : word, at = w & 0x07070707u;
+        const uint32_t hi = __builtin_amdgcn_perm(HI47, HI03, at) | (w & 0x08080808u) << 4;
+        if constexpr (EL == SLZ_EL_BF16) {
+            const uint32_t lo = __builtin_amdgcn_perm(LO47, LO03, at);
+            o[2 * h] = (int)__builtin_amdgcn_perm(hi, lo, 0x05010400u);
+            o[2 * h + 1] = (int)__builtin_amdgcn_perm(hi, lo, 0x07030602u);
+        } else {
+            o[2 * h] = (int)__builtin_amdgcn_perm(hi, 0u, 0x050c040cu);
+            o[2 * h + 1] = (int)__builtin_amdgcn_perm(hi, 0u, 0x070c060cu);
+        }
+    }
+    return o;
+}
+
+// What follows streams the weights past the matrix instructions with the entries as whole numbers; what a group sums up to in 32 bits is multiplied by its scale, so that no value is
+// rounded.  x is laid out in shared memory as operands, rows I4_PITCH bytes for 128 entries or one row's length, 16 bytes apart in the banks.
+struct i4_args {
+    const char *x, *q;
+    const float *scale;
+    char *y;
+    int64_t ld_x, ld_q, ld_scale, ld_y;                // of q in bytes
+    uint32_t M, N, K, group;
+};
+template <int TYPE> constexpr int i4_pieces = TYPE == SLZ_F32 ? 3 : 1;
+// Eight entries of a row of x at c as operands, zeros past its end: one, or three that 32-bit numbers are cut into, the large ones first
+template <int TYPE> __device__ __forceinline__ void i4_octet(const row8<TYPE> &q, uint32_t c, uint32_t cols, v4i32 (&o)[i4_pieces<TYPE>]) {
+    if constexpr (TYPE != SLZ_F32)
+        if (c + 8u <= cols) {
+            o[0] = q.w[0];
+            return;
+        }
+    float v[8];
+    row8_values<TYPE>(q, c, cols, v);
+    if constexpr (TYPE == SLZ_F32) {
+        uint16_t t[8][3];
+#pragma unroll
+        for (int i = 0; i < 8; i++) slz_split3(v[i], t[i]);
+#pragma unroll
+        for (int k = 0; k < 3; k++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) o[k][i] = (int)(t[2 * i][k] | (uint32_t)t[2 * i + 1][k] << 16);
+    } else
+#pragma unroll
+        for (int i = 0; i < 4; i++) o[0][i] = (int)(slz_half(v[2 * i], TYPE) | (uint32_t)slz_half(v[2 * i + 1], TYPE) << 16);
+}
+// A wave's share of the weights: 16 NB rows, a block's entries at a time.  Rows of a workgroup begin at uniform addresses, lanes' places are below 2^32 from there.
+template <int NB> struct i4_stream {
+    const char *q0;
+    const float *scale0;
+    uint32_t at_q[NB], shift, groups;                  // a group has 2^shift entries
+    __device__ __forceinline__ void init(const i4_args &p, uint32_t first, uint32_t lane) {
+        const uint32_t n0 = min(first, p.N - 1);       // a wave without rows reads the last one
+        q0 = p.q + (int64_t)n0 * p.ld_q;
+        scale0 = p.scale + (int64_t)n0 * p.ld_scale;
+#pragma unroll
+        for (int j = 0; j < NB; j++) {
+            const uint32_t row = min(j * 16 + (lane & 15u), p.N - 1 - n0);
+            at_q[j] = row * (uint32_t)p.ld_q + (lane >> 4) * 16u;
+        }
+        shift = p.group == 32 ? 5u : p.group == 64 ? 6u : 7u;
+        groups = (p.K + p.group - 1) >> shift;
+    }
+    __device__ __forceinline__ void load(uint32_t block, v4i32 (&w)[NB]) const {
+#pragma unroll
+        for (int j = 0; j < NB; j++) w[j] = *(const v4i32 *)(q0 + (at_q[j] + block * 64u));
+    }
+};
+// Sums of a block's four steps: part collects a group, acc the groups times their scales.  read(step, i, o): x's operands
+template <int EL, int PIECES, int MI, int NB, class READ>
+__device__ __forceinline__ void i4_block(const v4i32 (&w)[NB], const v4f (&s)[NB], uint32_t shift, v4f (&part)[MI][NB], v4f (&acc)[MI][NB], const READ &read) {
+#pragma unroll
+    for (int step = 0; step < 4; step++) {
+        v4i32 b[NB];
+#pragma unroll
+        for (int j = 0; j < NB; j++) b[j] = i4_operand<EL>((uint32_t)w[j][step]);
+#pragma unroll
+        for (int i = 0; i < MI; i++) {
+            v4i32 o[PIECES];
+            read(step, i, o);
+#pragma unroll
+            for (int k = PIECES - 1; k >= 0; k--)
+#pragma unroll
+                for (int j = 0; j < NB; j++) part[i][j] = slz_mma<EL>(o[k], b[j], part[i][j]);
+        }
+        if (step == 3 || shift == 5u || (shift == 6u && step == 1))                // a group ends
+#pragma unroll
+            for (int j = 0; j < NB; j++) {
+                const float of_32 = s[j][step], of_64 = s[j][step / 2], of_128 = s[j][0], f = shift == 5u ? of_32 : shift == 6u ? of_64 : of_128;
+#pragma unroll
+                for (int i = 0; i < MI; i++) {
+#pragma unroll
+                    for (int e = 0; e < 4; e++) acc[i][j][e] = __builtin_fmaf(part[i][j][e], f, acc[i][j][e]);
+                    part[i][j] = v4f{0, 0, 0, 0};
+                }
+            }
+    }
+}
+
+// A few rows, all of x and of the scales that a workgroup needs in shared memory.  A workgroup of eight waves has 16 NB rows of weights, each wave an eighth of the blocks of k.
+// Loads return in order, so those of x and the scales go first, then the wave's first blocks, before anything is looked at; the eight waves' sums meet in shared memory.
+#define THIN_WAVES 8
+#define THIN_LDS (128u << 10)
+#define THIN_SLOTS 2                 // octets of x, and scales, that a thread has under way
+static inline __host__ __device__ uint32_t thin_pitch(uint32_t k) { return i4_blocks(k) * 256u + 16u; }
+static inline __host__ __device__ uint32_t thin_scales(uint32_t groups) { return (groups | 3u) + 2u; }         // floats of a row: odd, and up to three past its end are there
+template <int TYPE, int NB>
+__global__ void __launch_bounds__(THIN_WAVES * 64) k_thin_i4(const i4_args p) {
+    constexpr int EL = TYPE == SLZ_F16 ? SLZ_EL_F16 : SLZ_EL_BF16, PIECES = i4_pieces<TYPE>, AHEAD = 4;
+    constexpr uint32_t THREADS = THIN_WAVES * 64, ROWS = 16 * NB;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15u, g = lane >> 4;
+    const uint32_t n0 = blockIdx.x * ROWS, blocks = (p.K + I4_BLOCK - 1) / I4_BLOCK, pitch = thin_pitch(p.K);
+    const uint32_t begin = wave * blocks / THIN_WAVES, end = (wave + 1) * blocks / THIN_WAVES;
+    i4_stream<NB> q;
+    q.init(p, n0, lane);
+    const uint32_t octets = p.M * blocks * 16u, count = ROWS * q.groups, pitch_s = thin_scales(q.groups);
+    float *scales = (float *)(lds + PIECES * p.M * pitch);
+    row8<TYPE> x[THIN_SLOTS];
+    float sc[THIN_SLOTS];
+    const auto octet = [&](uint32_t i, uint32_t &m) {
+        m = p.M == 1 ? 0u : i / (blocks * 16u);
+        return (i - m * (blocks * 16u)) * 8u;
+    };
+    const auto load_scale = [&](uint32_t i) {
+        const uint32_t row = i / q.groups;
+        return q.scale0[(size_t)min(row, p.N - 1 - n0) * p.ld_scale + i - row * q.groups];
+    };
+#pragma unroll
+    for (uint32_t t = 0; t < THIN_SLOTS; t++) {
+        const uint32_t i = threadIdx.x + t * THREADS;
+        uint32_t m;
+        const uint32_t c = octet(i, m);
+        if (i < octets) x[t] = row8_load<TYPE>(p.x, (size_t)m * p.ld_x, c, p.K);
+        if (i < count) sc[t] = load_scale(i);
+    }
+    v4i32 w[AHEAD][NB];
+    if (begin < end)
+#pragma unroll
+        for (int d = 0; d < AHEAD; d++) q.load(min(begin + d, end - 1), w[d]);
+    __builtin_amdgcn_sched_barrier(0);
+    const auto put_x = [&](uint32_t i, const row8<TYPE> &v) {
+        uint32_t m;
+        const uint32_t c = octet(i, m);
+        v4i32 o[PIECES];
+        i4_octet<TYPE>(v, c, p.K, o);
+#pragma unroll
+        for (int k = 0; k < PIECES; k++) *(v4i32 *)(lds + (k * p.M + m) * pitch + c * 2u) = o[k];
+    };
+#pragma unroll
+    for (uint32_t t = 0; t < THIN_SLOTS; t++) {
+        const uint32_t i = threadIdx.x + t * THREADS;
+        if (i < octets) put_x(i, x[t]);
+        if (i < count) scales[i / q.groups * pitch_s + i % q.groups] = sc[t];
+    }
+    for (uint32_t i = threadIdx.x + THIN_SLOTS * THREADS; i < octets; i += THREADS) {
+        uint32_t m;
+        const uint32_t c = octet(i, m);
+        put_x(i, row8_load<TYPE>(p.x, (size_t)m * p.ld_x, c, p.K));
+    }
+    for (uint32_t i = threadIdx.x + THIN_SLOTS * THREADS; i < count; i += THREADS) scales[i / q.groups * pitch_s + i % q.groups] = load_scale(i);
+    if (threadIdx.x < ROWS)                            // groups past the rows' ends
+        for (uint32_t c = q.groups; c < pitch_s; c++) scales[threadIdx.x * pitch_s + c] = 0.0f;
+    __syncthreads();
+    const char *from = lds + min(r, p.M - 1) * pitch + g * 16u;
+    const uint32_t piece = p.M * pitch;
+    v4f acc[1][NB], part[1][NB];
+#pragma unroll
+    for (int j = 0; j < NB; j++) acc[0][j] = part[0][j] = v4f{0, 0, 0, 0};
+    for (uint32_t b0 = begin; b0 < end; b0 += AHEAD)
+#pragma unroll
+        for (int d = 0; d < AHEAD; d++) {
+            const uint32_t block = b0 + d;
+            if (block >= end) break;
+            v4f s[NB];
+#pragma unroll
+            for (int j = 0; j < NB; j++) {
+                const float *at = scales + (j * 16 + r) * pitch_s + (block << (7u - q.shift));
+                if (q.shift == 7u) s[j] = v4f{at[0], 0, 0, 0};
+                else if (q.shift == 6u) s[j] = v4f{at[0], at[1], 0, 0};
+                else s[j] = v4f{at[0], at[1], at[2], at[3]};
+            }
+            i4_block<EL, PIECES>(w[d], s, q.shift, part, acc, [&](int step, int, v4i32 (&o)[PIECES]) {
+#pragma unroll
+                for (int k = 0; k < PIECES; k++) o[k] = *(const v4i32 *)(from + k * piece + block * 256u + step * 64u);
+            });
+            if (block + AHEAD < end) q.load(block + AHEAD, w[d]);
+        }
+    __syncthreads();
+    float *sums = (float *)lds;                        // [wave][row of x][row of weights]
+#pragma unroll
+    for (int j = 0; j < NB; j++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) sums[(wave * 16u + g * 4u + e) * ROWS + j * 16 + r] = acc[0][j][e];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < p.M * ROWS; i += THREADS) {
+        const uint32_t m = i / ROWS, n = n0 + i % ROWS;
+        if (n >= p.N) continue;
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < THIN_WAVES; k++) sum += sums[k * (16 * ROWS) + i];
+        slz_put(p.y, TYPE, (size_t)m * p.ld_y + n, sum);
+    }
+}
+
+// More rows: a workgroup has 16 MI rows of x and 32 WN of weights.  Its waves are WN by WK: in each phase WK blocks of k of x come to shared memory, on the way through registers
+// while the phase before is computed, and a wave multiplies one of them by its 32 rows of weights.  The WK waves' sums meet in shared memory at the end.
+template <int TYPE, int MI, int WN, int WK, int BUFFERS>
+__global__ void __launch_bounds__(WN *WK * 64) k_rows_i4(const i4_args p, uint32_t tiles_m, uint32_t tiles_n) {
+    constexpr int EL = TYPE == SLZ_F16 ? SLZ_EL_F16 : SLZ_EL_BF16, PIECES = i4_pieces<TYPE>, XB = TYPE == SLZ_F32 ? 4 : 2, NB = 2, AHEAD = 4, THREADS = WN * WK * 64;
+    constexpr uint32_t TM = MI * 16, TN = WN * NB * 16, PITCH = 272, PIECE = TM * PITCH, BLOCK = PIECES * PIECE, BUFFER = WK * BLOCK;
+    constexpr int OCTETS = WK * TM * 16 / THREADS;
+    static_assert(OCTETS * THREADS == WK * TM * 16, "");
+    constexpr uint32_t SUMS = WK * TM * TN * 4, LDS = BUFFERS * BUFFER > SUMS ? BUFFERS * BUFFER : SUMS;
+    constexpr int SCALES = (TN * WK * 4 + THREADS - 1) / THREADS;
+    __shared__ __attribute__((aligned(16))) char lds[LDS];
+    __shared__ float scales[2][WK * 4][TN + 4];         // [group of the phase][row of weights]
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15u, g = lane >> 4;
+    const uint32_t wn = wave % WN, wk = wave / WN;
+    // the tiles of x that meet one tile of weights follow each other on one XCD
+    const uint32_t eights = blockIdx.x / (8u * tiles_m), in = blockIdx.x % (8u * tiles_m), left = min(8u, tiles_n - eights * 8u);
+    const uint32_t n0 = (eights * 8u + in % left) * TN, m0 = in / left * TM;
+    const uint32_t blocks = (p.K + I4_BLOCK - 1) / I4_BLOCK, phases = (blocks + WK - 1) / WK;
+    // workgroups begin at different phases: where all read the same columns of x and of rows a power of two apart, a few memory channels have all the work
+    const uint32_t turn = n0 / TN % phases;
+    const auto phase_of = [&](uint32_t i) { return i + turn < phases ? i + turn : i + turn - phases; };
+    i4_stream<NB> q;
+    q.init(p, n0 + wn * (NB * 16), lane);
+    v4i32 w[AHEAD][NB];
+#pragma unroll
+    for (int d = 0; d < AHEAD; d++)
+        if (d < phases) q.load(min(phase_of(d) * WK + wk, blocks - 1), w[d]);
+    // this thread's scales of a phase: rows of weights and groups, 0 past the rows' ends
+    const uint32_t per_block = 7u - q.shift;
+    const float *scale0 = p.scale + (int64_t)n0 * p.ld_scale;
+    float sc[SCALES];
+    const auto group_of = [&](uint32_t phase, uint32_t i, uint32_t &row) {
+        row = i >> (per_block + (WK == 8 ? 3 : 2));
+        return (phase * WK << per_block) + (i & ((WK << per_block) - 1u));
+    };
+    const auto load_scales = [&](uint32_t number) {
+#pragma unroll
+        for (int t = 0; t < SCALES; t++) {
+            uint32_t row;
+            const uint32_t c = group_of(phase_of(number), threadIdx.x + t * THREADS, row);
+            sc[t] = scale0[min(row, p.N - 1 - n0) * (uint32_t)p.ld_scale + min(c, q.groups - 1)];
+        }
+    };
+    const auto store_scales = [&](uint32_t number) {
+#pragma unroll
+        for (int t = 0; t < SCALES; t++) {
+            uint32_t row;
+            const uint32_t i = threadIdx.x + t * THREADS, c = group_of(phase_of(number), i, row);
+            if (row < TN) scales[number & 1u][i & ((WK << per_block) - 1u)][row] = c < q.groups ? sc[t] : 0.0f;
+        }
+    };
+
+    // this thread's octets of x in a phase: column and row (the last one again where there are fewer, for sums that no one stores)
+    const uint32_t last = p.M - 1 - m0;
+    const char *x0 = p.x + (int64_t)m0 * p.ld_x * XB;
+    row8<TYPE> x[OCTETS];
+    const auto column = [&](uint32_t phase, int i) { return (phase * WK + (threadIdx.x + i * THREADS) / (TM * 16)) * I4_BLOCK + threadIdx.x % 16u * 8u; };
+    const auto row = [&](int i) { return (threadIdx.x + i * THREADS) / 16u % TM; };
+    const auto load_x = [&](uint32_t number) {
+        const uint32_t phase = phase_of(number);
+#pragma unroll
+        for (int i = 0; i < OCTETS; i++) {
+            // where the row ends inside, its last eight; i4_octet moves them down
+            const v4i32_any *at = (const v4i32_any *)(x0 + (size_t)((min(row(i), last) * (uint32_t)p.ld_x + min(column(phase, i), p.K - 8u)) * XB));
+            x[i].w[0] = at[0];
+            if constexpr (TYPE == SLZ_F32) x[i].w[1] = at[1];
+        }
+    };
+    const auto store_x = [&](uint32_t number) {
+        const uint32_t phase = phase_of(number);
+#pragma unroll
+        for (int i = 0; i < OCTETS; i++) {
+            v4i32 o[PIECES];
+            i4_octet<TYPE>(x[i], column(phase, i), p.K, o);
+            char *to = lds + (BUFFERS == 2 ? number & 1u : 0u) * BUFFER + (threadIdx.x + i * THREADS) / (TM * 16) * BLOCK + row(i) * PITCH + threadIdx.x % 16u * 16u;
+#pragma unroll
+            for (int k = 0; k < PIECES; k++) *(v4i32 *)(to + k * PIECE) = o[k];
+        }
+    };
+    v4f acc[MI][NB], part[MI][NB];
+#pragma unroll
+    for (int i = 0; i < MI; i++)
+#pragma unroll
+        for (int j = 0; j < NB; j++) acc[i][j] = part[i][j] = v4f{0, 0, 0, 0};
+    load_x(0);
+    load_scales(0);
+    store_x(0);
+    store_scales(0);
+    if (phases > 1) {
+        load_x(1);
+        load_scales(1);
+    }
+    __syncthreads();
+    for (uint32_t p0 = 0; p0 < phases; p0 += AHEAD)
+#pragma unroll
+        for (int d = 0; d < AHEAD; d++) {
+            const uint32_t phase = p0 + d;
+            if (phase >= phases) break;
+            if (phase + 1 < phases) {
+                store_scales(phase + 1);
+                if (phase + 2 < phases) load_scales(phase + 2);
+            }
+            if (BUFFERS == 2 && phase + 1 < phases) {
+                store_x(phase + 1);
+                if (phase + 2 < phases) load_x(phase + 2);
+            }
+            const char *from = lds + (BUFFERS == 2 ? phase & 1u : 0u) * BUFFER + wk * BLOCK + r * PITCH + g * 16u;
+            v4f s[NB];
+#pragma unroll
+            for (int j = 0; j < NB; j++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) s[j][e] = scales[phase & 1u][(wk << per_block) + (e & ((1u << per_block) - 1u))][(wn * NB + j) * 16 + r];
+            if (phase_of(phase) * WK + wk < blocks)
+                i4_block<EL, PIECES>(w[d], s, q.shift, part, acc, [&](int step, int i, v4i32 (&o)[PIECES]) {
+#pragma unroll
+                    for (int k = 0; k < PIECES; k++) o[k] = *(const v4i32 *)(from + k * PIECE + i * (16 * PITCH) + step * 64);
+                });
+            if (phase + AHEAD < phases) q.load(min(phase_of(phase + AHEAD) * WK + wk, blocks - 1), w[d]);
+            __syncthreads();
+            if (BUFFERS == 1 && phase + 1 < phases) {
+                store_x(phase + 1);
+                if (phase + 2 < phases) load_x(phase + 2);
+                __syncthreads();
+            }
+        }
+    float *sums = (float *)lds;                        // [wk][row of x][row of weights]
+#pragma unroll
+    for (int i = 0; i < MI; i++)
+#pragma unroll
+        for (int j = 0; j < NB; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) sums[(wk * TM + i * 16 + g * 4 + e) * TN + (wn * NB + j) * 16 + r] = acc[i][j][e];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < TM * TN; i += THREADS) {
+        const uint32_t m = m0 + i / TN, n = n0 + i % TN;
+        if (m >= p.M || n >= p.N) continue;
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < WK; k++) sum += sums[k * (TM * TN) + i];
+        slz_put(p.y, TYPE, (size_t)m * p.ld_y + n, sum);
+    }
+}
+
+static size_t thin_bytes(uint32_t m, uint32_t k, uint32_t group, int type, uint32_t nb) {
+    return (size_t)m * thin_pitch(k) * (type == SLZ_F32 ? 3 : 1) + (size_t)thin_scales(i4_groups(k, group)) * 64 * nb;
+}
+static bool thin_takes(const slz_i4_shape *sh) { return sh->m <= 8 && thin_bytes(sh->m, sh->k, sh->group, sh->type, 2) <= THIN_LDS; }
+static bool rows_takes(const slz_i4_shape *sh) { return sh->m <= 256 && sh->k >= 8; }
+template <int TYPE, int NB> static void thin_launch(const i4_args &p, hipStream_t s) {
+    const size_t x = thin_bytes(p.M, p.K, p.group, TYPE, NB), sums = (size_t)THIN_WAVES * 16 * NB * 16 * 4;
+    hipLaunchKernelGGL((k_thin_i4<TYPE, NB>), dim3((p.N + 16 * NB - 1) / (16 * NB)), dim3(THIN_WAVES * 64), x > sums ? x : sums, s, p);
+}
+template <int TYPE, int MI, int WN, int WK, int BUFFERS> static void rows_launch(const i4_args &p, hipStream_t s) {
+    const uint32_t tiles_m = (p.M + MI * 16 - 1) / (MI * 16), tiles_n = (p.N + WN * 32 - 1) / (WN * 32);
+    hipLaunchKernelGGL((k_rows_i4<TYPE, MI, WN, WK, BUFFERS>), dim3(tiles_m * tiles_n), dim3(WN * WK * 64), 0, s, p, tiles_m, tiles_n);
+}
+template <int TYPE> static void few_rows(const i4_args &p, bool thin, hipStream_t s) {
+    if (thin) p.N <= 8192 ? thin_launch<TYPE, 1>(p, s) : thin_launch<TYPE, 2>(p, s);
+    else if constexpr (TYPE == SLZ_F32) p.M <= 16 ? rows_launch<TYPE, 1, 2, 4, 1>(p, s) : rows_launch<TYPE, 2, 2, 4, 1>(p, s);
+    else if (p.M <= 16) rows_launch<TYPE, 1, 1, 8, 2>(p, s);
+    else if (p.M <= 32) rows_launch<TYPE, 2, 1, 8, 2>(p, s);
+    else rows_launch<TYPE, 4, 2, 4, 2>(p, s);
+}
+static int few_rows_product(const slz_i4_shape *sh, const void *x, const uint8_t *q, const float *scale, void *y, hipStream_t s) {
+    const bool thin = thin_takes(sh);
+    for (uint32_t first = 0, most = 1u << 22; first < sh->n; first += most) {         // threads of a launch stay below 2^32
+        const i4_args p{(const char *)x, (const char *)q + first * sh->ld_q, scale + first * sh->ld_scale, (char *)y + (size_t)first * slz_type_bytes(sh->type),
+                        sh->ld_x, sh->ld_q, sh->ld_scale, sh->ld_y, sh->m, sh->n - first < most ? sh->n - first : most, sh->k, sh->group};
+        if (sh->type == SLZ_F32) few_rows<SLZ_F32>(p, thin, s);
+        else if (sh->type == SLZ_BF16) few_rows<SLZ_BF16>(p, thin, s);
+        else few_rows<SLZ_F16>(p, thin, s);
+    }
+    return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
+}
+
 // ---- values as an operand ------------------------------------------------------------------------------------------------------------
 // f16 could not hold small scales, so its values are held times VALUES_UP / unit, the power of two above the largest finite scale: magnitudes of up to
 // 7 2^12 are below f16's largest, and rows whose scale is down to 2^-26 of the largest keep 11 bits.
@@ -233,6 +621,7 @@ static linear_plan plan_linear(const slz_i4_shape *sh, const void *x) {
     P.x = values_bytes(sh->type, sh->n, sh->k);
     P.ranges = P.x + slz_operand_bytes(x, sh->type, sh->m, sh->k, sh->ld_x);
     P.total = P.ranges + slz_ranges_bytes(P.c, sh->m, sh->n);
+    if (thin_takes(sh) || rows_takes(sh)) P.total = 0;
     return P;
 }
 extern "C" int slz_linear_i4_workspace(const slz_i4_shape *sh, const void *x, size_t *bytes) {
@@ -251,6 +640,7 @@ extern "C" int slz_linear_i4(const slz_i4_shape *sh, const void *x, const uint8_
     const linear_plan P = plan_linear(sh, x);
     if (!slz_ws_ok(ws, ws_bytes, P.total)) return SLZ_E_INVALID_ARG;
     hipStream_t s = (hipStream_t)stream;
+    if (thin_takes(sh) || rows_takes(sh)) return few_rows_product(sh, x, q, scale, y, s);
     char *at = (char *)ws;
     slz_layouts jobs = {};
     const slz_operand a = slz_operand_of(x, sh->type, sh->m, sh->k, sh->ld_x, at + P.x, jobs);
