@@ -186,30 +186,28 @@ template <int TYPE> __device__ __forceinline__ void i4_octet(const row8<TYPE> &q
 // A wave's share of the weights: 16 NB rows, a block's entries at a time.  Rows of a workgroup begin at uniform addresses, lanes' places are below 2^32 from there.
 template <int NB> struct i4_stream {
     const char *q0;
-    const float *scale0;
-    uint32_t at_q[NB], shift, groups;                  // a group has 2^shift entries
+    uint32_t at_q[NB];
     __device__ __forceinline__ void init(const i4_args &p, uint32_t first, uint32_t lane) {
         const uint32_t n0 = min(first, p.N - 1);       // a wave without rows reads the last one
         q0 = p.q + (int64_t)n0 * p.ld_q;
-        scale0 = p.scale + (int64_t)n0 * p.ld_scale;
 #pragma unroll
         for (int j = 0; j < NB; j++) {
             const uint32_t row = min(j * 16 + (lane & 15u), p.N - 1 - n0);
             at_q[j] = row * (uint32_t)p.ld_q + (lane >> 4) * 16u;
         }
-        shift = p.group == 32 ? 5u : p.group == 64 ? 6u : 7u;
-        groups = (p.K + p.group - 1) >> shift;
     }
     __device__ __forceinline__ void load(uint32_t block, v4i32 (&w)[NB]) const {
 #pragma unroll
         for (int j = 0; j < NB; j++) w[j] = *(const v4i32 *)(q0 + (at_q[j] + block * 64u));
     }
 };
-// Sums of a block's four steps: part collects a group, acc the groups times their scales.  read(step, i, o): x's operands
-template <int EL, int PIECES, int MI, int NB, class READ>
-__device__ __forceinline__ void i4_block(const v4i32 (&w)[NB], const v4f (&s)[NB], uint32_t shift, v4f (&part)[MI][NB], v4f (&acc)[MI][NB], const READ &read) {
+// Sums of a block's four steps: part collects a group (of 2^SHIFT entries), acc the groups times their scales.  read(step, i, o): x's operands
+template <int EL, int PIECES, int SHIFT, int MI, int NB, class READ>
+__device__ __forceinline__ void i4_block(const v4i32 (&w)[NB], const v4f (&s)[NB], v4f (&acc)[MI][NB], const READ &read) {
+    v4f part[MI][NB];
 #pragma unroll
     for (int step = 0; step < 4; step++) {
+        constexpr int OF = 1 << (SHIFT - 5);           // steps of a group
         v4i32 b[NB];
 #pragma unroll
         for (int j = 0; j < NB; j++) b[j] = i4_operand<EL>((uint32_t)w[j][step]);
@@ -220,19 +218,15 @@ __device__ __forceinline__ void i4_block(const v4i32 (&w)[NB], const v4f (&s)[NB
 #pragma unroll
             for (int k = PIECES - 1; k >= 0; k--)
 #pragma unroll
-                for (int j = 0; j < NB; j++) part[i][j] = slz_mma<EL>(o[k], b[j], part[i][j]);
+                for (int j = 0; j < NB; j++) part[i][j] = slz_mma<EL>(o[k], b[j], step % OF == 0 && k == PIECES - 1 ? v4f{0, 0, 0, 0} : part[i][j]);
         }
-        if (step == 3 || shift == 5u || (shift == 6u && step == 1))                // a group ends
+        if (step % OF == OF - 1)
 #pragma unroll
-            for (int j = 0; j < NB; j++) {
-                const float of_32 = s[j][step], of_64 = s[j][step / 2], of_128 = s[j][0], f = shift == 5u ? of_32 : shift == 6u ? of_64 : of_128;
+            for (int i = 0; i < MI; i++)
 #pragma unroll
-                for (int i = 0; i < MI; i++) {
+                for (int j = 0; j < NB; j++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) acc[i][j][e] = __builtin_fmaf(part[i][j][e], f, acc[i][j][e]);
-                    part[i][j] = v4f{0, 0, 0, 0};
-                }
-            }
+                    for (int e = 0; e < 4; e++) acc[i][j][e] = __builtin_fmaf(part[i][j][e], s[j][step / OF], acc[i][j][e]);
     }
 }
 
@@ -243,7 +237,7 @@ __device__ __forceinline__ void i4_block(const v4i32 (&w)[NB], const v4f (&s)[NB
 #define THIN_SLOTS 2                 // octets of x, and scales, that a thread has under way
 static inline __host__ __device__ uint32_t thin_pitch(uint32_t k) { return i4_blocks(k) * 256u + 16u; }
 static inline __host__ __device__ uint32_t thin_scales(uint32_t groups) { return (groups | 3u) + 2u; }         // floats of a row: odd, and up to three past its end are there
-template <int TYPE, int NB>
+template <int TYPE, int NB, int SHIFT>
 __global__ void __launch_bounds__(THIN_WAVES * 64) k_thin_i4(const i4_args p) {
     constexpr int EL = TYPE == SLZ_F16 ? SLZ_EL_F16 : SLZ_EL_BF16, PIECES = i4_pieces<TYPE>, AHEAD = 4;
     constexpr uint32_t THREADS = THIN_WAVES * 64, ROWS = 16 * NB;
@@ -253,7 +247,8 @@ __global__ void __launch_bounds__(THIN_WAVES * 64) k_thin_i4(const i4_args p) {
     const uint32_t begin = wave * blocks / THIN_WAVES, end = (wave + 1) * blocks / THIN_WAVES;
     i4_stream<NB> q;
     q.init(p, n0, lane);
-    const uint32_t octets = p.M * blocks * 16u, count = ROWS * q.groups, pitch_s = thin_scales(q.groups);
+    const uint32_t groups = (p.K + (1u << SHIFT) - 1) >> SHIFT, octets = p.M * blocks * 16u, count = ROWS * groups, pitch_s = thin_scales(groups);
+    const float *scale0 = p.scale + (int64_t)n0 * p.ld_scale;
     float *scales = (float *)(lds + PIECES * p.M * pitch);
     row8<TYPE> x[THIN_SLOTS];
     float sc[THIN_SLOTS];
@@ -262,8 +257,8 @@ __global__ void __launch_bounds__(THIN_WAVES * 64) k_thin_i4(const i4_args p) {
         return (i - m * (blocks * 16u)) * 8u;
     };
     const auto load_scale = [&](uint32_t i) {
-        const uint32_t row = i / q.groups;
-        return q.scale0[(size_t)min(row, p.N - 1 - n0) * p.ld_scale + i - row * q.groups];
+        const uint32_t row = i / groups;
+        return scale0[(size_t)min(row, p.N - 1 - n0) * p.ld_scale + i - row * groups];
     };
 #pragma unroll
     for (uint32_t t = 0; t < THIN_SLOTS; t++) {
@@ -290,22 +285,22 @@ __global__ void __launch_bounds__(THIN_WAVES * 64) k_thin_i4(const i4_args p) {
     for (uint32_t t = 0; t < THIN_SLOTS; t++) {
         const uint32_t i = threadIdx.x + t * THREADS;
         if (i < octets) put_x(i, x[t]);
-        if (i < count) scales[i / q.groups * pitch_s + i % q.groups] = sc[t];
+        if (i < count) scales[i / groups * pitch_s + i % groups] = sc[t];
     }
     for (uint32_t i = threadIdx.x + THIN_SLOTS * THREADS; i < octets; i += THREADS) {
         uint32_t m;
         const uint32_t c = octet(i, m);
         put_x(i, row8_load<TYPE>(p.x, (size_t)m * p.ld_x, c, p.K));
     }
-    for (uint32_t i = threadIdx.x + THIN_SLOTS * THREADS; i < count; i += THREADS) scales[i / q.groups * pitch_s + i % q.groups] = load_scale(i);
+    for (uint32_t i = threadIdx.x + THIN_SLOTS * THREADS; i < count; i += THREADS) scales[i / groups * pitch_s + i % groups] = load_scale(i);
     if (threadIdx.x < ROWS)                            // groups past the rows' ends
-        for (uint32_t c = q.groups; c < pitch_s; c++) scales[threadIdx.x * pitch_s + c] = 0.0f;
+        for (uint32_t c = groups; c < pitch_s; c++) scales[threadIdx.x * pitch_s + c] = 0.0f;
     __syncthreads();
     const char *from = lds + min(r, p.M - 1) * pitch + g * 16u;
     const uint32_t piece = p.M * pitch;
-    v4f acc[1][NB], part[1][NB];
+    v4f acc[1][NB];
 #pragma unroll
-    for (int j = 0; j < NB; j++) acc[0][j] = part[0][j] = v4f{0, 0, 0, 0};
+    for (int j = 0; j < NB; j++) acc[0][j] = v4f{0, 0, 0, 0};
     for (uint32_t b0 = begin; b0 < end; b0 += AHEAD)
 #pragma unroll
         for (int d = 0; d < AHEAD; d++) {
@@ -314,12 +309,10 @@ __global__ void __launch_bounds__(THIN_WAVES * 64) k_thin_i4(const i4_args p) {
             v4f s[NB];
 #pragma unroll
             for (int j = 0; j < NB; j++) {
-                const float *at = scales + (j * 16 + r) * pitch_s + (block << (7u - q.shift));
-                if (q.shift == 7u) s[j] = v4f{at[0], 0, 0, 0};
-                else if (q.shift == 6u) s[j] = v4f{at[0], at[1], 0, 0};
-                else s[j] = v4f{at[0], at[1], at[2], at[3]};
+                const float *at = scales + (j * 16 + r) * pitch_s + (block << (7 - SHIFT));
+                s[j] = SHIFT == 7 ? v4f{at[0], 0, 0, 0} : SHIFT == 6 ? v4f{at[0], at[1], 0, 0} : v4f{at[0], at[1], at[2], at[3]};
             }
-            i4_block<EL, PIECES>(w[d], s, q.shift, part, acc, [&](int step, int, v4i32 (&o)[PIECES]) {
+            i4_block<EL, PIECES, SHIFT>(w[d], s, acc, [&](int step, int, v4i32 (&o)[PIECES]) {
 #pragma unroll
                 for (int k = 0; k < PIECES; k++) o[k] = *(const v4i32 *)(from + k * piece + block * 256u + step * 64u);
             });
@@ -342,128 +335,128 @@ __global__ void __launch_bounds__(THIN_WAVES * 64) k_thin_i4(const i4_args p) {
     }
 }
 
-// More rows: a workgroup has 16 MI rows of x and 32 WN of weights.  Its waves are WN by WK: in each phase WK blocks of k of x come to shared memory, on the way through registers
-// while the phase before is computed, and a wave multiplies one of them by its 32 rows of weights.  The WK waves' sums meet in shared memory at the end.
-template <int TYPE, int MI, int WN, int WK, int BUFFERS>
+// More rows: a workgroup has 16 MI rows of x and 32 WN of weights.  Its waves are WN by WK: in each phase WK blocks of k of x and the scales that go with them come to shared memory, on
+// the way through registers while the phase before is computed, and a wave multiplies one of the blocks by its 32 rows of weights, whose words come AHEAD phases before.  The WK waves'
+// sums meet in shared memory at the end.  Every phase does all loads (past the end those of the last phase again), so that the compiler can count what is under way.
+template <int TYPE, int MI, int WN, int WK, int BUFFERS, int SHIFT>
 __global__ void __launch_bounds__(WN *WK * 64) k_rows_i4(const i4_args p, uint32_t tiles_m, uint32_t tiles_n) {
-    constexpr int EL = TYPE == SLZ_F16 ? SLZ_EL_F16 : SLZ_EL_BF16, PIECES = i4_pieces<TYPE>, XB = TYPE == SLZ_F32 ? 4 : 2, NB = 2, AHEAD = 4, THREADS = WN * WK * 64;
+    constexpr int EL = TYPE == SLZ_F16 ? SLZ_EL_F16 : SLZ_EL_BF16, PIECES = i4_pieces<TYPE>, XB = TYPE == SLZ_F32 ? 4 : 2, NB = 2, AHEAD = 2, THREADS = WN * WK * 64;
     constexpr uint32_t TM = MI * 16, TN = WN * NB * 16, PITCH = 272, PIECE = TM * PITCH, BLOCK = PIECES * PIECE, BUFFER = WK * BLOCK;
     constexpr int OCTETS = WK * TM * 16 / THREADS;
     static_assert(OCTETS * THREADS == WK * TM * 16, "");
     constexpr uint32_t SUMS = WK * TM * TN * 4, LDS = BUFFERS * BUFFER > SUMS ? BUFFERS * BUFFER : SUMS;
-    constexpr int SCALES = (TN * WK * 4 + THREADS - 1) / THREADS;
+    constexpr uint32_t GROUPS = WK << (7 - SHIFT);     // of a phase
+    constexpr int SCALES = (TN * GROUPS + THREADS - 1) / THREADS;
     __shared__ __attribute__((aligned(16))) char lds[LDS];
-    __shared__ float scales[2][WK * 4][TN + 4];         // [group of the phase][row of weights]
+    __shared__ float scales[2][GROUPS][TN + 4];        // [group][row of weights]
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15u, g = lane >> 4;
     const uint32_t wn = wave % WN, wk = wave / WN;
     // the tiles of x that meet one tile of weights follow each other on one XCD
     const uint32_t eights = blockIdx.x / (8u * tiles_m), in = blockIdx.x % (8u * tiles_m), left = min(8u, tiles_n - eights * 8u);
     const uint32_t n0 = (eights * 8u + in % left) * TN, m0 = in / left * TM;
-    const uint32_t blocks = (p.K + I4_BLOCK - 1) / I4_BLOCK, phases = (blocks + WK - 1) / WK;
+    const uint32_t blocks = (p.K + I4_BLOCK - 1) / I4_BLOCK, phases = (blocks + WK - 1) / WK, groups = (p.K + (1u << SHIFT) - 1) >> SHIFT;
     // workgroups begin at different phases: where all read the same columns of x and of rows a power of two apart, a few memory channels have all the work
     const uint32_t turn = n0 / TN % phases;
-    const auto phase_of = [&](uint32_t i) { return i + turn < phases ? i + turn : i + turn - phases; };
+    const auto phase_of = [&](uint32_t number) {
+        const uint32_t i = min(number, phases - 1) + turn;
+        return i < phases ? i : i - phases;
+    };
     i4_stream<NB> q;
     q.init(p, n0 + wn * (NB * 16), lane);
     v4i32 w[AHEAD][NB];
-#pragma unroll
-    for (int d = 0; d < AHEAD; d++)
-        if (d < phases) q.load(min(phase_of(d) * WK + wk, blocks - 1), w[d]);
-    // this thread's scales of a phase: rows of weights and groups, 0 past the rows' ends
-    const uint32_t per_block = 7u - q.shift;
-    const float *scale0 = p.scale + (int64_t)n0 * p.ld_scale;
-    float sc[SCALES];
-    const auto group_of = [&](uint32_t phase, uint32_t i, uint32_t &row) {
-        row = i >> (per_block + (WK == 8 ? 3 : 2));
-        return (phase * WK << per_block) + (i & ((WK << per_block) - 1u));
-    };
-    const auto load_scales = [&](uint32_t number) {
-#pragma unroll
-        for (int t = 0; t < SCALES; t++) {
-            uint32_t row;
-            const uint32_t c = group_of(phase_of(number), threadIdx.x + t * THREADS, row);
-            sc[t] = scale0[min(row, p.N - 1 - n0) * (uint32_t)p.ld_scale + min(c, q.groups - 1)];
-        }
-    };
-    const auto store_scales = [&](uint32_t number) {
-#pragma unroll
-        for (int t = 0; t < SCALES; t++) {
-            uint32_t row;
-            const uint32_t i = threadIdx.x + t * THREADS, c = group_of(phase_of(number), i, row);
-            if (row < TN) scales[number & 1u][i & ((WK << per_block) - 1u)][row] = c < q.groups ? sc[t] : 0.0f;
-        }
-    };
-
-    // this thread's octets of x in a phase: column and row (the last one again where there are fewer, for sums that no one stores)
-    const uint32_t last = p.M - 1 - m0;
+    // this thread's octets of x: row (the last one again where there are fewer, for sums that no one stores) and column in the phase
     const char *x0 = p.x + (int64_t)m0 * p.ld_x * XB;
     row8<TYPE> x[OCTETS];
-    const auto column = [&](uint32_t phase, int i) { return (phase * WK + (threadIdx.x + i * THREADS) / (TM * 16)) * I4_BLOCK + threadIdx.x % 16u * 8u; };
-    const auto row = [&](int i) { return (threadIdx.x + i * THREADS) / 16u % TM; };
-    const auto load_x = [&](uint32_t number) {
-        const uint32_t phase = phase_of(number);
+    uint32_t at_x[OCTETS], col_x[OCTETS], to_x[OCTETS];
+#pragma unroll
+    for (int i = 0; i < OCTETS; i++) {
+        const uint32_t o = threadIdx.x + i * THREADS, row = o / 16u % TM, block = o / (TM * 16);
+        at_x[i] = min(row, p.M - 1 - m0) * (uint32_t)p.ld_x;
+        col_x[i] = block * I4_BLOCK + o % 16u * 8u;
+        to_x[i] = block * BLOCK + row * PITCH + o % 16u * 16u;
+    }
+    const auto load_x = [&](uint32_t phase) {
 #pragma unroll
         for (int i = 0; i < OCTETS; i++) {
             // where the row ends inside, its last eight; i4_octet moves them down
-            const v4i32_any *at = (const v4i32_any *)(x0 + (size_t)((min(row(i), last) * (uint32_t)p.ld_x + min(column(phase, i), p.K - 8u)) * XB));
+            const v4i32_any *at = (const v4i32_any *)(x0 + (size_t)((at_x[i] + min(col_x[i] + phase * (WK * I4_BLOCK), p.K - 8u)) * XB));
             x[i].w[0] = at[0];
             if constexpr (TYPE == SLZ_F32) x[i].w[1] = at[1];
         }
     };
-    const auto store_x = [&](uint32_t number) {
-        const uint32_t phase = phase_of(number);
+    const auto store_x = [&](uint32_t phase, char *to) {
+        const bool inside = (phase + 1) * (WK * I4_BLOCK) <= p.K;
 #pragma unroll
         for (int i = 0; i < OCTETS; i++) {
             v4i32 o[PIECES];
-            i4_octet<TYPE>(x[i], column(phase, i), p.K, o);
-            char *to = lds + (BUFFERS == 2 ? number & 1u : 0u) * BUFFER + (threadIdx.x + i * THREADS) / (TM * 16) * BLOCK + row(i) * PITCH + threadIdx.x % 16u * 16u;
+            if (inside) i4_octet<TYPE>(x[i], 0, 8, o);
+            else i4_octet<TYPE>(x[i], col_x[i] + phase * (WK * I4_BLOCK), p.K, o);
 #pragma unroll
-            for (int k = 0; k < PIECES; k++) *(v4i32 *)(to + k * PIECE) = o[k];
+            for (int k = 0; k < PIECES; k++) *(v4i32 *)(to + to_x[i] + k * PIECE) = o[k];
         }
     };
-    v4f acc[MI][NB], part[MI][NB];
+    // this thread's scales: rows of weights and groups of the phase, 0 past the rows' ends
+    const float *scale0 = p.scale + (int64_t)n0 * p.ld_scale;
+    float sc[SCALES];
+    const auto load_scales = [&](uint32_t phase) {
+#pragma unroll
+        for (int t = 0; t < SCALES; t++) {
+            const uint32_t i = threadIdx.x + t * THREADS;
+            sc[t] = scale0[min(i / GROUPS, p.N - 1 - n0) * (uint32_t)p.ld_scale + min(phase * GROUPS + i % GROUPS, groups - 1)];
+        }
+    };
+    const auto store_scales = [&](uint32_t phase, int buffer) {
+#pragma unroll
+        for (int t = 0; t < SCALES; t++) {
+            const uint32_t i = threadIdx.x + t * THREADS;
+            if (TN * GROUPS % THREADS == 0 || i < TN * GROUPS) scales[buffer][i % GROUPS][i / GROUPS] = phase * GROUPS + i % GROUPS < groups ? sc[t] : 0.0f;
+        }
+    };
+    const auto load_w = [&](uint32_t phase, v4i32 (&to)[NB]) { q.load(min(phase * WK + wk, blocks - 1), to); };
+
+    load_x(phase_of(0));
+    load_scales(phase_of(0));
+#pragma unroll
+    for (int d = 0; d < AHEAD; d++) load_w(phase_of(d), w[d]);
+    store_x(phase_of(0), lds);
+    store_scales(phase_of(0), 0);
+    load_x(phase_of(1));
+    load_scales(phase_of(1));
+    v4f acc[MI][NB];
 #pragma unroll
     for (int i = 0; i < MI; i++)
 #pragma unroll
-        for (int j = 0; j < NB; j++) acc[i][j] = part[i][j] = v4f{0, 0, 0, 0};
-    load_x(0);
-    load_scales(0);
-    store_x(0);
-    store_scales(0);
-    if (phases > 1) {
-        load_x(1);
-        load_scales(1);
-    }
+        for (int j = 0; j < NB; j++) acc[i][j] = v4f{0, 0, 0, 0};
     __syncthreads();
     for (uint32_t p0 = 0; p0 < phases; p0 += AHEAD)
 #pragma unroll
         for (int d = 0; d < AHEAD; d++) {
-            const uint32_t phase = p0 + d;
-            if (phase >= phases) break;
-            if (phase + 1 < phases) {
-                store_scales(phase + 1);
-                if (phase + 2 < phases) load_scales(phase + 2);
+            const uint32_t number = p0 + d;
+            if (number >= phases) break;
+            if (BUFFERS == 2) {
+                store_x(phase_of(number + 1), lds + (1 - d) * BUFFER);
+                store_scales(phase_of(number + 1), 1 - d);
+                load_x(phase_of(number + 2));
+                load_scales(phase_of(number + 2));
             }
-            if (BUFFERS == 2 && phase + 1 < phases) {
-                store_x(phase + 1);
-                if (phase + 2 < phases) load_x(phase + 2);
-            }
-            const char *from = lds + (BUFFERS == 2 ? phase & 1u : 0u) * BUFFER + wk * BLOCK + r * PITCH + g * 16u;
+            const char *from = lds + (BUFFERS == 2 ? d : 0) * BUFFER + wk * BLOCK + r * PITCH + g * 16u;
             v4f s[NB];
 #pragma unroll
             for (int j = 0; j < NB; j++)
 #pragma unroll
-                for (int e = 0; e < 4; e++) s[j][e] = scales[phase & 1u][(wk << per_block) + (e & ((1u << per_block) - 1u))][(wn * NB + j) * 16 + r];
-            if (phase_of(phase) * WK + wk < blocks)
-                i4_block<EL, PIECES>(w[d], s, q.shift, part, acc, [&](int step, int i, v4i32 (&o)[PIECES]) {
+                for (int e = 0; e < 1 << (7 - SHIFT); e++) s[j][e] = scales[BUFFERS == 2 ? d : 0][(wk << (7 - SHIFT)) + e][(wn * NB + j) * 16 + r];
+            // a block past the end is the last one again, times zeros
+            i4_block<EL, PIECES, SHIFT>(w[d], s, acc, [&](int step, int i, v4i32 (&o)[PIECES]) {
 #pragma unroll
-                    for (int k = 0; k < PIECES; k++) o[k] = *(const v4i32 *)(from + k * PIECE + i * (16 * PITCH) + step * 64);
-                });
-            if (phase + AHEAD < phases) q.load(min(phase_of(phase + AHEAD) * WK + wk, blocks - 1), w[d]);
+                for (int k = 0; k < PIECES; k++) o[k] = *(const v4i32 *)(from + k * PIECE + i * (16 * PITCH) + step * 64);
+            });
+            load_w(phase_of(number + AHEAD), w[d]);
             __syncthreads();
-            if (BUFFERS == 1 && phase + 1 < phases) {
-                store_x(phase + 1);
-                if (phase + 2 < phases) load_x(phase + 2);
+            if (BUFFERS == 1) {
+                store_x(phase_of(number + 1), lds);
+                store_scales(phase_of(number + 1), 0);
+                load_x(phase_of(number + 2));
+                load_scales(phase_of(number + 2));
                 __syncthreads();
             }
         }
@@ -490,20 +483,23 @@ static size_t thin_bytes(uint32_t m, uint32_t k, uint32_t group, int type, uint3
 }
 static bool thin_takes(const slz_i4_shape *sh) { return sh->m <= 8 && thin_bytes(sh->m, sh->k, sh->group, sh->type, 2) <= THIN_LDS; }
 static bool rows_takes(const slz_i4_shape *sh) { return sh->m <= 256 && sh->k >= 8; }
-template <int TYPE, int NB> static void thin_launch(const i4_args &p, hipStream_t s) {
+template <int TYPE, int SHIFT, int NB> static void thin_launch(const i4_args &p, hipStream_t s) {
     const size_t x = thin_bytes(p.M, p.K, p.group, TYPE, NB), sums = (size_t)THIN_WAVES * 16 * NB * 16 * 4;
-    hipLaunchKernelGGL((k_thin_i4<TYPE, NB>), dim3((p.N + 16 * NB - 1) / (16 * NB)), dim3(THIN_WAVES * 64), x > sums ? x : sums, s, p);
+    hipLaunchKernelGGL((k_thin_i4<TYPE, NB, SHIFT>), dim3((p.N + 16 * NB - 1) / (16 * NB)), dim3(THIN_WAVES * 64), x > sums ? x : sums, s, p);
 }
-template <int TYPE, int MI, int WN, int WK, int BUFFERS> static void rows_launch(const i4_args &p, hipStream_t s) {
+template <int TYPE, int SHIFT, int MI, int WN, int WK, int BUFFERS> static void rows_launch(const i4_args &p, hipStream_t s) {
     const uint32_t tiles_m = (p.M + MI * 16 - 1) / (MI * 16), tiles_n = (p.N + WN * 32 - 1) / (WN * 32);
-    hipLaunchKernelGGL((k_rows_i4<TYPE, MI, WN, WK, BUFFERS>), dim3(tiles_m * tiles_n), dim3(WN * WK * 64), 0, s, p, tiles_m, tiles_n);
+    hipLaunchKernelGGL((k_rows_i4<TYPE, MI, WN, WK, BUFFERS, SHIFT>), dim3(tiles_m * tiles_n), dim3(WN * WK * 64), 0, s, p, tiles_m, tiles_n);
+}
+template <int TYPE, int SHIFT> static void few_rows_of(const i4_args &p, bool thin, hipStream_t s) {
+    if (thin) p.N <= 8192 ? thin_launch<TYPE, SHIFT, 1>(p, s) : thin_launch<TYPE, SHIFT, 2>(p, s);
+    else if constexpr (TYPE == SLZ_F32) p.M <= 16 ? rows_launch<TYPE, SHIFT, 1, 2, 4, 1>(p, s) : rows_launch<TYPE, SHIFT, 2, 2, 4, 1>(p, s);
+    else if (p.M <= 16) rows_launch<TYPE, SHIFT, 1, 1, 8, 2>(p, s);
+    else if (p.M <= 32) rows_launch<TYPE, SHIFT, 2, 1, 8, 2>(p, s);
+    else rows_launch<TYPE, SHIFT, 4, 2, 4, 2>(p, s);
 }
 template <int TYPE> static void few_rows(const i4_args &p, bool thin, hipStream_t s) {
-    if (thin) p.N <= 8192 ? thin_launch<TYPE, 1>(p, s) : thin_launch<TYPE, 2>(p, s);
-    else if constexpr (TYPE == SLZ_F32) p.M <= 16 ? rows_launch<TYPE, 1, 2, 4, 1>(p, s) : rows_launch<TYPE, 2, 2, 4, 1>(p, s);
-    else if (p.M <= 16) rows_launch<TYPE, 1, 1, 8, 2>(p, s);
-    else if (p.M <= 32) rows_launch<TYPE, 2, 1, 8, 2>(p, s);
-    else rows_launch<TYPE, 4, 2, 4, 2>(p, s);
+    p.group == 32 ? few_rows_of<TYPE, 5>(p, thin, s) : p.group == 64 ? few_rows_of<TYPE, 6>(p, thin, s) : few_rows_of<TYPE, 7>(p, thin, s);
 }
 static int few_rows_product(const slz_i4_shape *sh, const void *x, const uint8_t *q, const float *scale, void *y, hipStream_t s) {
     const bool thin = thin_takes(sh);
