@@ -3,10 +3,9 @@
 // A word of a 4-bit row has eight consecutive entries, which is what a lane feeds to a matrix instruction, and a block of 128 entries lies so that the
 // four words that a lane needs for the block's four instructions are 16 bytes in a row.
 #include "slz_gemm.h"
+#include "slz_i4_route.h"
 
-#define I4_BLOCK 128u                // entries of a block, 64 bytes
-__host__ __device__ static inline uint32_t i4_blocks(uint32_t cols) { return (cols + I4_BLOCK - 1) / I4_BLOCK; }
-static inline uint32_t i4_groups(uint32_t cols, uint32_t group) { return (cols + group - 1) / group; }
+#define THIN_WAVES (I4_THREADS / 64)
 
 // entries e of a word, in the order of k: a sign and a magnitude
 __device__ __forceinline__ float i4_entry(uint32_t word, int e) {
@@ -130,30 +129,26 @@ extern "C" int slz_values_i4(const uint8_t *q, int64_t ld_q, const float *scale,
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------------------------------
-// The entries of a word as eight numbers of a matrix operand, exact.  A number's high byte and, in bf16, its low byte depend on the three bits of the
-// magnitude: each is looked up for four entries at once by a byte permutation of the table 0 .. 7, whose selectors are the entries themselves.
+// The entries of a word as eight numbers of a matrix operand, exact.  As a byte, sign and magnitude in the lowest bits of its fields, an entry is a subnormal e4m3 number, 2^-9 times the
+// entry; the conversion to two bf16 or f16 takes a factor.  10 instructions a word (tables of the numbers' bytes by permutation: 15).
 template <int EL> __device__ __forceinline__ v4i32 i4_operand(uint32_t word) {
-    constexpr uint32_t HI03 = EL == SLZ_EL_BF16 ? 0x40403f00u : 0x42403c00u, HI47 = EL == SLZ_EL_BF16 ? 0x40404040u : 0x47464544u;
-    constexpr uint32_t LO03 = 0x40008000u, LO47 = 0xe0c0a080u;                     // bf16: 0, 3f80, 4000, 4040, 4080, 40a0, 40c0, 40e0; f16: low bytes are 0
     v4i32 o;
 #pragma unroll
     for (int h = 0; h < 2; h++) {
-        const uint32_t w = h ? word >> 4 : word, at = w & 0x07070707u;
-        const uint32_t hi = __builtin_amdgcn_perm(HI47, HI03, at) | (w & 0x08080808u) << 4;
+        const uint32_t b = h ? (word >> 4 & 0x07070707u) | (word & 0x80808080u) : (word & 0x07070707u) | (word << 4 & 0x80808080u);
         if constexpr (EL == SLZ_EL_BF16) {
-            const uint32_t lo = __builtin_amdgcn_perm(LO47, LO03, at);
-            o[2 * h] = (int)__builtin_amdgcn_perm(hi, lo, 0x05010400u);
-            o[2 * h + 1] = (int)__builtin_amdgcn_perm(hi, lo, 0x07030602u);
+            o[2 * h] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, 512.0f, false));
+            o[2 * h + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, 512.0f, true));
         } else {
-            o[2 * h] = (int)__builtin_amdgcn_perm(hi, 0u, 0x050c040cu);
-            o[2 * h + 1] = (int)__builtin_amdgcn_perm(hi, 0u, 0x070c060cu);
+            o[2 * h] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, 512.0f, false));
+            o[2 * h + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, 512.0f, true));
         }
     }
     return o;
 }
 
 // What follows streams the weights past the matrix instructions with the entries as whole numbers; what a group sums up to in 32 bits is multiplied by its scale, so that no value is
-// rounded.  x is laid out in shared memory as operands, rows I4_PITCH bytes for 128 entries or one row's length, 16 bytes apart in the banks.
+// rounded.  x lies in shared memory as operands.
 struct i4_args {
     const char *x, *q;
     const float *scale;
@@ -201,25 +196,31 @@ template <int NB> struct i4_stream {
         for (int j = 0; j < NB; j++) w[j] = *(const v4i32 *)(q0 + (at_q[j] + block * 64u));
     }
 };
-// Sums of a block's four steps: part collects a group (of 2^SHIFT entries), acc the groups times their scales.  read(step, i, o): x's operands
+// Sums of a block's four steps: part collects a group (of 2^SHIFT entries), acc the groups times their scales.  read(step, i, o): x's operands.  A step's operands are read and
+// its entries converted while the matrix instructions of the step before run.
 template <int EL, int PIECES, int SHIFT, int MI, int NB, class READ>
 __device__ __forceinline__ void i4_block(const v4i32 (&w)[NB], const v4f (&s)[NB], v4f (&acc)[MI][NB], const READ &read) {
+    constexpr int OF = 1 << (SHIFT - 5);               // steps of a group
     v4f part[MI][NB];
+    v4i32 o[2][MI][PIECES], b[2][NB];
+    const auto prepare = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < MI; i++) read(step, i, o[step & 1][i]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < NB; j++) b[step & 1][j] = i4_operand<EL>((uint32_t)w[j][step]);
+    };
+    prepare(0);
 #pragma unroll
     for (int step = 0; step < 4; step++) {
-        constexpr int OF = 1 << (SHIFT - 5);           // steps of a group
-        v4i32 b[NB];
+        if (step < 3) prepare(step + 1);
 #pragma unroll
-        for (int j = 0; j < NB; j++) b[j] = i4_operand<EL>((uint32_t)w[j][step]);
-#pragma unroll
-        for (int i = 0; i < MI; i++) {
-            v4i32 o[PIECES];
-            read(step, i, o);
+        for (int i = 0; i < MI; i++)
 #pragma unroll
             for (int k = PIECES - 1; k >= 0; k--)
 #pragma unroll
-                for (int j = 0; j < NB; j++) part[i][j] = slz_mma<EL>(o[k], b[j], step % OF == 0 && k == PIECES - 1 ? v4f{0, 0, 0, 0} : part[i][j]);
-        }
+                for (int j = 0; j < NB; j++)
+                    part[i][j] = slz_mma<EL>(o[step & 1][i][k], b[step & 1][j], step % OF == 0 && k == PIECES - 1 ? v4f{0, 0, 0, 0} : part[i][j]);
         if (step % OF == OF - 1)
 #pragma unroll
             for (int i = 0; i < MI; i++)
@@ -232,22 +233,18 @@ __device__ __forceinline__ void i4_block(const v4i32 (&w)[NB], const v4f (&s)[NB
 
 // A few rows, all of x and of the scales that a workgroup needs in shared memory.  A workgroup of eight waves has 16 NB rows of weights, each wave an eighth of the blocks of k.
 // Loads return in order, so those of x and the scales go first, then the wave's first blocks, before anything is looked at; the eight waves' sums meet in shared memory.
-#define THIN_WAVES 8
-#define THIN_LDS (128u << 10)
 #define THIN_SLOTS 2                 // octets of x, and scales, that a thread has under way
-static inline __host__ __device__ uint32_t thin_pitch(uint32_t k) { return i4_blocks(k) * 256u + 16u; }
-static inline __host__ __device__ uint32_t thin_scales(uint32_t groups) { return (groups | 3u) + 2u; }         // floats of a row: odd, and up to three past its end are there
 template <int TYPE, int NB, int SHIFT>
 __global__ void __launch_bounds__(THIN_WAVES * 64) k_thin_i4(const i4_args p) {
     constexpr int EL = TYPE == SLZ_F16 ? SLZ_EL_F16 : SLZ_EL_BF16, PIECES = i4_pieces<TYPE>, AHEAD = 4;
     constexpr uint32_t THREADS = THIN_WAVES * 64, ROWS = 16 * NB;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15u, g = lane >> 4;
-    const uint32_t n0 = blockIdx.x * ROWS, blocks = (p.K + I4_BLOCK - 1) / I4_BLOCK, pitch = thin_pitch(p.K);
+    const uint32_t n0 = blockIdx.x * ROWS, blocks = (p.K + I4_BLOCK - 1) / I4_BLOCK, pitch = i4_pitch(p.K);
     const uint32_t begin = wave * blocks / THIN_WAVES, end = (wave + 1) * blocks / THIN_WAVES;
     i4_stream<NB> q;
     q.init(p, n0, lane);
-    const uint32_t groups = (p.K + (1u << SHIFT) - 1) >> SHIFT, octets = p.M * blocks * 16u, count = ROWS * groups, pitch_s = thin_scales(groups);
+    const uint32_t groups = (p.K + (1u << SHIFT) - 1) >> SHIFT, octets = p.M * blocks * 16u, count = ROWS * groups, pitch_s = i4_pitch_scales(groups);
     const float *scale0 = p.scale + (int64_t)n0 * p.ld_scale;
     float *scales = (float *)(lds + PIECES * p.M * pitch);
     row8<TYPE> x[THIN_SLOTS];
@@ -341,7 +338,7 @@ __global__ void __launch_bounds__(THIN_WAVES * 64) k_thin_i4(const i4_args p) {
 template <int TYPE, int MI, int WN, int WK, int BUFFERS, int SHIFT>
 __global__ void __launch_bounds__(WN *WK * 64) k_rows_i4(const i4_args p, uint32_t tiles_m, uint32_t tiles_n) {
     constexpr int EL = TYPE == SLZ_F16 ? SLZ_EL_F16 : SLZ_EL_BF16, PIECES = i4_pieces<TYPE>, XB = TYPE == SLZ_F32 ? 4 : 2, NB = 2, AHEAD = 2, THREADS = WN * WK * 64;
-    constexpr uint32_t TM = MI * 16, TN = WN * NB * 16, PITCH = 272, PIECE = TM * PITCH, BLOCK = PIECES * PIECE, BUFFER = WK * BLOCK;
+    constexpr uint32_t TM = MI * 16, TN = WN * NB * 16, HALF = TM * 128, PIECE = 2 * HALF, BLOCK = PIECES * PIECE, BUFFER = WK * BLOCK;
     constexpr int OCTETS = WK * TM * 16 / THREADS;
     static_assert(OCTETS * THREADS == WK * TM * 16, "");
     constexpr uint32_t SUMS = WK * TM * TN * 4, LDS = BUFFERS * BUFFER > SUMS ? BUFFERS * BUFFER : SUMS;
@@ -355,45 +352,42 @@ __global__ void __launch_bounds__(WN *WK * 64) k_rows_i4(const i4_args p, uint32
     const uint32_t eights = blockIdx.x / (8u * tiles_m), in = blockIdx.x % (8u * tiles_m), left = min(8u, tiles_n - eights * 8u);
     const uint32_t n0 = (eights * 8u + in % left) * TN, m0 = in / left * TM;
     const uint32_t blocks = (p.K + I4_BLOCK - 1) / I4_BLOCK, phases = (blocks + WK - 1) / WK, groups = (p.K + (1u << SHIFT) - 1) >> SHIFT;
-    // workgroups begin at different phases: where all read the same columns of x and of rows a power of two apart, a few memory channels have all the work
-    const uint32_t turn = n0 / TN % phases;
-    const auto phase_of = [&](uint32_t number) {
-        const uint32_t i = min(number, phases - 1) + turn;
-        return i < phases ? i : i - phases;
-    };
+    const auto phase_of = [&](uint32_t number) { return min(number, phases - 1); };
     i4_stream<NB> q;
     q.init(p, n0 + wn * (NB * 16), lane);
     v4i32 w[AHEAD][NB];
     // this thread's octets of x: row (the last one again where there are fewer, for sums that no one stores) and column in the phase
     const char *x0 = p.x + (int64_t)m0 * p.ld_x * XB;
     row8<TYPE> x[OCTETS];
-    uint32_t at_x[OCTETS], col_x[OCTETS], to_x[OCTETS];
+    constexpr int PER_BLOCK = TM * 16 > THREADS ? TM * 16 / THREADS : 1, BLOCKS = TM * 16 > THREADS ? 1 : THREADS / (TM * 16);       // of a block in a row, blocks at once
+    const uint32_t row0 = threadIdx.x / 16u % TM, col0 = threadIdx.x / (TM * 16) * I4_BLOCK + threadIdx.x % 16u * 8u;
+    const uint32_t to0 = threadIdx.x / (TM * 16) * BLOCK + threadIdx.x % 16u / 8u * HALF + row0 * 128u + slz_piece_k<0>(row0, threadIdx.x % 8u) * 16u;
+    uint32_t at_x[PER_BLOCK];
 #pragma unroll
-    for (int i = 0; i < OCTETS; i++) {
-        const uint32_t o = threadIdx.x + i * THREADS, row = o / 16u % TM, block = o / (TM * 16);
-        at_x[i] = min(row, p.M - 1 - m0) * (uint32_t)p.ld_x;
-        col_x[i] = block * I4_BLOCK + o % 16u * 8u;
-        to_x[i] = block * BLOCK + row * PITCH + o % 16u * 16u;
-    }
+    for (int i = 0; i < PER_BLOCK; i++) at_x[i] = min(row0 + i * (THREADS / 16), p.M - 1 - m0) * (uint32_t)p.ld_x * XB;
     const auto load_x = [&](uint32_t phase) {
 #pragma unroll
         for (int i = 0; i < OCTETS; i++) {
             // where the row ends inside, its last eight; i4_octet moves them down
-            const v4i32_any *at = (const v4i32_any *)(x0 + (size_t)((at_x[i] + min(col_x[i] + phase * (WK * I4_BLOCK), p.K - 8u)) * XB));
+            const uint32_t c = min(col0 + i / PER_BLOCK * BLOCKS * I4_BLOCK + phase * (WK * I4_BLOCK), p.K - 8u) * XB;
+            const v4i32_any *at = (const v4i32_any *)(x0 + (size_t)(at_x[i % PER_BLOCK] + c));
             x[i].w[0] = at[0];
             if constexpr (TYPE == SLZ_F32) x[i].w[1] = at[1];
         }
     };
     const auto store_x = [&](uint32_t phase, char *to) {
-        const bool inside = (phase + 1) * (WK * I4_BLOCK) <= p.K;
+        const auto all = [&](auto inside) {
 #pragma unroll
-        for (int i = 0; i < OCTETS; i++) {
-            v4i32 o[PIECES];
-            if (inside) i4_octet<TYPE>(x[i], 0, 8, o);
-            else i4_octet<TYPE>(x[i], col_x[i] + phase * (WK * I4_BLOCK), p.K, o);
+            for (int i = 0; i < OCTETS; i++) {
+                v4i32 o[PIECES];
+                if constexpr (decltype(inside)::value) i4_octet<TYPE>(x[i], 0, 8, o);
+                else i4_octet<TYPE>(x[i], col0 + i / PER_BLOCK * BLOCKS * I4_BLOCK + phase * (WK * I4_BLOCK), p.K, o);
 #pragma unroll
-            for (int k = 0; k < PIECES; k++) *(v4i32 *)(to + to_x[i] + k * PIECE) = o[k];
-        }
+                for (int k = 0; k < PIECES; k++) *(v4i32 *)(to + to0 + (i / PER_BLOCK * BLOCKS * BLOCK + i % PER_BLOCK * (THREADS / 16 * 128) + k * PIECE)) = o[k];
+            }
+        };
+        if ((phase + 1) * (WK * I4_BLOCK) <= p.K) all(std::true_type());
+        else all(std::false_type());
     };
     // this thread's scales: rows of weights and groups of the phase, 0 past the rows' ends
     const float *scale0 = p.scale + (int64_t)n0 * p.ld_scale;
@@ -414,14 +408,15 @@ __global__ void __launch_bounds__(WN *WK * 64) k_rows_i4(const i4_args p, uint32
     };
     const auto load_w = [&](uint32_t phase, v4i32 (&to)[NB]) { q.load(min(phase * WK + wk, blocks - 1), to); };
 
+    // in the order of the loop's
     load_x(phase_of(0));
     load_scales(phase_of(0));
-#pragma unroll
-    for (int d = 0; d < AHEAD; d++) load_w(phase_of(d), w[d]);
+    load_w(phase_of(0), w[0]);
     store_x(phase_of(0), lds);
     store_scales(phase_of(0), 0);
     load_x(phase_of(1));
     load_scales(phase_of(1));
+    load_w(phase_of(1), w[1]);
     v4f acc[MI][NB];
 #pragma unroll
     for (int i = 0; i < MI; i++)
@@ -438,8 +433,9 @@ __global__ void __launch_bounds__(WN *WK * 64) k_rows_i4(const i4_args p, uint32
                 store_scales(phase_of(number + 1), 1 - d);
                 load_x(phase_of(number + 2));
                 load_scales(phase_of(number + 2));
+                __builtin_amdgcn_sched_barrier(0);
             }
-            const char *from = lds + (BUFFERS == 2 ? d : 0) * BUFFER + wk * BLOCK + r * PITCH + g * 16u;
+            const char *from = lds + (BUFFERS == 2 ? d : 0) * BUFFER + wk * BLOCK + r * 128u;
             v4f s[NB];
 #pragma unroll
             for (int j = 0; j < NB; j++)
@@ -448,7 +444,7 @@ __global__ void __launch_bounds__(WN *WK * 64) k_rows_i4(const i4_args p, uint32
             // a block past the end is the last one again, times zeros
             i4_block<EL, PIECES, SHIFT>(w[d], s, acc, [&](int step, int i, v4i32 (&o)[PIECES]) {
 #pragma unroll
-                for (int k = 0; k < PIECES; k++) o[k] = *(const v4i32 *)(from + k * PIECE + i * (16 * PITCH) + step * 64);
+                for (int k = 0; k < PIECES; k++) o[k] = *(const v4i32 *)(from + k * PIECE + step / 2 * HALF + i * 2048 + slz_piece_k<0>(r, step % 2 * 4u + g) * 16u);
             });
             load_w(phase_of(number + AHEAD), w[d]);
             __syncthreads();
@@ -476,41 +472,6 @@ __global__ void __launch_bounds__(WN *WK * 64) k_rows_i4(const i4_args p, uint32
         for (int k = 0; k < WK; k++) sum += sums[k * (TM * TN) + i];
         slz_put(p.y, TYPE, (size_t)m * p.ld_y + n, sum);
     }
-}
-
-static size_t thin_bytes(uint32_t m, uint32_t k, uint32_t group, int type, uint32_t nb) {
-    return (size_t)m * thin_pitch(k) * (type == SLZ_F32 ? 3 : 1) + (size_t)thin_scales(i4_groups(k, group)) * 64 * nb;
-}
-static bool thin_takes(const slz_i4_shape *sh) { return sh->m <= 8 && thin_bytes(sh->m, sh->k, sh->group, sh->type, 2) <= THIN_LDS; }
-static bool rows_takes(const slz_i4_shape *sh) { return sh->m <= 256 && sh->k >= 8; }
-template <int TYPE, int SHIFT, int NB> static void thin_launch(const i4_args &p, hipStream_t s) {
-    const size_t x = thin_bytes(p.M, p.K, p.group, TYPE, NB), sums = (size_t)THIN_WAVES * 16 * NB * 16 * 4;
-    hipLaunchKernelGGL((k_thin_i4<TYPE, NB, SHIFT>), dim3((p.N + 16 * NB - 1) / (16 * NB)), dim3(THIN_WAVES * 64), x > sums ? x : sums, s, p);
-}
-template <int TYPE, int SHIFT, int MI, int WN, int WK, int BUFFERS> static void rows_launch(const i4_args &p, hipStream_t s) {
-    const uint32_t tiles_m = (p.M + MI * 16 - 1) / (MI * 16), tiles_n = (p.N + WN * 32 - 1) / (WN * 32);
-    hipLaunchKernelGGL((k_rows_i4<TYPE, MI, WN, WK, BUFFERS, SHIFT>), dim3(tiles_m * tiles_n), dim3(WN * WK * 64), 0, s, p, tiles_m, tiles_n);
-}
-template <int TYPE, int SHIFT> static void few_rows_of(const i4_args &p, bool thin, hipStream_t s) {
-    if (thin) p.N <= 8192 ? thin_launch<TYPE, SHIFT, 1>(p, s) : thin_launch<TYPE, SHIFT, 2>(p, s);
-    else if constexpr (TYPE == SLZ_F32) p.M <= 16 ? rows_launch<TYPE, SHIFT, 1, 2, 4, 1>(p, s) : rows_launch<TYPE, SHIFT, 2, 2, 4, 1>(p, s);
-    else if (p.M <= 16) rows_launch<TYPE, SHIFT, 1, 1, 8, 2>(p, s);
-    else if (p.M <= 32) rows_launch<TYPE, SHIFT, 2, 1, 8, 2>(p, s);
-    else rows_launch<TYPE, SHIFT, 4, 2, 4, 2>(p, s);
-}
-template <int TYPE> static void few_rows(const i4_args &p, bool thin, hipStream_t s) {
-    p.group == 32 ? few_rows_of<TYPE, 5>(p, thin, s) : p.group == 64 ? few_rows_of<TYPE, 6>(p, thin, s) : few_rows_of<TYPE, 7>(p, thin, s);
-}
-static int few_rows_product(const slz_i4_shape *sh, const void *x, const uint8_t *q, const float *scale, void *y, hipStream_t s) {
-    const bool thin = thin_takes(sh);
-    for (uint32_t first = 0, most = 1u << 22; first < sh->n; first += most) {         // threads of a launch stay below 2^32
-        const i4_args p{(const char *)x, (const char *)q + first * sh->ld_q, scale + first * sh->ld_scale, (char *)y + (size_t)first * slz_type_bytes(sh->type),
-                        sh->ld_x, sh->ld_q, sh->ld_scale, sh->ld_y, sh->m, sh->n - first < most ? sh->n - first : most, sh->k, sh->group};
-        if (sh->type == SLZ_F32) few_rows<SLZ_F32>(p, thin, s);
-        else if (sh->type == SLZ_BF16) few_rows<SLZ_BF16>(p, thin, s);
-        else few_rows<SLZ_F16>(p, thin, s);
-    }
-    return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
 }
 
 // ---- values as an operand ------------------------------------------------------------------------------------------------------------
@@ -610,14 +571,43 @@ static int shape_check(const slz_i4_shape *sh) {
 static i4_rows weights_of(const slz_i4_shape *sh, const uint8_t *q, const float *scale) { return {q, sh->ld_q, scale, sh->ld_scale, sh->group, sh->n, sh->k}; }
 static uint32_t pairs_of(int type) { return type == SLZ_F32 ? 6 : 1; }
 
-struct linear_plan { size_t x, ranges, total; slz_choice c; };
+template <int TYPE, int SHIFT, int NB> static void thin_launch(const i4_args &p, hipStream_t s) {
+    const size_t x = i4_thin_bytes(p.M, p.K, p.group, TYPE == SLZ_F32, NB), sums = (size_t)THIN_WAVES * 16 * NB * 16 * 4;
+    hipLaunchKernelGGL((k_thin_i4<TYPE, NB, SHIFT>), dim3((p.N + 16 * NB - 1) / (16 * NB)), dim3(THIN_WAVES * 64), x > sums ? x : sums, s, p);
+}
+template <int TYPE, int SHIFT, int MI, int WN, int WK, int BUFFERS> static void rows_launch(const i4_args &p, hipStream_t s) {
+    const uint32_t tiles_m = (p.M + MI * 16 - 1) / (MI * 16), tiles_n = (p.N + WN * 32 - 1) / (WN * 32);
+    hipLaunchKernelGGL((k_rows_i4<TYPE, MI, WN, WK, BUFFERS, SHIFT>), dim3(tiles_m * tiles_n), dim3(WN * WK * 64), 0, s, p, tiles_m, tiles_n);
+}
+template <int TYPE, int SHIFT> static void stream_of(const i4_args &p, const i4_route &R, hipStream_t s) {
+    if (R.way == i4_route::THIN) p.N <= 8192 ? thin_launch<TYPE, SHIFT, 1>(p, s) : thin_launch<TYPE, SHIFT, 2>(p, s);
+    else if constexpr (TYPE == SLZ_F32) rows_launch<TYPE, SHIFT, 1, 2, 4, 1>(p, s);
+    else if (R.kind == 0) rows_launch<TYPE, SHIFT, 1, 1, 8, 2>(p, s);
+    else if (R.kind == 1) rows_launch<TYPE, SHIFT, 1, 2, 4, 2>(p, s);
+    else if (R.kind == 2) rows_launch<TYPE, SHIFT, 2, 2, 4, 2>(p, s);
+    else rows_launch<TYPE, SHIFT, 4, 2, 4, 2>(p, s);
+}
+template <int TYPE> static void stream_typed(const i4_args &p, const i4_route &R, hipStream_t s) {
+    p.group == 32 ? stream_of<TYPE, 5>(p, R, s) : p.group == 64 ? stream_of<TYPE, 6>(p, R, s) : stream_of<TYPE, 7>(p, R, s);
+}
+static int stream_product(const slz_i4_shape *sh, const i4_route &R, const void *x, const uint8_t *q, const float *scale, void *y, hipStream_t s) {
+    for (uint32_t first = 0; first < sh->n; first += I4_MOST_ROWS) {                      // threads of a launch stay below 2^32
+        const i4_args p{(const char *)x, (const char *)q + first * sh->ld_q, scale + first * sh->ld_scale, (char *)y + (size_t)first * slz_type_bytes(sh->type),
+                        sh->ld_x, sh->ld_q, sh->ld_scale, sh->ld_y, sh->m, sh->n - first < I4_MOST_ROWS ? sh->n - first : I4_MOST_ROWS, sh->k, sh->group};
+        if (sh->type == SLZ_F32) stream_typed<SLZ_F32>(p, R, s);
+        else if (sh->type == SLZ_BF16) stream_typed<SLZ_BF16>(p, R, s);
+        else stream_typed<SLZ_F16>(p, R, s);
+    }
+    return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
+}
+
+struct linear_plan { size_t x, ranges, total; i4_route R; };
 static linear_plan plan_linear(const slz_i4_shape *sh, const void *x) {
     linear_plan P;
-    P.c = slz_choose(sh->m, sh->n, (sh->k + 63) / 64 * pairs_of(sh->type), 1, false, 16);
+    P.R = i4_route_of(sh->m, sh->n, sh->k, sh->type == SLZ_F32, sh->group);
     P.x = values_bytes(sh->type, sh->n, sh->k);
     P.ranges = P.x + slz_operand_bytes(x, sh->type, sh->m, sh->k, sh->ld_x);
-    P.total = P.ranges + slz_ranges_bytes(P.c, sh->m, sh->n);
-    if (thin_takes(sh) || rows_takes(sh)) P.total = 0;
+    P.total = P.R.way == i4_route::TILES && sh->m && sh->n ? P.ranges + slz_ranges_bytes(P.R.c, sh->m, sh->n) : 0;
     return P;
 }
 extern "C" int slz_linear_i4_workspace(const slz_i4_shape *sh, const void *x, size_t *bytes) {
@@ -636,7 +626,7 @@ extern "C" int slz_linear_i4(const slz_i4_shape *sh, const void *x, const uint8_
     const linear_plan P = plan_linear(sh, x);
     if (!slz_ws_ok(ws, ws_bytes, P.total)) return SLZ_E_INVALID_ARG;
     hipStream_t s = (hipStream_t)stream;
-    if (thin_takes(sh) || rows_takes(sh)) return few_rows_product(sh, x, q, scale, y, s);
+    if (P.R.way != i4_route::TILES) return stream_product(sh, P.R, x, q, scale, y, s);
     char *at = (char *)ws;
     slz_layouts jobs = {};
     const slz_operand a = slz_operand_of(x, sh->type, sh->m, sh->k, sh->ld_x, at + P.x, jobs);
@@ -645,8 +635,8 @@ extern "C" int slz_linear_i4(const slz_i4_shape *sh, const void *x, const uint8_
     const slz_operand b = values_operand(weights_of(sh, q, scale), sh->type, at, &unit, s);
     const slz_gemm p = slz_gemm_of(a, b, sh->m, sh->n, sh->k);
     const slz_times_unit f{unit, 1.0f / VALUES_UP};
-    rc = sh->type == SLZ_F16 ? slz_gemm_to<SLZ_EL_F16, false, false>(p, P.c, f, y, sh->type, sh->ld_y, at + P.ranges, s)
-                             : slz_gemm_to<SLZ_EL_BF16, false, false>(p, P.c, f, y, sh->type, sh->ld_y, at + P.ranges, s);
+    rc = sh->type == SLZ_F16 ? slz_gemm_to<SLZ_EL_F16, false, false>(p, P.R.c, f, y, sh->type, sh->ld_y, at + P.ranges, s)
+                             : slz_gemm_to<SLZ_EL_BF16, false, false>(p, P.R.c, f, y, sh->type, sh->ld_y, at + P.ranges, s);
     if (rc != SLZ_OK) return rc;
     SLZ_HIP(hipGetLastError());
     return SLZ_OK;

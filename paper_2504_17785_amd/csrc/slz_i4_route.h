@@ -1,0 +1,51 @@
+// Which kernel takes a product with 4-bit weights (slz_i4.hip); host code that needs no GPU.
+#pragma once
+#include <stddef.h>
+#include "slz_tiling.h"
+#ifndef __HIPCC__
+#define __host__
+#define __device__
+#endif
+
+#define I4_BLOCK 128u                // entries of a block, 64 bytes
+#define I4_THREADS 512u              // of a workgroup that streams weights
+#define I4_MOST_ROWS (1u << 22)      // rows of weights in a launch: threads of a launch stay below 2^32
+#define I4_LDS (128u << 10)          // shared memory for x and scales
+__host__ __device__ static inline uint32_t i4_blocks(uint32_t cols) { return (cols + I4_BLOCK - 1) / I4_BLOCK; }
+__host__ __device__ static inline uint32_t i4_groups(uint32_t cols, uint32_t group) { return (cols + group - 1) / group; }
+// k_thin_i4: bytes of a row of x in shared memory, 16 bytes apart in the banks; floats of a row of scales: odd, and up to three past its end are there
+__host__ __device__ static inline uint32_t i4_pitch(uint32_t k) { return i4_blocks(k) * 256u + 16u; }
+__host__ __device__ static inline uint32_t i4_pitch_scales(uint32_t groups) { return (groups | 3u) + 2u; }
+static inline size_t i4_thin_bytes(uint32_t m, uint32_t k, uint32_t group, bool wide, uint32_t nb) {
+    return (size_t)m * i4_pitch(k) * (wide ? 3 : 1) + (size_t)i4_pitch_scales(i4_groups(k, group)) * 64 * nb;
+}
+
+// THIN: k_thin_i4; ROWS: k_rows_i4 with the tiles `kind`; TILES: the matrix product of the values, tiled as c says.
+// A phase of k_rows_i4 takes 1.15 us with tiles of 16 by 32, 0.9 with 16 by 64, 1.0 with 32 by 64 and 1.75 with 64 by 64, on every compute unit at once (f32: 1.7 with 16 by 64); the
+// matrix product of the values, which are laid out for it at 4.2 TB/s, takes more launches.  Measured and estimated, bf16, 4096 x 4096 with 64, 256, 512, 1024 rows: streamed 10.0, 17.8, 33.5,
+// 68 (10.7, 17.5, 31.5, 59.5), laid out 29, 40, 52, 62 (28, 38, 41, 58); 8192 x 8192 with 512: 111 (116) and 124 (125); f32, 4096 x 8192 with 512: 207 (221) and 246 (236).
+struct i4_kind { uint32_t tm, tn, wk; double us; };                               // wk: blocks of k in a phase
+static const i4_kind I4_KINDS[] = {{16, 32, 8, 1.15}, {16, 64, 4, 0.9}, {32, 64, 4, 1.0}, {64, 64, 4, 1.75}}, I4_KINDS_WIDE[] = {{16, 64, 4, 1.7}};
+struct i4_route { enum { THIN, ROWS, TILES } way; int kind; slz_choice c; };
+// wide: f32
+static inline i4_route i4_route_of(uint32_t m, uint32_t n, uint32_t k, bool wide, uint32_t group) {
+    i4_route R = {i4_route::TILES, 0, slz_choose(m, n, (k + 63) / 64 * (wide ? 6 : 1), 1, false, 16)};
+    // k_thin_i4's time grows with each row, k_rows_i4's not within a tile, and with more than 16384 rows of weights the latter's wider tiles fill the chip (bf16, one row by 32768 x 2048:
+    // 12.7 and 10.2 us; 8192 x 4096: one row 6.9 and 7.7, three 8.1 and 7.9; 4096 x 4096: one 5.5 and 7.2, eight 7.4 and 7.4; f32, four rows by 4096 x 4096 8.8 and 17.4, by 8192 x 4096 16.3 and 18.0)
+    const bool few = m <= 2 ? n <= 16384 : m <= 8 && n <= (wide ? 8192u : 4096u);
+    if ((few || (m <= 8 && k < 8)) && i4_thin_bytes(m, k, group, wide, 2) <= I4_LDS) R.way = i4_route::THIN;
+    else if (k >= 8 && n > 0) {
+        const uint32_t of_launch = n < I4_MOST_ROWS ? n : I4_MOST_ROWS, launches = (n - 1) / of_launch + 1;
+        double least = 8.0 + (double)n * k * (wide ? 6.5 : 2.5) / 4.2e6 + R.c.us;
+        for (int i = 0; i < (wide ? 1 : 4); i++) {
+            const i4_kind &of = wide ? I4_KINDS_WIDE[i] : I4_KINDS[i];
+            const uint64_t tiles = (uint64_t)((m + of.tm - 1) / of.tm) * ((of_launch + of.tn - 1) / of.tn), phases = (i4_blocks(k) + of.wk - 1) / of.wk;
+            const double us = 3.5 + (double)((tiles + 255) / 256 * phases * launches) * of.us;
+            if (us >= least || tiles > 0xffffffffu / I4_THREADS) continue;
+            least = us;
+            R.way = i4_route::ROWS;
+            R.kind = i;
+        }
+    }
+    return R;
+}

@@ -30,7 +30,7 @@ def test_quantize_and_values_refuse():
 def test_products_refuse():
     L = slz.lib()
     need = ctypes.c_size_t(7)
-    ok = dict(m=300, n=8, k=200, type=1, group=64, ld_x=200, ld_q=128, ld_scale=4, ld_y=8)
+    ok = dict(m=5000, n=5000, k=200, type=1, group=64, ld_x=200, ld_q=128, ld_scale=4, ld_y=5000)
 
     def each(code, x=P, q=P, scale=P, y=P, ws=P, size=1 << 40, which="lxw", **kw):
         sh = SlzI4Shape(**{**ok, **kw})
@@ -41,7 +41,7 @@ def test_products_refuse():
         if "w" in which:
             assert L.slz_linear_i4_grad(ref(sh), y, x, q, scale, None, 0, P, 200, ws, size, None) == code
 
-    for kw in (dict(type=5), dict(group=65), dict(y=None), dict(y=P + 1), dict(ld_y=7), dict(ws=None), dict(ws=P + 64), dict(size=64)):
+    for kw in (dict(type=5), dict(group=65), dict(y=None), dict(y=P + 1), dict(ld_y=4999), dict(ws=None), dict(ws=P + 64), dict(size=64)):
         each(INVALID, **kw)
     for kw in (dict(x=None), dict(x=P + 1), dict(ld_x=199)):
         each(INVALID, which="lw", **kw)
@@ -62,6 +62,12 @@ def test_products_refuse():
         assert f(ref(SlzI4Shape(**{**ok, "k": 1 << 31})), *args, ref(need)) == TOO_LARGE
         assert f(ref(sh), *args, ref(need)) == 0 and need.value > 0
     # nothing to compute
+    for kw in (dict(m=0), dict(n=0)):
+        need.value = 7
+        assert L.slz_linear_i4_workspace(ref(SlzI4Shape(**{**ok, **kw})), P, ref(need)) == 0 and need.value == 0
+    for kw in (dict(m=0), dict(n=0), dict(k=0), dict(m=0, n=0, k=0)):
+        assert L.slz_linear_i4_workspace(ref(SlzI4Shape(**{**ok, **kw})), P, ref(need)) == 0
+        assert L.slz_linear_i4_grad_workspace(ref(SlzI4Shape(**{**ok, **kw})), P, P, ref(need)) == 0
     each(0, which="l", m=0, x=None, y=None, ws=None, size=0)
     each(0, which="l", n=0, q=None, scale=None, y=None, ws=None, size=0)
     each(0, which="xw", k=0, x=None, q=None, scale=None, ws=None, size=0)
