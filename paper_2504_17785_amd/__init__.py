@@ -46,6 +46,8 @@ EXPORTS = ("slz_ctx_create", "slz_ctx_destroy", "slz_ctx_set_option", "slz_lut_e
            "slz_bivariate_workspace", "slz_bivariate_lookup", "slz_loss_luts", "slz_loss_workspace", "slz_int_ce_loss_deriv",
            "slz_weight_update_luts", "slz_weight_update",
            "slz_matmul_highres_luts", "slz_matmul_highres_workspace", "slz_matmul_highres",
+           "slz_quantize_i4", "slz_values_i4", "slz_linear_i4_workspace", "slz_linear_i4", "slz_linear_i4_grad_workspace", "slz_linear_i4_grad",
+           "slz_clip_workspace", "slz_grad_norm", "slz_clip_by_norm",
            "slz_quantize_i8", "slz_matmul_i8_workspace", "slz_matmul_i8", "slz_linear_i8_workspace", "slz_linear_i8",
            "slz_matmul_i8_grad_workspace", "slz_matmul_i8_grad", "slz_linear_ce_workspace", "slz_linear_ce",
            "slz_linear_ce_grad_workspace", "slz_linear_ce_grad", "slz_orthogonalize_workspace", "slz_orthogonalize")

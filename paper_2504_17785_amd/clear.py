@@ -85,6 +85,19 @@ def _lib():
     return slz.lib()
 
 
+@functools.lru_cache(maxsize=None)
+def _tensors():
+    """The reader of tensor lists (csrc/slz_tensors.cpp)."""
+    import os
+    from . import build
+    if not os.path.exists(build.TORCH_LIB):
+        build._build_tensors()
+    T = ctypes.PyDLL(build.TORCH_LIB)
+    T.slz_tensors_table.argtypes = [ctypes.py_object, ctypes.py_object, ctypes.c_int, ctypes.c_int, ctypes.c_void_p]
+    T.slz_tensors_written.argtypes = [ctypes.py_object]
+    return T
+
+
 def _check(rc: int, where: str):
     if rc != 0:
         import paper_2504_17785_amd as slz
@@ -358,6 +371,8 @@ def orthogonalize(g, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
 
 def _grad_place(t, what: str, device: int):
     """(rows, cols, row distance) of a tensor of any shape whose elements are one run, or of a matrix."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s: need a tensor, got %s" % (what, type(t).__name__))
     if t.dtype not in _TYPES or t.get_device() != device:
         raise TypeError("%s: need a CUDA tensor of float32, bfloat16 or float16 on device %d, got %s on %s" % (what, device, t.dtype, t.device))
     if t.is_contiguous():
@@ -372,14 +387,13 @@ def _grad_place(t, what: str, device: int):
     return (*t.shape, _matrix(t, what, _TYPES))
 
 
-def _grad_table(grads, out, device: int):
-    flat = []
-    for i, g in enumerate(grads):
+def _grad_table(grads, out, device: int, recording: bool = False):
+    """An array of slz_grad_tensor; recording: autograd is, and would not know of what is written."""
+    table = (SlzGradTensor * len(grads))()
+    if _tensors().slz_tensors_table(grads, out, device, recording, table) == 0:
+        return table
+    for i, (g, o) in enumerate(zip(grads, out)):
         rows, cols, ld = _grad_place(g, "gradient %d" % i, device)
-        if out is None:
-            flat += (g.data_ptr(), 0, rows | cols << 32, ld, ld, _TYPES[g.dtype])
-            continue
-        o = out[i]
         if o is g:
             ld_o = ld
         else:
@@ -389,8 +403,10 @@ def _grad_table(grads, out, device: int):
             if (rows, cols) != (rows_o, cols_o):               # one of them is a run, the other is not
                 rows, cols = g.shape
                 ld, ld_o = _matrix(g, "gradient %d" % i, _TYPES), _matrix(o, "output %d" % i, _TYPES)
-        flat += (g.data_ptr(), o.data_ptr(), rows | cols << 32, ld, ld_o, _TYPES[g.dtype])
-    return (ctypes.c_uint64 * len(flat))(*flat)                # a slz_grad_tensor is six of 64 bits
+        if recording and (g.requires_grad or o.requires_grad):
+            raise RuntimeError("clip_by_norm: autograd has no formula for it; call it on detached tensors or under torch.no_grad()")
+        table[i] = SlzGradTensor(g.data_ptr(), o.data_ptr(), rows, cols, ld, ld_o, _TYPES[g.dtype])
+    return table
 
 
 def _clip_norm(grads, norm):
@@ -407,7 +423,7 @@ def _clip_norm(grads, norm):
 def grad_norm(grads):
     """slz_grad_norm: the norm that all tensors of a list have together, a float32 scalar tensor."""
     grads, norm, device = _clip_norm(grads, None)
-    table, L = _grad_table(grads, None, device), _lib()
+    table, L = _grad_table(grads, grads, device), _lib()
     ws, at, need = _workspace(L.slz_clip_workspace, "slz_clip", norm, table, len(grads))
     _check(L.slz_grad_norm(table, len(grads), norm.data_ptr(), at, need, torch._C._cuda_getCurrentRawStream(device)), "slz_grad_norm")
     return _results("grad_norm", grads, norm) if grads else norm
@@ -420,13 +436,10 @@ def clip_by_norm(grads, max_norm: float, eps: float = 1e-6, norm=None, out=None)
     out = grads if out is None else list(out)
     if len(out) != len(grads):
         raise ValueError("out: %d tensors for %d gradients" % (len(out), len(grads)))
-    if torch.is_grad_enabled():
-        for t in (*grads, *out):
-            if t.requires_grad:
-                raise RuntimeError("clip_by_norm: autograd has no formula for it; call it on detached tensors or under torch.no_grad()")
-    table, L = _grad_table(grads, out, device), _lib()
+    table, L = _grad_table(grads, out, device, torch.is_grad_enabled()), _lib()
     ws, at, need = _workspace(L.slz_clip_workspace, "slz_clip", at_norm, table, len(grads))
     _check(L.slz_clip_by_norm(table, len(grads), max_norm, eps, norm is not None, at_norm.data_ptr(), at, need, torch._C._cuda_getCurrentRawStream(device)),
            "slz_clip_by_norm")
-    torch.autograd.graph.increment_version([t for t in out if not t.is_inference()])
+    if _tensors().slz_tensors_written(out):
+        raise RuntimeError("clip_by_norm: the outputs' versions could not be counted up")
     return at_norm

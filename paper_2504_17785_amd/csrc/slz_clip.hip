@@ -3,6 +3,7 @@
 // The tensors are cut into chunks of as many elements, numbered through all of them.  Workgroup b of G takes the chunks b, b + G, ..., adds up squares in 64 bits
 // and leaves one sum; the second launch adds the sums in their order, so the result is the same bits whatever ran when, and multiplies.
 #include "slz_clear.h"
+#include <algorithm>
 #include <stdlib.h>
 
 #define CLIP_INLINE 64u              // tensors that a launch takes in its arguments
@@ -128,7 +129,8 @@ __global__ void __launch_bounds__(256) k_clip(const T table, const clip_work wor
     } else n = *norm;
     const double limit = (double)n + (double)eps;
     const float f = limit > (double)max_norm ? (float)((double)max_norm / limit) : limit <= (double)max_norm ? 1.0f : __builtin_nanf("");
-    for (uint32_t c = blockIdx.x; c < work.chunks; c += gridDim.x) {
+    for (uint32_t b = blockIdx.x; b < work.chunks; b += gridDim.x) {
+        const uint32_t c = work.chunks - 1u - b;       // from the last one on: what was read last is still in the cache
         const uint32_t i = clip_find(table, work.count, c);
         const clip_desc d = clip_at(table, i);
         if (f == 1.0f && d.g == d.out) continue;
@@ -159,6 +161,28 @@ __global__ void __launch_bounds__(64) k_clip_table(const clip_few few, uint32_t 
     }
 }
 
+// the same of tensors that are runs, from 24 bytes each: the chunks before a tensor are counted here.  1000 tensors: seven launches instead of sixteen
+#define CLIP_RUNS 160u
+struct clip_runs { struct { const char *g; char *out; uint64_t count_type; } run[CLIP_RUNS]; };
+__global__ void __launch_bounds__(256) k_clip_runs(const clip_runs runs, uint32_t begin, uint32_t count, uint32_t before, uint32_t chunk, uint32_t *__restrict__ first, clip_desc *__restrict__ desc) {
+    __shared__ uint32_t sums[4];
+    const uint32_t i = threadIdx.x, lane = i & 63u;
+    const auto r = runs.run[min(i, count - 1)];
+    const uint64_t elements = r.count_type >> 2;
+    const uint32_t mine = i < count ? (uint32_t)((elements + chunk - 1) / chunk) : 0u;
+    uint32_t sum = mine;
+    for (uint32_t o = 1; o < 64; o *= 2) {
+        const uint32_t other = __shfl_up(sum, o);
+        if (lane >= o) sum += other;
+    }
+    if (lane == 63) sums[i >> 6] = sum;
+    __syncthreads();
+    for (uint32_t w = 0; w < i >> 6; w++) before += sums[w];
+    if (i >= count) return;
+    first[begin + i] = before + sum - mine;
+    desc[begin + i] = {r.g, r.out, elements, 0, 0, 0u, (int)(r.count_type & 3u)};
+}
+
 // ---- host ------------------------------------------------------------------------------------------------------------------------------
 static int clip_check(const slz_grad_tensor *t, uint32_t count, bool outputs) {
     if (count > 0 && !t) return SLZ_E_INVALID_ARG;
@@ -184,10 +208,6 @@ static clip_place place_of(const slz_grad_tensor &t, uint32_t i, bool out) {
     if (t.rows == 1 || ld == row) return {p, p + t.rows * row, t.rows * row, 0, i, out ? 1u : 0u};
     return {p, p + (t.rows - 1) * ld + row, row, ld, i, out ? 1u : 0u};
 }
-static int by_begin(const void *a, const void *b) {
-    const uintptr_t x = ((const clip_place *)a)->begin, y = ((const clip_place *)b)->begin;
-    return x < y ? -1 : x > y;
-}
 // a begins at b's begin or before: whether an element belongs to both.  Rows the same distance apart, as of ranges of one matrix's columns, may lie between each other.
 static bool meet(const clip_place &a, const clip_place &b) {
     if (b.begin >= a.end) return false;
@@ -208,7 +228,7 @@ static int clip_overlaps(const slz_grad_tensor *t, uint32_t count) {
         if (t[i].out == t[i].g) rc = t[i].rows > 1 && t[i].ld_out != t[i].ld_g ? SLZ_E_INVALID_ARG : SLZ_OK;
         else p[n++] = place_of(t[i], i, false);
     }
-    qsort(p, n, sizeof(clip_place), by_begin);
+    std::sort(p, p + n, [](const clip_place &a, const clip_place &b) { return a.begin < b.begin; });
     for (size_t i = 0; i < n && rc == SLZ_OK; i++)
         for (size_t j = i + 1; j < n && p[j].begin < p[i].end && rc == SLZ_OK; j++)
             if ((p[i].out || p[j].out) && meet(p[i], p[j])) rc = SLZ_E_INVALID_ARG;
@@ -249,15 +269,33 @@ extern "C" int slz_clip_workspace(const slz_grad_tensor *t, uint32_t count, size
 }
 // the kernels with their table: in their arguments, or in the workspace, filled first
 template <class F> static void with_table(const slz_grad_tensor *t, uint32_t count, const clip_plan &P, bool outputs, char *ws, hipStream_t s, const F &run) {
-    clip_few few;
     uint32_t at = 0, done = 0;
     uint64_t chunk = 0;
     uint32_t *first = (uint32_t *)(ws + P.first);
     clip_desc *desc = (clip_desc *)(ws + P.desc);
+    const auto is_run = [&](const slz_grad_tensor &g) { return g.rows == 1 || (g.ld_g == (int64_t)g.cols && (!outputs || g.ld_out == (int64_t)g.cols)); };
+    bool all = P.tensors > CLIP_INLINE;
+    for (uint32_t i = 0; i < count && all; i++) all = is_run(t[i]) || t[i].rows == 0 || t[i].cols == 0;
+    if (all) {
+        clip_runs runs;
+        for (uint32_t i = 0, before = 0; i < count; i++) {
+            const uint64_t n = (uint64_t)t[i].rows * t[i].cols;
+            if (n == 0) continue;
+            runs.run[at] = {(const char *)t[i].g, (char *)t[i].out, n << 2 | (uint32_t)t[i].type};
+            chunk += (n + P.work.chunk - 1) / P.work.chunk;
+            if (++at < CLIP_RUNS && done + at < P.tensors) continue;
+            hipLaunchKernelGGL(k_clip_runs, dim3(1), dim3(256), 0, s, runs, done, at, before, P.work.chunk, first, desc);
+            before = (uint32_t)chunk;
+            done += at;
+            at = 0;
+        }
+        return run(clip_table{first, desc});
+    }
+    clip_few few;
     for (uint32_t i = 0; i < count; i++) {
         const uint64_t n = (uint64_t)t[i].rows * t[i].cols;
         if (n == 0) continue;
-        const bool run_of = t[i].rows == 1 || (t[i].ld_g == (int64_t)t[i].cols && (!outputs || t[i].ld_out == (int64_t)t[i].cols));
+        const bool run_of = is_run(t[i]);
         few.first[at] = (uint32_t)chunk;
         few.desc[at] = {(const char *)t[i].g, (char *)t[i].out, n, t[i].ld_g, t[i].ld_out, run_of ? 0u : t[i].cols, t[i].type};
         chunk += (n + P.work.chunk - 1) / P.work.chunk;

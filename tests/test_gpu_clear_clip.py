@@ -56,6 +56,8 @@ SHAPES = [
     [(i % 37 + 1, i % 11) for i in range(63)],
     [(i % 37 + 1, 5) for i in range(64)],
     [(i % 37 + 1, 3) for i in range(65)],
+    [(i % 5 + 1, i % 3) for i in range(240)],
+    [(i * 97 % 4000 + 1,) for i in range(161)],
     [(i % 5 + 1,) for i in range(4097)],
     [(3000, 1001), (5,), (4096, 4096), (1,)],
 ]
@@ -86,6 +88,12 @@ def test_clip_of_any_address_and_distance(slz, dtype):  # noqa: F811
     # what lies between them stays
     assert torch.equal(base[9:20, 100:], kept_base[9:20, 100:]) and torch.equal(base[:3, 100:], kept_base[:3, 100:])
     assert flat[0] == kept_flat[0] and flat[2500] == kept_flat[2500] and torch.equal(flat[2502:], kept_flat[2502:])
+    # more of them than a launch takes in its arguments, rows further apart among them
+    many = [randn((7, 5 + i % 3), 10 + i, dtype, slack=i % 4, skip=i % 2) for i in range(150)]
+    kept = [g.clone() for g in many]
+    norm = slz.clip_by_norm(many, 0.5)
+    near(norm, wide_norm(kept))
+    assert all(torch.equal(g, (k.float() * factor(norm.item(), 0.5)).to(dtype)) for g, k in zip(many, kept))
     # from rows further apart into one run, and the other way round
     g = randn((33, 64), 4, dtype, slack=2)
     run, rows = torch.zeros((33, 64), dtype=dtype, device="cuda"), torch.zeros((33, 70), dtype=dtype, device="cuda")
