@@ -148,7 +148,9 @@ __global__ void __launch_bounds__(256) k_clip(const T table, const clip_work wor
                     for (int e = 0; e < 4; e++)
                         o[e] = (int)(slz_half(run_value<TYPE>(w, 2 * e) * f, TYPE) | ((uint32_t)slz_half(run_value<TYPE>(w, 2 * e + 1) * f, TYPE) << 16));
                 }
-                *(v4i32_any *)(d.out + at * (16 / E)) = f == 1.0f ? w : o;
+                // past the caches where the tensors are more than these hold: 1 GiB 593 us, 584 so; 256 MiB 150 and 126
+                if (work.chunk >= 16384u) __builtin_nontemporal_store(f == 1.0f ? w : o, (v4i32_any *)(d.out + at * (16 / E)));
+                else *(v4i32_any *)(d.out + at * (16 / E)) = f == 1.0f ? w : o;
             }, [&](uint64_t, uint64_t to, float x) { slz_put(d.out, TYPE, to, x * f); });
         });
     }

@@ -7,63 +7,117 @@
 
 #define THIN_WAVES (I4_THREADS / 64)
 
-// entries e of a word, in the order of k: a sign and a magnitude
-__device__ __forceinline__ float i4_entry(uint32_t word, int e) {
-    const uint32_t code = word >> (8 * (e & 3) + 4 * (e >> 2));
-    return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, (float)(code & 7u)) | (code & 8u) << 28);
+// four entries of a word (half 0 or 1) in the order of k, times a scale: as bytes they are subnormal e4m3 numbers (i4_operand)
+__device__ __forceinline__ void i4_numbers(uint32_t word, int half, float scale, float *v) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    const uint32_t w = half ? word >> 4 : word, b = (w & 0x07070707u) | (w << 4 & 0x80808080u);
+    const f2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(b, 512.0f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(b, 512.0f, true);
+    v[0] = lo[0] * scale;
+    v[1] = lo[1] * scale;
+    v[2] = hi[0] * scale;
+    v[3] = hi[1] * scale;
 }
 // place of the word with the entries 8 i to 8 i + 7 of a row
 __device__ __forceinline__ uint32_t i4_place(uint32_t i) { return (i & ~15u) + (i & 3u) * 4u + (i >> 2 & 3u); }
 
 // ---- quantisation ------------------------------------------------------------------------------------------------------------------
-// The whole number next to 7 a / top for 0 <= a <= top, ties to even.  A quotient in 32 bits decides wrongly where it is next to a half, and in 16-bit
-// types exact halves are common; so it is compared exactly, 14 a against (2 q - 1) top and (2 q + 1) top: those have 11 + 4 bits for 16-bit types, and
-// 24 + 4 bits for f32, compared in 64.
-template <int TYPE> __device__ __forceinline__ uint32_t i4_nearest(float a, float top, float inv) {
-    using wide = typename std::conditional<TYPE == SLZ_F32, double, float>::type;
-    const float q = fminf(rintf(a * inv), 7.0f);
-    const uint32_t n = (uint32_t)q;
-    const wide at = (wide)a * 14, half = top;
-    wide off;                                          // exact: 14 a and 2 q top are within a factor of 64 of each other where q > 0
-    if constexpr (TYPE == SLZ_F32) off = __builtin_fma(half, (double)(-2.0f * q), at);
-    else off = __builtin_fmaf(half, -2.0f * q, at);
-    const bool odd = n & 1u;
-    const bool up = off > half || (off == half && odd), down = -off > half || (-off == half && odd);
-    return n + (up ? 1u : 0u) - (down ? 1u : 0u);
+// How the kernels that go over whole matrices share them: a wave has 64 words of a row, or 32 or 16 of two or four rows where a row has no more, and as many of the three rows (or twos, or
+// fours) that follow.  In rows further apart 8192 x 8192 took 34.6 us instead of 32.6 (quantisation of bf16) and 91 instead of 83 (f32 values), in runs of 256 words of one row 37 and 83.
+#define I4_DOWN 4u
+struct i4_walk {
+    uint32_t i, row, next, step;     // the lane's word within a row; its first row, those that follow it, and the distance to the next ones
+    __device__ __forceinline__ i4_walk(uint32_t wide) {                            // log2 of the words of a row that a wave has
+        const uint32_t lane = threadIdx.x & 63u, rows = 64u >> wide;
+        i = (blockIdx.x << wide) + (lane & ((1u << wide) - 1u));
+        row = (blockIdx.y * 4u + (threadIdx.x >> 6)) * I4_DOWN * rows + (lane >> wide);
+        next = rows;
+        step = gridDim.y * 4u * I4_DOWN * rows;
+    }
+};
+static inline uint32_t walk_wide(uint32_t words) { return words <= 16 ? 4u : words <= 32 ? 5u : 6u; }
+static inline dim3 walk_grid(uint32_t rows, uint32_t words) {
+    const uint32_t wide = walk_wide(words), x = (words + (1u << wide) - 1) >> wide;
+    const uint64_t of_block = (4u << (6 - wide)) * I4_DOWN, y = (rows + of_block - 1) / of_block, most = 16384u / x ? 16384u / x : 1u;
+    return dim3(x, (unsigned)(y < most ? y : most));
 }
-// A thread makes a word, a group is 4, 8 or 16 lanes.  Bound by memory.
+__device__ __forceinline__ uint32_t i4_max(uint32_t a, uint32_t b) { return a > b ? a : b; }
+template <int CONTROL> __device__ __forceinline__ uint32_t i4_dpp_max(uint32_t x) { return i4_max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CONTROL, 0xf, 0xf, true)); }
+
+// The eight entries of a word.  7 |v| / top, ties to even, exactly: for 16-bit types the quotient is a half exactly or at least 2^-15 from one (14 v - (2 n + 1) top is a whole number of eighths of top's
+// last place, of 2^12 of them at most), so the product with a reciprocal, less than 2^-19 off, is rounded to multiples of 2^-17 by adding 64: halves become exact, nothing else becomes one.  Adding 2^23
+// rounds it to a whole number in the last bits.  For f32 the same in 64 bits: 2^-28, 2^-30 by adding 2^22, and 2^52.
+template <int TYPE> __device__ __forceinline__ uint32_t i4_word(const row8<TYPE> &q, const float (&v)[8], float top) {
+    uint32_t w = 0, sign;
+    if constexpr (TYPE == SLZ_F32) {
+        const double inv = 7.0 / (double)top;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const double s = __builtin_fma((double)fabsf(v[e]), inv, 0x1p22) + 0x1p52;
+            w += ((uint32_t)__builtin_bit_cast(uint64_t, s) & 7u) << (8 * (e & 3) + 4 * (e >> 2));
+        }
+        sign = 0;
+#pragma unroll
+        for (int e = 0; e < 8; e++) sign |= (__builtin_bit_cast(uint32_t, v[e]) >> 31) << (8 * (e & 3) + 4 * (e >> 2) + 3);
+    } else {
+        // moved to where 1 / top is an ordinary number
+        const float up = TYPE == SLZ_F16 ? 1.0f : top < 0x1p-100f ? 0x1p100f : top > 0x1p100f ? 0x1p-100f : 1.0f, inv = 7.0f * __builtin_amdgcn_rcpf(top * up);
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const float s = __builtin_fmaf(fabsf(TYPE == SLZ_BF16 ? v[e] * up : v[e]), inv, 64.0f) + 0x1p23f;
+            w += __builtin_bit_cast(uint32_t, s) << (8 * (e & 3) + 4 * (e >> 2));
+        }
+        // what the numbers of 64 + 2^23 are in 32 bits
+        constexpr uint32_t base = __builtin_bit_cast(uint32_t, 0x1p23f + 64.0f);
+        constexpr uint32_t all = (base << 0) + (base << 8) + (base << 16) + (base << 24) + (base << 4) + (base << 12) + (base << 20) + (base << 28);
+        w -= all;
+        const uint32_t a = __builtin_amdgcn_perm((uint32_t)q.w[0][1], (uint32_t)q.w[0][0], 0x07050301u), b = __builtin_amdgcn_perm((uint32_t)q.w[0][3], (uint32_t)q.w[0][2], 0x07050301u);
+        sign = (a >> 4 & 0x08080808u) | (b & 0x80808080u);
+    }
+    return w | (sign & ((w + 0x77777777u) & 0x88888888u));                         // zeros have none
+}
+// A lane makes a word, a group is 4, 8 or 16 lanes.  Bound by memory: 8192 x 8192 bf16 32.6 us (5.2 TB/s), f32 60 (5.1).
 template <int TYPE>
 __global__ void __launch_bounds__(256)
 k_quantize_i4(const void *__restrict__ w, uint32_t rows, uint32_t cols, int64_t ld_w, uint32_t group, char *__restrict__ q, int64_t ld_q, float *__restrict__ scale,
-              int64_t ld_scale) {
-    const uint32_t per_row = (cols + I4_BLOCK - 1) / I4_BLOCK * 16u;
-    const size_t total = (size_t)rows * per_row;
-    for (size_t g = (size_t)blockIdx.x * 256 + threadIdx.x; g < total; g += (size_t)gridDim.x * 256) {             // a block's 16 lanes together
-        uint32_t i;
-        const size_t r = slz_divide(g, per_row, total <= 0xffffffffu, i);
-        const uint32_t c = i * 8u;
-        float v[8], top = 0.0f;
-        row8_values<TYPE>(row8_load<TYPE>(w, r * ld_w, c, cols), c, cols, v);
+              int64_t ld_scale, uint32_t wide) {
+    const i4_walk at(wide);
+    const uint32_t c = at.i * 8u;
+    if (at.i >= (cols + I4_BLOCK - 1) / I4_BLOCK * 16u) return;                    // a block's 16 lanes together
+    for (uint32_t r0 = at.row; r0 < rows; r0 += at.step) {
+        row8<TYPE> x[I4_DOWN];
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const float a = fabsf(v[e]);
-            top = a < __builtin_inff() ? fmaxf(top, a) : __builtin_inff();
-        }
-        top = slz_dpp_max<0x4e>(slz_dpp_max<0xb1>(top));
-        if (group > 32) top = slz_dpp_max<0x141>(top);
-        if (group > 64) top = slz_dpp_max<0x140>(top);
-        const bool finite = top < __builtin_inff();
-        // held where neither 14 a nor 1 / top leaves 32 bits
-        const float by = top < 0x1p-100f ? 0x1p100f : top > 0x1p100f ? 0x1p-100f : 1.0f, t = top * by, inv = t > 0.0f ? 7.0f / t : 0.0f;
-        uint32_t word = 0;
-        if (finite)
+        for (uint32_t d = 0; d < I4_DOWN; d++) x[d] = row8_load<TYPE>(w, (size_t)min(r0 + d * at.next, rows - 1) * ld_w, c, cols);
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const uint32_t n = t > 0.0f ? i4_nearest<TYPE>(fabsf(v[e]) * by, t, inv) : 0u;
-                word |= (n | (v[e] < 0.0f && n ? 8u : 0u)) << (8 * (e & 3) + 4 * (e >> 2));
+        for (uint32_t d = 0; d < I4_DOWN; d++) {
+            const size_t r = r0 + d * at.next;
+            if (r >= rows) break;
+            float v[8];
+            row8_values<TYPE>(x[d], c, cols, v);
+            if (TYPE != SLZ_F32 && c + 8u > cols)      // as they were moved down
+#pragma unroll
+                for (int i = 0; i < 4; i++) x[d].w[0][i] = (int)(slz_half(v[2 * i], TYPE) | (uint32_t)slz_half(v[2 * i + 1], TYPE) << 16);
+            // magnitudes as whole numbers, so that infinities and NaN are the largest
+            uint32_t m = 0;
+            if constexpr (TYPE == SLZ_F32) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) m = i4_max(m, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
+            } else {
+                typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+                us2 p = {0, 0};
+#pragma unroll
+                for (int i = 0; i < 4; i++) p = __builtin_elementwise_max(p, __builtin_bit_cast(us2, (uint32_t)x[d].w[0][i] & 0x7fff7fffu));
+                m = i4_max(p[0], p[1]);
             }
-        *(uint32_t *)(q + r * ld_q + i4_place(i) * 4u) = word;
-        if ((c & (group - 1u)) == 0 && c < cols) scale[r * ld_scale + c / group] = finite ? top / 7.0f : __builtin_nanf("");
+            m = i4_dpp_max<0x4e>(i4_dpp_max<0xb1>(m));
+            if (group > 32) m = i4_dpp_max<0x141>(m);
+            if (group > 64) m = i4_dpp_max<0x140>(m);
+            const bool finite = m < (TYPE == SLZ_F32 ? 0x7f800000u : TYPE == SLZ_BF16 ? 0x7f80u : 0x7c00u);
+            const float top = TYPE == SLZ_F32 ? __builtin_bit_cast(float, m) : TYPE == SLZ_BF16 ? slz_bf16_to_f32((uint16_t)m) : slz_f16_to_f32((uint16_t)m);
+            const uint32_t word = finite && m ? i4_word<TYPE>(x[d], v, top) : 0u;
+            *(uint32_t *)(q + r * ld_q + i4_place(at.i) * 4u) = word;
+            // top / 7 correctly rounded: it is never within 2^-30 of halfway between two numbers
+            if ((c & (group - 1u)) == 0 && c < cols) scale[r * ld_scale + c / group] = finite ? (float)((double)top * (1.0 / 7.0)) : __builtin_nanf("");
+        }
     }
 }
 
@@ -86,33 +140,42 @@ extern "C" int slz_quantize_i4(const void *w, int type, uint32_t rows, uint32_t 
     if (rc == SLZ_OK) rc = slz_matrix_check(w, rows, cols, ld_w, slz_type_bytes(type));
     if (rc != SLZ_OK || rows == 0 || cols == 0) return rc;
     const auto k = type == SLZ_F32 ? k_quantize_i4<SLZ_F32> : type == SLZ_BF16 ? k_quantize_i4<SLZ_BF16> : k_quantize_i4<SLZ_F16>;
-    hipLaunchKernelGGL(k, ew_grid((size_t)rows * i4_blocks(cols) * 16u), dim3(256), 0, (hipStream_t)stream, w, rows, cols, ld_w, group, (char *)q, ld_q, scale, ld_scale);
+    const uint32_t words = i4_blocks(cols) * 16u;
+    hipLaunchKernelGGL(k, walk_grid(rows, words), dim3(256), 0, (hipStream_t)stream, w, rows, cols, ld_w, group, (char *)q, ld_q, scale, ld_scale, walk_wide(words));
     SLZ_HIP(hipGetLastError());
     return SLZ_OK;
 }
 
 // ---- values ------------------------------------------------------------------------------------------------------------------------
-// Eight values of a row, zeros past its end
-__device__ __forceinline__ void i4_values(const char *q, const float *scale, size_t r, uint32_t i, uint32_t cols, int64_t ld_q, int64_t ld_scale, uint32_t group,
-                                          float (&v)[8]) {
-    const uint32_t c = i * 8u;
-    const uint32_t word = *(const uint32_t *)(q + r * ld_q + i4_place(i) * 4u);
-    const float sc = scale[r * ld_scale + c / group];
-#pragma unroll
-    for (int e = 0; e < 8; e++) v[e] = c + e < cols ? i4_entry(word, e) * sc : 0.0f;
-}
-// Bound by memory.
+// Bound by memory: 8192 x 8192 bf16 29 us (5.8 TB/s), f32 83 (3.6, most of it written).  A lane has 16 bytes of the result: a word's eight entries, or four.
+template <int TYPE>
 __global__ void __launch_bounds__(256)
 k_values_i4(const char *__restrict__ q, int64_t ld_q, const float *__restrict__ scale, int64_t ld_scale, uint32_t group, uint32_t rows, uint32_t cols, char *__restrict__ out,
-            int type, int64_t ld_out, uint32_t aligned) {
-    const uint32_t per_row = (cols + 7u) / 8u;
-    const size_t total = (size_t)rows * per_row;
-    for (size_t g = (size_t)blockIdx.x * 256 + threadIdx.x; g < total; g += (size_t)gridDim.x * 256) {
-        uint32_t i;
-        const size_t r = slz_divide(g, per_row, total <= 0xffffffffu, i);
-        float v[8];
-        i4_values(q, scale, r, i, cols, ld_q, ld_scale, group, v);
-        slz_put_run<8>(out + (r * ld_out + i * 8u) * slz_type_bytes(type), type, v, cols - i * 8u, aligned);
+            int64_t ld_out, uint32_t aligned, uint32_t wide) {
+    constexpr uint32_t E = TYPE == SLZ_F32 ? 4 : 8;
+    const i4_walk at(wide);
+    const uint32_t c = at.i * E;
+    if (c >= cols) return;
+    for (uint32_t r0 = at.row; r0 < rows; r0 += at.step) {
+        uint32_t word[I4_DOWN];
+        float sc[I4_DOWN];
+#pragma unroll
+        for (uint32_t d = 0; d < I4_DOWN; d++) {
+            const size_t r = min(r0 + d * at.next, rows - 1);
+            word[d] = *(const uint32_t *)(q + r * ld_q + i4_place(c / 8u) * 4u);
+            sc[d] = scale[r * ld_scale + c / group];
+        }
+#pragma unroll
+        for (uint32_t d = 0; d < I4_DOWN; d++) {
+            const size_t r = r0 + d * at.next;
+            if (r >= rows) break;
+            float v[E];
+            if constexpr (E == 8) {
+                i4_numbers(word[d], 0, sc[d], v);
+                i4_numbers(word[d], 1, sc[d], v + 4);
+            } else i4_numbers(word[d], c >> 2 & 1, sc[d], v);
+            slz_put_run<E>(out + (r * ld_out + c) * slz_type_bytes(TYPE), TYPE, v, cols - c, aligned);
+        }
     }
 }
 
@@ -122,8 +185,10 @@ extern "C" int slz_values_i4(const uint8_t *q, int64_t ld_q, const float *scale,
     int rc = i4_check(q, ld_q, scale, ld_scale, rows, cols, group);
     if (rc == SLZ_OK) rc = slz_matrix_check(out, rows, cols, ld_out, slz_type_bytes(type));
     if (rc != SLZ_OK || rows == 0 || cols == 0) return rc;
-    hipLaunchKernelGGL(k_values_i4, ew_grid((size_t)rows * ((cols + 7u) / 8u)), dim3(256), 0, (hipStream_t)stream, (const char *)q, ld_q, scale, ld_scale, group, rows, cols,
-                       (char *)out, type, ld_out, slz_in_place(out, 16, ld_out, slz_type_bytes(type)) ? 1u : 0u);
+    const uint32_t words = type == SLZ_F32 ? (cols + 3u) / 4u : (cols + 7u) / 8u;
+    const auto k = type == SLZ_F32 ? k_values_i4<SLZ_F32> : type == SLZ_BF16 ? k_values_i4<SLZ_BF16> : k_values_i4<SLZ_F16>;
+    hipLaunchKernelGGL(k, walk_grid(rows, words), dim3(256), 0, (hipStream_t)stream, (const char *)q, ld_q, scale, ld_scale, group, rows, cols, (char *)out, ld_out,
+                       slz_in_place(out, 16, ld_out, slz_type_bytes(type)) ? 1u : 0u, walk_wide(words));
     SLZ_HIP(hipGetLastError());
     return SLZ_OK;
 }
@@ -519,7 +584,14 @@ k_values_operand(const char *__restrict__ q, int64_t ld_q, const float *__restri
         uint32_t i;
         const size_t r = slz_divide(g, per_row, total <= 0xffffffffu, i);
         float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (i * 8u < cols) i4_values(q, scale, r, i, cols, ld_q, ld_scale, group, v);
+        if (i * 8u < cols) {
+            const uint32_t word = *(const uint32_t *)(q + r * ld_q + i4_place(i) * 4u);
+            const float sc = scale[r * ld_scale + i * 8u / group];
+            i4_numbers(word, 0, sc, v);
+            i4_numbers(word, 1, sc, v + 4);
+#pragma unroll
+            for (uint32_t e = 0; e < 8; e++) v[e] = i * 8u + e < cols ? v[e] : 0.0f;
+        }
         uint16_t t[PIECES][8];
 #pragma unroll
         for (int e = 0; e < 8; e++) {
