@@ -262,37 +262,44 @@ template <int NB> struct i4_stream {
     }
 };
 // Sums of a block's four steps: part collects a group (of 2^SHIFT entries), acc the groups times their scales.  read(step, i, o): x's operands.  A step's operands are read and
-// its entries converted while the matrix instructions of the step before run.
+// its entries converted while the matrix instructions of the step before run; of more than four tiles of x's rows, four at a time, for which the entries are converted once.
 template <int EL, int PIECES, int SHIFT, int MI, int NB, class READ>
 __device__ __forceinline__ void i4_block(const v4i32 (&w)[NB], const v4f (&s)[NB], v4f (&acc)[MI][NB], const READ &read) {
-    constexpr int OF = 1 << (SHIFT - 5);               // steps of a group
-    v4f part[MI][NB];
-    v4i32 o[2][MI][PIECES], b[2][NB];
-    const auto prepare = [&](int step) {
+    constexpr int OF = 1 << (SHIFT - 5), PART = MI < 4 ? MI : 4;                   // steps of a group, tiles at a time
+    constexpr bool KEPT = MI > PART;
+    static_assert(MI % PART == 0, "");
+    v4i32 b[KEPT ? 4 : 2][NB];
 #pragma unroll
-        for (int i = 0; i < MI; i++) read(step, i, o[step & 1][i]);
-        __builtin_amdgcn_sched_barrier(0);
+    for (int first = 0; first < MI; first += PART) {
+        v4f part[PART][NB];
+        v4i32 o[2][PART][PIECES];
+        const auto prepare = [&](int step) {
 #pragma unroll
-        for (int j = 0; j < NB; j++) b[step & 1][j] = i4_operand<EL>((uint32_t)w[j][step]);
-    };
-    prepare(0);
+            for (int i = 0; i < PART; i++) read(step, first + i, o[step & 1][i]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (first == 0)
 #pragma unroll
-    for (int step = 0; step < 4; step++) {
-        if (step < 3) prepare(step + 1);
+                for (int j = 0; j < NB; j++) b[KEPT ? step : step & 1][j] = i4_operand<EL>((uint32_t)w[j][step]);
+        };
+        prepare(0);
 #pragma unroll
-        for (int i = 0; i < MI; i++)
+        for (int step = 0; step < 4; step++) {
+            if (step < 3) prepare(step + 1);
 #pragma unroll
-            for (int k = PIECES - 1; k >= 0; k--)
+            for (int i = 0; i < PART; i++)
 #pragma unroll
-                for (int j = 0; j < NB; j++)
-                    part[i][j] = slz_mma<EL>(o[step & 1][i][k], b[step & 1][j], step % OF == 0 && k == PIECES - 1 ? v4f{0, 0, 0, 0} : part[i][j]);
-        if (step % OF == OF - 1)
+                for (int k = PIECES - 1; k >= 0; k--)
 #pragma unroll
-            for (int i = 0; i < MI; i++)
+                    for (int j = 0; j < NB; j++)
+                        part[i][j] = slz_mma<EL>(o[step & 1][i][k], b[KEPT ? step : step & 1][j], step % OF == 0 && k == PIECES - 1 ? v4f{0, 0, 0, 0} : part[i][j]);
+            if (step % OF == OF - 1)
 #pragma unroll
-                for (int j = 0; j < NB; j++)
+                for (int i = 0; i < PART; i++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) acc[i][j][e] = __builtin_fmaf(part[i][j][e], s[j][step / OF], acc[i][j][e]);
+                    for (int j = 0; j < NB; j++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) acc[first + i][j][e] = __builtin_fmaf(part[i][j][e], s[j][step / OF], acc[first + i][j][e]);
+        }
     }
 }
 
@@ -730,7 +737,8 @@ template <int TYPE, int SHIFT> static void stream_of(const i4_args &p, const i4_
     else if (R.kind == 0) rows_launch<TYPE, SHIFT, 1, 1, 8, 2>(p, s);
     else if (R.kind == 1) rows_launch<TYPE, SHIFT, 1, 2, 4, 2>(p, s);
     else if (R.kind == 2) rows_launch<TYPE, SHIFT, 2, 2, 4, 2>(p, s);
-    else rows_launch<TYPE, SHIFT, 4, 2, 4, 2>(p, s);
+    else if (R.kind == 3) rows_launch<TYPE, SHIFT, 4, 2, 4, 2>(p, s);
+    else rows_launch<TYPE, SHIFT, 8, 4, 2, 2>(p, s);
 }
 template <int TYPE> static void stream_typed(const i4_args &p, const i4_route &R, hipStream_t s) {
     p.group == 32 ? stream_of<TYPE, 5>(p, R, s) : p.group == 64 ? stream_of<TYPE, 6>(p, R, s) : stream_of<TYPE, 7>(p, R, s);

@@ -21,11 +21,12 @@ static inline size_t i4_thin_bytes(uint32_t m, uint32_t k, uint32_t group, bool 
 }
 
 // THIN: k_thin_i4; ROWS: k_rows_i4 with the tiles `kind`; TILES: the matrix product of the values, tiled as c says.
-// A phase of k_rows_i4 takes 1.15 us with tiles of 16 by 32, 0.9 with 16 by 64, 1.0 with 32 by 64 and 1.75 with 64 by 64, on every compute unit at once (f32: 1.7 with 16 by 64); the
-// matrix product of the values, which are laid out for it at 4.2 TB/s, takes more launches.  Measured and estimated, bf16, 4096 x 4096 with 64, 256, 512, 1024 rows: streamed 10.0, 17.8, 33.5,
-// 68 (10.7, 17.5, 31.5, 59.5), laid out 29, 40, 52, 62 (28, 38, 41, 58); 8192 x 8192 with 512: 111 (116) and 124 (125); f32, 4096 x 8192 with 512: 207 (221) and 246 (236).
-struct i4_kind { uint32_t tm, tn, wk; double us; };                               // wk: blocks of k in a phase
-static const i4_kind I4_KINDS[] = {{16, 32, 8, 1.15}, {16, 64, 4, 0.9}, {32, 64, 4, 1.0}, {64, 64, 4, 1.75}}, I4_KINDS_WIDE[] = {{16, 64, 4, 1.7}};
+// A phase of k_rows_i4 takes 1.0 us with tiles of 16 by 32, 0.8 with 16 by 64, 1.0 with 32 by 64, 1.55 with 64 by 64 and 2.0 with 128 by 128, on every compute unit at once, and a tile's beginning
+// and end together 0.6, 0.5, 0.6, 3.2 and 7.5 (f32: 1.6 and 0.4 with 16 by 64); the matrix product of the values, which are laid out for it at 4.2 TB/s, takes more launches.
+// Measured and estimated, bf16, 4096 x 4096 with 64, 256, 512, 1024, 2048 rows: streamed 10.0, 17.8, 36, 44, 85 (12, 19, 35, 43, 83), laid out 29, 38, 52, 62, 75 (28, 38, 41, 58, 74);
+// 8192 x 8192 with 512: 74 (75) and 107 (125); 4096 x 1024 with 1024 and 2048: 19.5, 36 (19, 35) and 28, 33 (20, 25); f32, 8192 x 4096 with 512: 207 (218) and 246 (236).
+struct i4_kind { uint32_t tm, tn, wk; double us, ends; };                         // wk: blocks of k in a phase
+static const i4_kind I4_KINDS[] = {{16, 32, 8, 1.0, 0.6}, {16, 64, 4, 0.8, 0.5}, {32, 64, 4, 1.0, 0.6}, {64, 64, 4, 1.55, 3.2}, {128, 128, 2, 2.0, 7.5}}, I4_KINDS_WIDE[] = {{16, 64, 4, 1.6, 0.4}};
 struct i4_route { enum { THIN, ROWS, TILES } way; int kind; slz_choice c; };
 // wide: f32
 static inline i4_route i4_route_of(uint32_t m, uint32_t n, uint32_t k, bool wide, uint32_t group) {
@@ -37,10 +38,10 @@ static inline i4_route i4_route_of(uint32_t m, uint32_t n, uint32_t k, bool wide
     else if (k >= 8 && n > 0) {
         const uint32_t of_launch = n < I4_MOST_ROWS ? n : I4_MOST_ROWS, launches = (n - 1) / of_launch + 1;
         double least = 8.0 + (double)n * k * (wide ? 6.5 : 2.5) / 4.2e6 + R.c.us;
-        for (int i = 0; i < (wide ? 1 : 4); i++) {
+        for (int i = 0; i < (wide ? 1 : 5); i++) {
             const i4_kind &of = wide ? I4_KINDS_WIDE[i] : I4_KINDS[i];
             const uint64_t tiles = (uint64_t)((m + of.tm - 1) / of.tm) * ((of_launch + of.tn - 1) / of.tn), phases = (i4_blocks(k) + of.wk - 1) / of.wk;
-            const double us = 3.5 + (double)((tiles + 255) / 256 * phases * launches) * of.us;
+            const double us = 3.5 + (double)((tiles + 255) / 256 * launches) * (phases * of.us + of.ends);
             if (us >= least || tiles > 0xffffffffu / I4_THREADS) continue;
             least = us;
             R.way = i4_route::ROWS;

@@ -15,10 +15,13 @@ ROUTES = [
     ((11, 17000, 300, 64), False, ("rows", 1)),
     ((1, 33000, 129, 32), False, ("rows", 1)),
     ((90, 5000, 1100, 32), False, ("rows", 2)),
-    ((200, 3001, 700, 128), False, ("rows", 3)),
+    ((200, 3001, 700, 128), False, ("rows", 2)),
     ((300, 3500, 1290, 64), False, ("rows", 2)),
     ((250, 4090, 2053, 32), False, ("rows", 3)),
     ((70, 16400, 517, 128), False, ("rows", 2)),
+    ((500, 8100, 700, 64), False, ("rows", 4)),
+    ((250, 16001, 2053, 32), False, ("rows", 4)),
+    ((1000, 4001, 1111, 128), False, ("rows", 4)),
     ((9, 5001, 777, 32), True, ("rows", 0)),
     ((100, 1000, 1030, 64), True, ("rows", 0)),
     ((33, 70, 9001, 128), True, ("tiles", 0)),

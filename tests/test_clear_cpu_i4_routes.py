@@ -45,7 +45,7 @@ def route(tmp_path_factory):
 
 def test_shapes_take_their_kernels(route):
     assert {(wide, taken) for _, wide, taken in clear_i4_routes.ROUTES} == {
-        *((False, ("rows", i)) for i in range(4)), (True, ("rows", 0)), *((w, (way, 0)) for w in (False, True) for way in ("thin", "tiles"))}
+        *((False, ("rows", i)) for i in range(5)), (True, ("rows", 0)), *((w, (way, 0)) for w in (False, True) for way in ("thin", "tiles"))}
     for shape, wide, taken in clear_i4_routes.ROUTES:
         assert route(*shape, wide)[0] == taken, (shape, wide)
 
