@@ -250,12 +250,20 @@ def _rows_i4(q, scale, rows, cols, group, like):
     return ld_q, _matrix(scale, "scale", (torch.float32,), q, q.shape[0], (cols + group - 1) // group)
 
 
-_linear_i4_known = {}
+# What has been found out of calls that are alike in all that the checks look at
+_quantize_i4_known, _values_i4_known, _linear_i4_known = {}, {}, {}
+
+
+def _remember(known, alike, what):
+    if len(known) >= 1024:
+        known.clear()
+    known[alike] = what
+    return what
 
 
 @functools.lru_cache(maxsize=1024)
 def _i4_plan(grad: bool, shape, *places):
-    """A call's slz_i4_shape and workspace; places: addresses' last four bits, which is all that the library looks at.  3 of a call's 9.5 us of the host."""
+    """A call's slz_i4_shape and workspace; places: addresses' last four bits, which is all that the library looks at."""
     sh, need = SlzI4Shape(*shape), ctypes.c_size_t(0)
     L = _lib()
     if grad:
@@ -267,36 +275,42 @@ def _i4_plan(grad: bool, shape, *places):
 
 def quantize_i4(w, group: int = 128):
     """slz_quantize_i4: w [rows][cols] -> (4-bit rows, uint8 [rows][64 for every 128 columns], scale float32 [rows][one for every `group` columns])."""
-    ld = _matrix(w, "w", _TYPES)
-    rows, cols = w.shape
-    if group not in (32, 64, 128):
-        raise ValueError("group: %s, need 32, 64 or 128" % (group,))
-    stream = _stream(w)
-    q = torch.empty((rows, (cols + 127) // 128 * 64), dtype=torch.uint8, device=w.device)
-    scale = torch.empty((rows, (cols + group - 1) // group), dtype=torch.float32, device=w.device)
-    _check(_lib().slz_quantize_i4(w.data_ptr(), _TYPES[w.dtype], rows, cols, ld, group, q.data_ptr(), q.shape[1], scale.data_ptr(), scale.shape[1], stream),
-           "slz_quantize_i4")
+    alike = (w.dtype, w.shape, w.stride(), w.get_device(), group)
+    known = _quantize_i4_known.get(alike)
+    if known is None:
+        ld = _matrix(w, "w", _TYPES)
+        rows, cols = w.shape
+        if group not in (32, 64, 128):
+            raise ValueError("group: %s, need 32, 64 or 128" % (group,))
+        known = _remember(_quantize_i4_known, alike, (rows, cols, ld, _TYPES[w.dtype], (cols + 127) // 128 * 64, (cols + group - 1) // group))
+    rows, cols, ld, code, row, groups = known
+    stream, device = _stream(w), w.device
+    q = torch.empty((rows, row), dtype=torch.uint8, device=device)
+    scale = torch.empty((rows, groups), dtype=torch.float32, device=device)
+    _check(_lib().slz_quantize_i4(w.data_ptr(), code, rows, cols, ld, group, q.data_ptr(), row, scale.data_ptr(), groups, stream), "slz_quantize_i4")
     return _results("quantize_i4", (w,), q, scale)
 
 
 def values_i4(q, scale, cols: int, group: int = 128, dtype=torch.bfloat16):
     """slz_values_i4: 4-bit rows of `cols` entries and their scales -> the values [rows][cols] of `dtype`."""
-    if dtype not in _TYPES:
-        raise TypeError("dtype: need float32, bfloat16 or float16, got %s" % dtype)
-    if not 0 <= cols <= 0x7fffffff:
-        raise ValueError("cols: %d" % cols)
-    ld_q, ld_scale = _rows_i4(q, scale, None, cols, group, None)
+    alike = (q.dtype, q.shape, q.stride(), q.get_device(), scale.dtype, scale.shape, scale.stride(), scale.get_device(), cols, group, dtype)
+    known = _values_i4_known.get(alike)
+    if known is None:
+        if dtype not in _TYPES:
+            raise TypeError("dtype: need float32, bfloat16 or float16, got %s" % dtype)
+        if not 0 <= cols <= 0x7fffffff:
+            raise ValueError("cols: %d" % cols)
+        known = _remember(_values_i4_known, alike, (q.shape[0], *_rows_i4(q, scale, None, cols, group, None), _TYPES[dtype]))
+    rows, ld_q, ld_scale, code = known
     stream = _stream(q)
-    out = torch.empty((q.shape[0], cols), dtype=dtype, device=q.device)
-    _check(_lib().slz_values_i4(q.data_ptr(), ld_q, scale.data_ptr(), ld_scale, group, q.shape[0], cols, out.data_ptr(), _TYPES[dtype], max(cols, 1), stream),
-           "slz_values_i4")
+    out = torch.empty((rows, cols), dtype=dtype, device=q.device)
+    _check(_lib().slz_values_i4(q.data_ptr(), ld_q, scale.data_ptr(), ld_scale, group, rows, cols, out.data_ptr(), code, max(cols, 1), stream), "slz_values_i4")
     return _results("values_i4", (scale,), out)
 
 
 def linear_i4(x, q, scale, group: int = 128):
     """slz_linear_i4: x [m][k] times the values of 4-bit rows q [n] with their scales -> y [m][n] of x's type."""
     at_x = x.data_ptr()
-    # what the checks look at: calls that are alike in it are checked once
     alike = (x.dtype, x.shape, x.stride(), x.get_device(), q.dtype, q.shape, q.stride(), q.get_device(), scale.dtype, scale.shape, scale.stride(), scale.get_device(), group, at_x & 15)
     known = _linear_i4_known.get(alike)
     if known is None:
@@ -304,10 +318,7 @@ def linear_i4(x, q, scale, group: int = 128):
         m, k = x.shape
         ld_q, ld_scale = _rows_i4(q, scale, None, k, group, x)
         n = q.shape[0]
-        known = ((m, n), *_i4_plan(False, (m, n, k, _TYPES[x.dtype], group, ld_x, ld_q, ld_scale, max(n, 1)), at_x & 15))
-        if len(_linear_i4_known) >= 1024:
-            _linear_i4_known.clear()
-        _linear_i4_known[alike] = known
+        known = _remember(_linear_i4_known, alike, ((m, n), *_i4_plan(False, (m, n, k, _TYPES[x.dtype], group, ld_x, ld_q, ld_scale, max(n, 1)), at_x & 15)))
     shape, sh, need = known
     stream = _stream(x)
     y = torch.empty(shape, dtype=x.dtype, device=x.device)

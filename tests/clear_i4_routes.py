@@ -7,6 +7,8 @@ ROUTES = [
     ((2, 9001, 1290, 64), False, ("thin", 0)),         # 32 rows of weights a workgroup
     ((8, 4001, 500, 128), False, ("thin", 0)),
     ((3, 100, 9000, 32), False, ("thin", 0)),          # more scales and entries than are under way at once
+    ((8, 500, 6007, 64), False, ("thin", 0)),          # more shared memory than 64 KiB
+    ((2, 300, 9001, 128), True, ("thin", 0)),
     ((5, 700, 1000, 64), True, ("thin", 0)),
     ((2, 8300, 260, 128), True, ("thin", 0)),
     ((13, 1000, 2100, 128), False, ("rows", 0)),

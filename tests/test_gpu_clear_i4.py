@@ -316,6 +316,21 @@ def test_values_of_any_scale(slz, dtype):  # noqa: F811
             inside(torch.where(fits, y, 0), torch.where(fits, want_y, 0), bound, "y of %d" % m)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_small_inputs_are_not_lost(slz, dtype):  # noqa: F811
+    # inputs below the type's smallest ordinary number, times scales that bring the results back
+    n, k, group = 40, 256, 64
+    q, packed, _ = weights(n, k, group, 3)
+    scale = torch.full((n, k // group), 2.0 ** 13 if dtype == torch.float16 else 2.0 ** 120, device="cuda")
+    w = values(q, scale, group)
+    step = 2.0 ** -24 if dtype == torch.float16 else 2.0 ** -133
+    for m in (1, 5, 40, 200):
+        x = (torch.randint(-60, 61, (m, k), device="cuda", generator=torch.Generator(device="cuda").manual_seed(m)).to(WIDE) * step).to(dtype)
+        assert (x != 0).any() and x.abs().max() < torch.finfo(dtype).tiny
+        want = x.to(WIDE) @ w.t()
+        inside(slz.linear_i4(x, packed, scale, group), want, bounds(x.to(WIDE), w, want, dtype, k), "y")
+
+
 # ---- all ----------------------------------------------------------------------------------------------------------------------------
 def calls(slz):  # noqa: F811
     out = []
