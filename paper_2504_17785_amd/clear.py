@@ -251,7 +251,7 @@ def _rows_i4(q, scale, rows, cols, group, like):
 
 
 # What has been found out of calls that are alike in all that the checks look at
-_quantize_i4_known, _values_i4_known, _linear_i4_known = {}, {}, {}
+_quantize_i4_known, _values_i4_known, _linear_i4_known, _linear_i4_grad_known = {}, {}, {}, {}
 
 
 def _remember(known, alike, what):
@@ -261,7 +261,6 @@ def _remember(known, alike, what):
     return what
 
 
-@functools.lru_cache(maxsize=1024)
 def _i4_plan(grad: bool, shape, *places):
     """A call's slz_i4_shape and workspace; places: addresses' last four bits, which is all that the library looks at."""
     sh, need = SlzI4Shape(*shape), ctypes.c_size_t(0)
@@ -330,17 +329,22 @@ def linear_i4(x, q, scale, group: int = 128):
 def linear_i4_grad(dy, x, q, scale, group: int = 128, need_x: bool = True, need_w: bool = True):
     """slz_linear_i4_grad: dy [m][n] and what linear_i4 was called with -> (gradient of x [m][k], of the weights' values [n][k]), of dy's type; None for one
     that is not needed."""
-    ld_y = _matrix(dy, "dy", _TYPES)
-    m, n = dy.shape
-    ld_x = _matrix(x, "x", (dy.dtype,), dy, m)
-    k = x.shape[1]
-    ld_q, ld_scale = _rows_i4(q, scale, n, k, group, dy)
-    stream = _stream(dy)
-    dx = torch.empty((m, k), dtype=dy.dtype, device=dy.device) if need_x else None
-    dw = torch.empty((n, k), dtype=dy.dtype, device=dy.device) if need_w else None
     at_dy, at_x = dy.data_ptr(), x.data_ptr()
-    sh, need = _i4_plan(True, (m, n, k, _TYPES[dy.dtype], group, ld_x, ld_q, ld_scale, ld_y), at_dy & 15, at_x & 15)
-    ws = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None
+    alike = (dy.dtype, dy.shape, dy.stride(), dy.get_device(), x.dtype, x.shape, x.stride(), x.get_device(), q.dtype, q.shape, q.stride(), q.get_device(),
+             scale.dtype, scale.shape, scale.stride(), scale.get_device(), group, at_dy & 15, at_x & 15)
+    known = _linear_i4_grad_known.get(alike)
+    if known is None:
+        ld_y = _matrix(dy, "dy", _TYPES)
+        m, n = dy.shape
+        ld_x = _matrix(x, "x", (dy.dtype,), dy, m)
+        k = x.shape[1]
+        ld_q, ld_scale = _rows_i4(q, scale, n, k, group, dy)
+        known = _remember(_linear_i4_grad_known, alike, (m, n, k, *_i4_plan(True, (m, n, k, _TYPES[dy.dtype], group, ld_x, ld_q, ld_scale, ld_y), at_dy & 15, at_x & 15)))
+    m, n, k, sh, need = known
+    stream, device = _stream(dy), dy.device
+    dx = torch.empty((m, k), dtype=dy.dtype, device=device) if need_x else None
+    dw = torch.empty((n, k), dtype=dy.dtype, device=device) if need_w else None
+    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
     _check(_lib().slz_linear_i4_grad(sh, at_dy, at_x, q.data_ptr(), scale.data_ptr(), dx.data_ptr() if need_x else None, max(k, 1),
                                      dw.data_ptr() if need_w else None, max(k, 1), ws.data_ptr() if need else None, need, stream), "slz_linear_i4_grad")
     return _results("linear_i4_grad", (dy, x, scale), dx, dw)
