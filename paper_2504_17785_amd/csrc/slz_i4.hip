@@ -810,10 +810,11 @@ struct i4_grad_plan { size_t dy, x, values, ranges, total; slz_choice dx, dw; };
 static i4_grad_plan plan_i4_grad(const slz_i4_shape *sh, const void *dy, const void *x) {
     i4_grad_plan P;
     const uint32_t pairs = pairs_of(sh->type);
-    P.dx = slz_choose(sh->m, sh->k, (sh->n + 63) / 64 * pairs, 1, false, 16);
-    // a step with both operands' rows k takes 2.3 to 2.8 times what the choice reckons, which leaves sides as they are and makes ranges worth more: 1555 x 1001 by 777 deep f32 42 us for 63, 2000 x
-    // 500 by 1000 deep 37 for 48
+    // a step with both operands' rows k takes 2.3 to 2.8 times what the choice reckons, which leaves sides as they are and makes ranges worth more: 1555 x 1001 by 777 deep f32 42 us for 63,
+    // 2000 x 500 by 1000 deep 37 for 48
     P.dw = slz_choose(sh->n, sh->k, (sh->m + 63) / 64 * pairs * 5 / 2, 1, false, 16, true);
+    // and one of small tiles twice as long: 777 x 1001 by 1555 deep f16 28.6 us with what lays out for 31.4, 256 x 1024 by 1024 15.9 for 17.5
+    P.dx = slz_choose(sh->m, sh->k, (sh->n + 63) / 64 * pairs * 2, 1, false, 16);
     P.dy = 0;
     P.x = slz_operand_bytes(dy, sh->type, sh->m, sh->n, sh->ld_y);
     P.values = P.x + slz_operand_bytes(x, sh->type, sh->m, sh->k, sh->ld_x);
