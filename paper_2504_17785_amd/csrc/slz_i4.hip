@@ -750,13 +750,10 @@ template <int TYPE> static void stream_typed(const i4_args &p, const i4_route &R
     p.group == 32 ? stream_of<TYPE, 5>(p, R, s) : p.group == 64 ? stream_of<TYPE, 6>(p, R, s) : stream_of<TYPE, 7>(p, R, s);
 }
 static int stream_product(const slz_i4_shape *sh, const i4_route &R, const void *x, const uint8_t *q, const float *scale, void *y, hipStream_t s) {
-    for (uint32_t first = 0; first < sh->n; first += I4_MOST_ROWS) {                      // threads of a launch stay below 2^32
-        const i4_args p{(const char *)x, (const char *)q + first * sh->ld_q, scale + first * sh->ld_scale, (char *)y + (size_t)first * slz_type_bytes(sh->type),
-                        sh->ld_x, sh->ld_q, sh->ld_scale, sh->ld_y, sh->m, sh->n - first < I4_MOST_ROWS ? sh->n - first : I4_MOST_ROWS, sh->k, sh->group};
-        if (sh->type == SLZ_F32) stream_typed<SLZ_F32>(p, R, s);
-        else if (sh->type == SLZ_BF16) stream_typed<SLZ_BF16>(p, R, s);
-        else stream_typed<SLZ_F16>(p, R, s);
-    }
+    const i4_args p{(const char *)x, (const char *)q, scale, (char *)y, sh->ld_x, sh->ld_q, sh->ld_scale, sh->ld_y, sh->m, sh->n, sh->k, sh->group};
+    if (sh->type == SLZ_F32) stream_typed<SLZ_F32>(p, R, s);
+    else if (sh->type == SLZ_BF16) stream_typed<SLZ_BF16>(p, R, s);
+    else stream_typed<SLZ_F16>(p, R, s);
     return hipGetLastError() == hipSuccess ? SLZ_OK : SLZ_E_HIP;
 }
 

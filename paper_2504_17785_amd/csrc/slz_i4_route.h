@@ -9,7 +9,6 @@
 
 #define I4_BLOCK 128u                // entries of a block, 64 bytes
 #define I4_THREADS 512u              // of a workgroup that streams weights
-#define I4_MOST_ROWS (1u << 22)      // rows of weights in a launch: threads of a launch stay below 2^32
 #define I4_LDS (128u << 10)          // shared memory for x and scales
 __host__ __device__ static inline uint32_t i4_blocks(uint32_t cols) { return (cols + I4_BLOCK - 1) / I4_BLOCK; }
 __host__ __device__ static inline uint32_t i4_groups(uint32_t cols, uint32_t group) { return (cols + group - 1) / group; }
@@ -28,7 +27,7 @@ static inline size_t i4_thin_bytes(uint32_t m, uint32_t k, uint32_t group, bool 
 struct i4_kind { uint32_t tm, tn, wk; double us, ends; };                         // wk: blocks of k in a phase
 static const i4_kind I4_KINDS[] = {{16, 32, 8, 1.0, 0.6}, {16, 64, 4, 0.8, 0.5}, {32, 64, 4, 1.0, 0.6}, {64, 64, 4, 1.55, 3.2}, {128, 128, 2, 2.0, 7.5}}, I4_KINDS_WIDE[] = {{16, 64, 4, 1.6, 0.4}};
 struct i4_route { enum { THIN, ROWS, TILES } way; int kind; slz_choice c; };
-// wide: f32
+// wide: f32; n is at most 2^22, the longest row of y
 static inline i4_route i4_route_of(uint32_t m, uint32_t n, uint32_t k, bool wide, uint32_t group) {
     i4_route R = {i4_route::TILES, 0, slz_choose(m, n, (k + 63) / 64 * (wide ? 6 : 1), 1, false, 16)};
     // k_thin_i4's time grows with each row, k_rows_i4's not within a tile, and with more than 16384 rows of weights the latter's wider tiles fill the chip (bf16, one row by 32768 x 2048:
@@ -36,13 +35,12 @@ static inline i4_route i4_route_of(uint32_t m, uint32_t n, uint32_t k, bool wide
     const bool few = m <= 2 ? n <= 16384 : m <= 8 && n <= (wide ? 8192u : 4096u);
     if ((few || (m <= 8 && k < 8)) && i4_thin_bytes(m, k, group, wide, 2) <= I4_LDS) R.way = i4_route::THIN;
     else if (k >= 8 && n > 0) {
-        const uint32_t of_launch = n < I4_MOST_ROWS ? n : I4_MOST_ROWS, launches = (n - 1) / of_launch + 1;
         double least = 8.0 + (double)n * k * (wide ? 6.5 : 2.5) / 4.2e6 + R.c.us;
         for (int i = 0; i < (wide ? 1 : 5); i++) {
             const i4_kind &of = wide ? I4_KINDS_WIDE[i] : I4_KINDS[i];
-            const uint64_t tiles = (uint64_t)((m + of.tm - 1) / of.tm) * ((of_launch + of.tn - 1) / of.tn), phases = (i4_blocks(k) + of.wk - 1) / of.wk;
-            const double us = 3.5 + (double)((tiles + 255) / 256 * launches) * (phases * of.us + of.ends);
-            if (us >= least || tiles > 0xffffffffu / I4_THREADS) continue;
+            const uint64_t tiles = (uint64_t)((m + of.tm - 1) / of.tm) * ((n + of.tn - 1) / of.tn), phases = (i4_blocks(k) + of.wk - 1) / of.wk;
+            const double us = 3.5 + (double)((tiles + 255) / 256) * (phases * of.us + of.ends);
+            if (us >= least || tiles > 0xffffffffu / I4_THREADS) continue;         // threads of a launch stay below 2^32
             least = us;
             R.way = i4_route::ROWS;
             R.kind = i;

@@ -331,6 +331,67 @@ def test_small_inputs_are_not_lost(slz, dtype):  # noqa: F811
         inside(slz.linear_i4(x, packed, scale, group), want, bounds(x.to(WIDE), w, want, dtype, k), "y")
 
 
+def test_the_c_entries_write_between_other_data(slz):  # noqa: F811
+    # rows of everything further apart than they are long, and results at addresses that are no multiples of 16 bytes; what lies between stays
+    import ctypes
+    from paper_2504_17785_amd.clear import SlzI4Shape, _TYPES
+    L = slz.lib()
+    stream = torch.cuda.current_stream().cuda_stream
+    for dtype in TYPES:
+        for m, n, k, group in ((1, 50, 333, 32), (40, 70, 260, 64), (300, 90, 129, 128), (3000, 3200, 72, 64)):
+            e = torch.finfo(dtype).bits // 8
+            w = randn((n, k), 1, dtype, slack=3)
+            blocks, groups = (k + 127) // 128, (k + group - 1) // group
+            q = torch.full((n, blocks * 64 + 48), 0xaa, dtype=torch.uint8, device="cuda")
+            scale = torch.full((n, groups + 2), -5.0, device="cuda")
+            assert L.slz_quantize_i4(w.data_ptr(), _TYPES[dtype], n, k, k + 3, group, q.data_ptr(), q.shape[1], scale.data_ptr(), groups + 2, stream) == 0
+            want_q, want_scale = slz.quantize_i4(w, group)
+            assert torch.equal(q[:, :blocks * 64], want_q) and (q[:, blocks * 64:] == 0xaa).all()
+            assert torch.equal(scale[:, :groups], want_scale) and (scale[:, groups:] == -5).all()
+
+            def room(rows, cols):
+                t = torch.full((rows * (cols + 5) + 1,), 7.0, dtype=dtype, device="cuda")
+                return t, t[1:].view(rows, cols + 5)[:, :cols], t.data_ptr() + e
+
+            whole, values, at = room(n, k)
+            assert L.slz_values_i4(q.data_ptr(), q.shape[1], scale.data_ptr(), groups + 2, group, n, k, at, _TYPES[dtype], k + 5, stream) == 0
+            assert torch.equal(values, slz.values_i4(want_q, want_scale, k, group, dtype))
+            values.fill_(7.0)
+            assert (whole == 7).all()
+            x, dy = randn((m, k), 2, dtype, slack=1), randn((m, n), 3, dtype, slack=2)
+            sh = SlzI4Shape(m, n, k, _TYPES[dtype], group, k + 1, q.shape[1], groups + 2, n + 5)
+            need = ctypes.c_size_t(0)
+            assert L.slz_linear_i4_workspace(ctypes.byref(sh), x.data_ptr(), ctypes.byref(need)) == 0
+            ws = torch.empty(need.value + 256, dtype=torch.uint8, device="cuda")
+            whole, y, at = room(m, n)
+            assert L.slz_linear_i4(ctypes.byref(sh), x.data_ptr(), q.data_ptr(), scale.data_ptr(), at, ws.data_ptr(), need.value, stream) == 0
+            assert torch.equal(y, slz.linear_i4(x, want_q, want_scale, group))
+            y.fill_(7.0)
+            assert (whole == 7).all()
+            sh.ld_y = n + 2
+            assert L.slz_linear_i4_grad_workspace(ctypes.byref(sh), dy.data_ptr(), x.data_ptr(), ctypes.byref(need)) == 0
+            ws = torch.empty(need.value + 256, dtype=torch.uint8, device="cuda")
+            (whole_x, dx, at_x), (whole_w, dw, at_w) = room(m, k), room(n, k)
+            assert L.slz_linear_i4_grad(ctypes.byref(sh), dy.data_ptr(), x.data_ptr(), q.data_ptr(), scale.data_ptr(), at_x, k + 5, at_w, k + 5, ws.data_ptr(), need.value, stream) == 0
+            want_x, want_w = slz.linear_i4_grad(dy, x, want_q, want_scale, group)
+            assert torch.equal(dx, want_x) and torch.equal(dw, want_w)
+            dx.fill_(7.0)
+            dw.fill_(7.0)
+            assert (whole_x == 7).all() and (whole_w == 7).all()
+
+
+def test_more_rows_than_a_launch_of_small_tiles_takes(slz):  # noqa: F811
+    m, n, k, group = (1 << 27) + 5, 4, 8, 32
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((m, k), device="cuda", generator=gen, dtype=torch.bfloat16)
+    q, packed, scale = weights(n, k, group, 2)
+    w = values(q, scale, group)
+    y = slz.linear_i4(x, packed, scale, group)
+    for rows in (slice(0, 1000), slice(m // 2, m // 2 + 1000), slice(m - 1000, m)):
+        want = x[rows].to(WIDE) @ w.t()
+        inside(y[rows], want, bounds(x[rows].to(WIDE), w, want, torch.bfloat16, k), "y")
+
+
 # ---- all ----------------------------------------------------------------------------------------------------------------------------
 def calls(slz):  # noqa: F811
     out = []
