@@ -232,13 +232,25 @@ template <int TYPE> __device__ __forceinline__ void i4_octet(const row8<TYPE> &q
     float v[8];
     row8_values<TYPE>(q, c, cols, v);
     if constexpr (TYPE == SLZ_F32) {
-        uint16_t t[8][3];
+        // the leading 8 bits, the next 8 and the last, of what is left exactly; an infinity is all in the first.  6 instructions an entry
+        uint32_t u[3][8];
+        float top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; i++) slz_split3(v[i], t[i]);
+        for (int i = 0; i < 8; i++) {
+            const float r = v[i] - __int_as_float(__float_as_int(v[i]) & (int)0xffff0000u), l = r - __int_as_float(__float_as_int(r) & (int)0xffff0000u);
+            u[0][i] = __float_as_int(v[i]);
+            u[1][i] = __float_as_int(r);
+            u[2][i] = __float_as_int(l);
+            top = fmaxf(top, fabsf(v[i]));
+        }
+        if (top == INFINITY)
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (fabsf(v[i]) == INFINITY) u[1][i] = u[2][i] = 0;
 #pragma unroll
         for (int k = 0; k < 3; k++)
 #pragma unroll
-            for (int i = 0; i < 4; i++) o[k][i] = (int)(t[2 * i][k] | (uint32_t)t[2 * i + 1][k] << 16);
+            for (int i = 0; i < 4; i++) o[k][i] = (int)__builtin_amdgcn_perm(u[k][2 * i + 1], u[k][2 * i], 0x07060302u);
     } else
 #pragma unroll
         for (int i = 0; i < 4; i++) o[0][i] = (int)(slz_half(v[2 * i], TYPE) | (uint32_t)slz_half(v[2 * i + 1], TYPE) << 16);

@@ -26,7 +26,7 @@ ROUTES = [
     ((1000, 4001, 1111, 128), False, ("rows", 4)),
     ((9, 5001, 777, 32), True, ("rows", 0)),
     ((100, 1000, 1030, 64), True, ("rows", 0)),
-    ((33, 70, 9001, 128), True, ("tiles", 0)),
+    ((33, 70, 9001, 128), True, ("rows", 0)),
     ((3000, 4000, 300, 64), False, ("tiles", 0)),
     ((2500, 3100, 777, 32), False, ("tiles", 0)),
     ((40, 300, 7, 128), False, ("tiles", 0)),

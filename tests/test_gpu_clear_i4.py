@@ -207,6 +207,24 @@ def test_linear_keeps_infinities_and_nan_where_they_belong(slz, dtype, m):  # no
     assert not torch.isfinite(got[m // 2]).any() and torch.equal(got[others], want[others])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m, n, k", [(1, 70, 333), (7, 70, 333), (20, 70, 333), (90, 70, 1333), (2500, 90, 333)])
+def test_linear_of_an_infinity_is_the_formulas(slz, dtype, m, n, k):  # noqa: F811
+    # an infinity times an entry is that infinity, its negative, or NaN for an entry of zero; the other columns of its row and the other rows have no part in it
+    q, packed, scale = weights(n, k, 64, 17, dead=False)
+    x = randn((m, k), 18, dtype)
+    x[m // 2, 40] = float("inf")
+    x[m - 1, k - 1] = float("-inf")
+    got = slz.linear_i4(x, packed, scale, 64).float().cpu().numpy()
+    want = np.zeros((m, n))
+    with np.errstate(invalid="ignore"):
+        want[m // 2] += np.inf * q[:, 40]
+        want[m - 1] += -np.inf * q[:, k - 1]
+    lost = ~np.isfinite(want)
+    np.testing.assert_array_equal(got[lost], want[lost])
+    assert np.isfinite(got[~lost]).all()
+
+
 def test_products_without_elements(slz):  # noqa: F811
     _, q, scale = weights(6, 100, 64, 1)
     for m in (1, 40, 300):
