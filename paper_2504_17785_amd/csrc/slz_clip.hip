@@ -204,12 +204,12 @@ static int clip_check(const slz_grad_tensor *t, uint32_t count, bool outputs) {
     return SLZ_OK;
 }
 // Memory of a matrix: from `begin` to `end`, rows of `row` bytes `step` apart (0: one run)
-struct clip_place { uintptr_t begin, end; uint64_t row, step; uint32_t tensor, out; };
-static clip_place place_of(const slz_grad_tensor &t, uint32_t i, bool out) {
+struct clip_place { uintptr_t begin, end; uint64_t row, step; uint32_t out; };
+static clip_place place_of(const slz_grad_tensor &t, bool out) {
     const uint64_t b = slz_type_bytes(t.type), ld = (uint64_t)(out ? t.ld_out : t.ld_g) * b, row = t.cols * b;
     const uintptr_t p = (uintptr_t)(out ? t.out : t.g);
-    if (t.rows == 1 || ld == row) return {p, p + t.rows * row, t.rows * row, 0, i, out ? 1u : 0u};
-    return {p, p + (t.rows - 1) * ld + row, row, ld, i, out ? 1u : 0u};
+    if (t.rows == 1 || ld == row) return {p, p + t.rows * row, t.rows * row, 0, out ? 1u : 0u};
+    return {p, p + (t.rows - 1) * ld + row, row, ld, out ? 1u : 0u};
 }
 // a begins at b's begin or before: whether an element belongs to both.  Rows the same distance apart, as of ranges of one matrix's columns, may lie between each other.
 static bool meet(const clip_place &a, const clip_place &b) {
@@ -219,17 +219,18 @@ static bool meet(const clip_place &a, const clip_place &b) {
     if (b.step == a.step || (b.step == 0 && b.row <= a.step)) return at < a.row || at + b.row > a.step;
     return true;
 }
-// outputs apart from each other and from other tensors' gradients
-static int clip_overlaps(const slz_grad_tensor *t, uint32_t count) {
-    clip_place *p = (clip_place *)malloc(sizeof(clip_place) * 2 * (size_t)count + 1);
+// outputs apart from each other, from other tensors' gradients and from the norm; the norm from the gradients too where it is written
+static int clip_overlaps(const slz_grad_tensor *t, uint32_t count, const float *norm, bool norm_given) {
+    clip_place *p = (clip_place *)malloc(sizeof(clip_place) * (2 * (size_t)count + 1));
     if (!p) return SLZ_E_NOMEM;
     size_t n = 0;
+    p[n++] = {(uintptr_t)norm, (uintptr_t)norm + 4, 4, 0, norm_given ? 0u : 1u};
     int rc = SLZ_OK;
     for (uint32_t i = 0; i < count && rc == SLZ_OK; i++) {
         if (t[i].rows == 0 || t[i].cols == 0) continue;
-        p[n++] = place_of(t[i], i, true);
+        p[n++] = place_of(t[i], true);
         if (t[i].out == t[i].g) rc = t[i].rows > 1 && t[i].ld_out != t[i].ld_g ? SLZ_E_INVALID_ARG : SLZ_OK;
-        else p[n++] = place_of(t[i], i, false);
+        else p[n++] = place_of(t[i], false);
     }
     std::sort(p, p + n, [](const clip_place &a, const clip_place &b) { return a.begin < b.begin; });
     for (size_t i = 0; i < n && rc == SLZ_OK; i++)
@@ -334,7 +335,7 @@ extern "C" int slz_clip_by_norm(const slz_grad_tensor *t, uint32_t count, float 
     if (!(max_norm >= 0.0f) || !(eps >= 0.0f)) return SLZ_E_INVALID_ARG;
     int rc = clip_check(t, count, true);
     if (rc == SLZ_OK) rc = slz_matrix_check(norm, 1, 1, 1, 4);
-    if (rc == SLZ_OK) rc = clip_overlaps(t, count);
+    if (rc == SLZ_OK) rc = clip_overlaps(t, count, norm, norm_given != 0);
     clip_plan P;
     if (rc == SLZ_OK) rc = clip_plan_of(t, count, P);
     if (rc != SLZ_OK) return rc;

@@ -125,6 +125,16 @@ def test_clip_refuses_outputs_that_overlap(items):
         assert slz.lib().slz_clip_by_norm(tensors(*order), len(order), 1.0, 0.0, 0, P, P, 1 << 40, None) == INVALID
 
 
+def test_clip_refuses_a_norm_inside_the_tensors():
+    clip = slz.lib().slz_clip_by_norm
+    Q = P + 0x1000
+    for given in (0, 1):                                                           # written while others still read it
+        for at in (P, P + 124):
+            assert clip(tensors({}), 1, 1.0, 0.0, given, at, Q, 1 << 40, None) == INVALID
+            assert clip(tensors(dict(g=Q)), 1, 1.0, 0.0, given, at, Q, 1 << 40, None) == INVALID
+    assert clip(tensors(dict(out=Q)), 1, 1.0, 0.0, 0, P + 64, Q, 1 << 40, None) == INVALID
+
+
 def test_binding_refuses_what_is_not_on_the_gpu():
     torch = pytest.importorskip("torch")
     x, q, s = torch.zeros(4, 128), torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(4, 1)
