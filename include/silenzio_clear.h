@@ -96,7 +96,7 @@ typedef struct {
 /* y_ij = sum_k x_ik w_jk with the values w, summed in 32 bits and rounded to the type.  Few rows of x are multiplied by the entries as they are, and each group's sum by its
  * scale; for many (a thousand, about) the values are held in the type first: rounded to 8 bits for bf16 and to 11 for f16 (to fewer where the scale is below 2^-26 of the
  * largest finite one), and carried in 24 for f32.  What of an f32 input lies below 2^-133 is lost.
- * A group's sum is one of 32 bits before its scale brings it down: elements of x up to 2^118 never overflow it, larger ones may.
+ * A group's sum does not overflow before its scale brings it down.  bf16: where entries are multiplied as they are, what of a group's product lies below 2^-139 is lost.
  * An infinity or NaN in x makes its row's results infinite or NaN, a NaN scale its column's. */
 int slz_linear_i4_workspace(const slz_i4_shape *shape, const void *x_dev, size_t *bytes);
 int slz_linear_i4(const slz_i4_shape *shape, const void *x_dev, const uint8_t *q_dev, const float *scale_dev, void *y_dev, void *workspace_dev,

@@ -195,18 +195,18 @@ extern "C" int slz_values_i4(const uint8_t *q, int64_t ld_q, const float *scale,
 
 // ---- few rows ------------------------------------------------------------------------------------------------------------------------
 // The entries of a word as eight numbers of a matrix operand, exact.  As a byte, sign and magnitude in the lowest bits of its fields, an entry is a subnormal e4m3 number, 2^-9 times the
-// entry; the conversion to two bf16 or f16 takes a factor.  10 instructions a word (tables of the numbers' bytes by permutation: 15).
-template <int EL> __device__ __forceinline__ v4i32 i4_operand(uint32_t word) {
+// entry; the conversion to two bf16 or f16 takes a factor `by`, 512 or what i4_by says.  10 instructions a word (tables of the numbers' bytes by permutation: 15).
+template <int EL> __device__ __forceinline__ v4i32 i4_operand(uint32_t word, float by) {
     v4i32 o;
 #pragma unroll
     for (int h = 0; h < 2; h++) {
         const uint32_t b = h ? (word >> 4 & 0x07070707u) | (word & 0x80808080u) : (word & 0x07070707u) | (word << 4 & 0x80808080u);
         if constexpr (EL == SLZ_EL_BF16) {
-            o[2 * h] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, 512.0f, false));
-            o[2 * h + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, 512.0f, true));
+            o[2 * h] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, by, false));
+            o[2 * h + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, by, true));
         } else {
-            o[2 * h] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, 512.0f, false));
-            o[2 * h + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, 512.0f, true));
+            o[2 * h] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, by, false));
+            o[2 * h + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, by, true));
         }
     }
     return o;
@@ -222,6 +222,12 @@ struct i4_args {
     uint32_t M, N, K, group;
 };
 template <int TYPE> constexpr int i4_pieces = TYPE == SLZ_F32 ? 3 : 1;
+// A group's sum is up to 7 * 128 times the largest element of x, which for bf16 and f32 may be more than 32 bits hold.  So their entries are multiplied times 2^-10 (exactly: elements of x
+// are multiples of 2^-133, and 2^-143 is one of 32 bits' numbers), and bf16's results times 2^10 at the end, where sums to multiples of 2^-139 are enough.  f32's are not to lose that, so
+// there each scale is taken times 2^10, and one of 2^100 or more as it is with whole entries: where x is large enough for its group's sum to overflow, its products do too.
+template <int EL, int PIECES> __device__ __forceinline__ float i4_by(float scale) { return EL == SLZ_EL_F16 || (PIECES > 1 && !(fabsf(scale) < 0x1p100f)) ? 512.0f : 0.5f; }
+template <int PIECES> __device__ __forceinline__ float i4_scale(float scale) { return PIECES > 1 && fabsf(scale) < 0x1p100f ? scale * 0x1p10f : scale; }
+template <int TYPE> constexpr float i4_sums_by = TYPE == SLZ_BF16 ? 0x1p10f : 1.0f;
 // Eight entries of a row of x at c as operands, zeros past its end: one, or three that 32-bit numbers are cut into, the large ones first
 template <int TYPE> __device__ __forceinline__ void i4_octet(const row8<TYPE> &q, uint32_t c, uint32_t cols, v4i32 (&o)[i4_pieces<TYPE>]) {
     if constexpr (TYPE != SLZ_F32)
@@ -291,7 +297,7 @@ __device__ __forceinline__ void i4_block(const v4i32 (&w)[NB], const v4f (&s)[NB
             __builtin_amdgcn_sched_barrier(0);
             if (first == 0)
 #pragma unroll
-                for (int j = 0; j < NB; j++) b[KEPT ? step : step & 1][j] = i4_operand<EL>((uint32_t)w[j][step]);
+                for (int j = 0; j < NB; j++) b[KEPT ? step : step & 1][j] = i4_operand<EL>((uint32_t)w[j][step], i4_by<EL, PIECES>(s[j][step / OF]));
         };
         prepare(0);
 #pragma unroll
@@ -310,7 +316,7 @@ __device__ __forceinline__ void i4_block(const v4i32 (&w)[NB], const v4f (&s)[NB
 #pragma unroll
                     for (int j = 0; j < NB; j++)
 #pragma unroll
-                        for (int e = 0; e < 4; e++) acc[first + i][j][e] = __builtin_fmaf(part[i][j][e], s[j][step / OF], acc[first + i][j][e]);
+                        for (int e = 0; e < 4; e++) acc[first + i][j][e] = __builtin_fmaf(part[i][j][e], i4_scale<PIECES>(s[j][step / OF]), acc[first + i][j][e]);
         }
     }
 }
@@ -414,7 +420,7 @@ __global__ void __launch_bounds__(THIN_WAVES * 64) k_thin_i4(const i4_args p) {
         float sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < THIN_WAVES; k++) sum += sums[k * (16 * ROWS) + i];
-        slz_put(p.y, TYPE, (size_t)m * p.ld_y + n, sum);
+        slz_put(p.y, TYPE, (size_t)m * p.ld_y + n, sum * i4_sums_by<TYPE>);
     }
 }
 
@@ -558,7 +564,7 @@ __global__ void __launch_bounds__(WN *WK * 64) k_rows_i4(const i4_args p, uint32
         float sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < WK; k++) sum += sums[k * (TM * TN) + i];
-        slz_put(p.y, TYPE, (size_t)m * p.ld_y + n, sum);
+        slz_put(p.y, TYPE, (size_t)m * p.ld_y + n, sum * i4_sums_by<TYPE>);
     }
 }
 
