@@ -43,7 +43,7 @@ template <int TYPE> __device__ __forceinline__ float run_value(const v4i32 &w, i
         return TYPE == SLZ_BF16 ? slz_bf16_to_f32(h) : slz_f16_to_f32(h);
     }
 }
-// What is done with n elements from `start` on of a tensor: whole runs of 16 bytes, several under way, and single elements
+// What is done with n elements from `start` on of a tensor: whole runs of 16 bytes, several under way, and single elements, of which the places are given
 template <int TYPE, class RUN, class ONE> __device__ __forceinline__ void clip_chunk(const clip_desc &d, uint64_t start, uint32_t n, const RUN &on_run, const ONE &on_one) {
     constexpr uint32_t E = run16<TYPE>::E, AHEAD = 4, B = TYPE == SLZ_F32 ? 4 : 2;
     if (d.cols == 0) {
@@ -58,14 +58,14 @@ template <int TYPE, class RUN, class ONE> __device__ __forceinline__ void clip_c
                 if (r0 + a * 256u < runs) on_run(start + (uint64_t)(r0 + a * 256u) * E, w[a]);
         }
         const uint32_t i = runs * E + threadIdx.x;
-        if (i < n) on_one(start + i, start + i, slz_get(d.g, TYPE, start + i));
+        if (i < n) on_one(start + i, start + i);
         return;
     }
     for (uint32_t i = threadIdx.x; i < n; i += 256u) {
         uint32_t c;
         const size_t r = slz_divide(start + i, d.cols, start + i <= 0xffffffffu, c);
         const size_t from = r * d.ld_g + c;
-        on_one(from, r * d.ld_out + c, slz_get(d.g, TYPE, from));
+        on_one(from, r * d.ld_out + c);
     }
 }
 template <class F> __device__ __forceinline__ void clip_typed(int type, const F &f) {
@@ -100,7 +100,10 @@ template <class T> __global__ void __launch_bounds__(256) k_squares(const T tabl
                     const double v = run_value<TYPE>(w, e);
                     sum[e & 3] = __builtin_fma(v, v, sum[e & 3]);
                 }
-            }, [&](uint64_t, uint64_t, float x) { sum[0] = __builtin_fma((double)x, (double)x, sum[0]); });
+            }, [&](uint64_t at, uint64_t) {
+                const double v = slz_get(d.g, TYPE, at);
+                sum[0] = __builtin_fma(v, v, sum[0]);
+            });
         });
     }
     const double all = clip_sum((sum[0] + sum[1]) + (sum[2] + sum[3]), sums);
@@ -152,7 +155,16 @@ __global__ void __launch_bounds__(256) k_clip(const T table, const clip_work wor
                 // past the caches where the tensors are more than these hold: 1 GiB 593 us, 584 so; 256 MiB 150 and 126
                 if (work.chunk >= 16384u) __builtin_nontemporal_store(f == 1.0f ? w : o, (v4i32_any *)(d.out + at * (16 / E)));
                 else *(v4i32_any *)(d.out + at * (16 / E)) = f == 1.0f ? w : o;
-            }, [&](uint64_t, uint64_t to, float x) { slz_put(d.out, TYPE, to, x * f); });
+            }, [&](uint64_t at, uint64_t to) {
+                // bits in the first place: a product would change a NaN's
+                if constexpr (TYPE == SLZ_F32) {
+                    const uint32_t w = ((const uint32_t *)d.g)[at];
+                    ((uint32_t *)d.out)[to] = f == 1.0f ? w : __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, w) * f);
+                } else {
+                    const uint16_t w = ((const uint16_t *)d.g)[at];
+                    ((uint16_t *)d.out)[to] = f == 1.0f ? w : slz_half((TYPE == SLZ_BF16 ? slz_bf16_to_f32(w) : slz_f16_to_f32(w)) * f, TYPE);
+                }
+            });
         });
     }
 }
