@@ -425,6 +425,9 @@ def _grad_place(t, what: str, device: int):
     return (*t.shape, _matrix(t, what, _TYPES))
 
 
+_NO_FORMULA = "clip_by_norm: autograd has no formula for it; call it on detached tensors or under torch.no_grad()"
+
+
 def _grad_table(grads, out, device: int, recording: bool = False):
     """An array of slz_grad_tensor; recording: autograd is, and would not know of what is written."""
     table = (SlzGradTensor * len(grads))()
@@ -442,7 +445,7 @@ def _grad_table(grads, out, device: int, recording: bool = False):
                 rows, cols = g.shape
                 ld, ld_o = _matrix(g, "gradient %d" % i, _TYPES), _matrix(o, "output %d" % i, _TYPES)
         if recording and (g.requires_grad or o.requires_grad):
-            raise RuntimeError("clip_by_norm: autograd has no formula for it; call it on detached tensors or under torch.no_grad()")
+            raise RuntimeError(_NO_FORMULA)
         table[i] = SlzGradTensor(g.data_ptr(), o.data_ptr(), rows, cols, ld, ld_o, _TYPES[g.dtype])
     return table
 
@@ -474,7 +477,10 @@ def clip_by_norm(grads, max_norm: float, eps: float = 1e-6, norm=None, out=None)
     out = grads if out is None else list(out)
     if len(out) != len(grads):
         raise ValueError("out: %d tensors for %d gradients" % (len(out), len(grads)))
-    table, L = _grad_table(grads, out, device, torch.is_grad_enabled()), _lib()
+    recording = torch.is_grad_enabled()
+    if recording and at_norm.requires_grad:
+        raise RuntimeError(_NO_FORMULA)
+    table, L = _grad_table(grads, out, device, recording), _lib()
     ws, at, need = _workspace(L.slz_clip_workspace, "slz_clip", at_norm, table, len(grads))
     _check(L.slz_clip_by_norm(table, len(grads), max_norm, eps, norm is not None, at_norm.data_ptr(), at, need, torch._C._cuda_getCurrentRawStream(device)),
            "slz_clip_by_norm")
