@@ -3,6 +3,7 @@
 // The tensors are cut into chunks of as many elements, numbered through all of them.  Workgroup b of G takes the chunks b, b + G, ..., adds up squares in 64 bits
 // and leaves one sum; the second launch adds the sums in their order, so the result is the same bits whatever ran when, and multiplies.
 #include "slz_clear.h"
+#include "slz_clip_places.h"
 #include <algorithm>
 #include <stdlib.h>
 
@@ -215,21 +216,11 @@ static int clip_check(const slz_grad_tensor *t, uint32_t count, bool outputs) {
     }
     return SLZ_OK;
 }
-// Memory of a matrix: from `begin` to `end`, rows of `row` bytes `step` apart (0: one run)
-struct clip_place { uintptr_t begin, end; uint64_t row, step; uint32_t out; };
 static clip_place place_of(const slz_grad_tensor &t, bool out) {
     const uint64_t b = slz_type_bytes(t.type), ld = (uint64_t)(out ? t.ld_out : t.ld_g) * b, row = t.cols * b;
     const uintptr_t p = (uintptr_t)(out ? t.out : t.g);
     if (t.rows == 1 || ld == row) return {p, p + t.rows * row, t.rows * row, 0, out ? 1u : 0u};
     return {p, p + (t.rows - 1) * ld + row, row, ld, out ? 1u : 0u};
-}
-// a begins at b's begin or before: whether an element belongs to both.  Rows the same distance apart, as of ranges of one matrix's columns, may lie between each other.
-static bool meet(const clip_place &a, const clip_place &b) {
-    if (b.begin >= a.end) return false;
-    if (a.step == 0) return true;
-    const uint64_t at = (b.begin - a.begin) % a.step;
-    if (b.step == a.step || (b.step == 0 && b.row <= a.step)) return at < a.row || at + b.row > a.step;
-    return true;
 }
 // outputs apart from each other, from other tensors' gradients and from the norm; the norm from the gradients too where it is written
 static int clip_overlaps(const slz_grad_tensor *t, uint32_t count, const float *norm, bool norm_given) {
@@ -247,7 +238,7 @@ static int clip_overlaps(const slz_grad_tensor *t, uint32_t count, const float *
     std::sort(p, p + n, [](const clip_place &a, const clip_place &b) { return a.begin < b.begin; });
     for (size_t i = 0; i < n && rc == SLZ_OK; i++)
         for (size_t j = i + 1; j < n && p[j].begin < p[i].end && rc == SLZ_OK; j++)
-            if ((p[i].out || p[j].out) && meet(p[i], p[j])) rc = SLZ_E_INVALID_ARG;
+            if ((p[i].out || p[j].out) && clip_meet(p[i], p[j])) rc = SLZ_E_INVALID_ARG;
     free(p);
     return rc;
 }
