@@ -1,4 +1,4 @@
-"""Builds libsilenzio_pbs.so (HIP, gfx950 only) in-tree with hipcc, and libsilenzio_torch.so, the binding's reader of tensor lists, with g++."""
+"""Builds libsilenzio_pbs.so (HIP, gfx950 only) in-tree with hipcc, and libsilenzio_torch.*.so, the binding's reader of tensor lists, with g++."""
 from __future__ import annotations
 
 import concurrent.futures
@@ -8,7 +8,6 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsilenzio_pbs.so")
-TORCH_LIB = os.path.join(HERE, "libsilenzio_torch.so")
 SOURCES = ["slz_api.hip", "slz_tables.hip", "slz_generic.hip", "slz_fft.hip", "slz_fft512.hip", "slz_fft1024.hip", "slz_fft2048.hip", "slz_fft2048_team.hip", "slz_fft2048_pair.hip", "slz_fft4096.hip", "slz_fft4096_pair.hip", "slz_fused_n512.hip", "slz_fused_n1024.hip", "slz_bign.hip", "slz_bign_xcd.hip", "slz_keyswitch.hip", "slz_keyswitch_mfma.hip",
            "slz_lincomb_mfma.hip", "slz_matmul_rns.hip", "slz_loss.hip",
            "slz_clear_common.hip", "slz_i8.hip", "slz_i4.hip", "slz_linear_ce.hip", "slz_orthogonalize.hip", "slz_clip.hip"]
@@ -36,18 +35,26 @@ def _compile(src: str) -> str:
     return obj
 
 
+def torch_lib() -> str:
+    """The reader's path: it holds for one torch and one Python, which its name has."""
+    import sys
+    import torch
+    return os.path.join(HERE, "libsilenzio_torch.%s.%s.so" % (torch.__version__.replace("+", "_"), sys.implementation.cache_tag))
+
+
 def _build_tensors() -> None:
     import sysconfig
     import torch
+    lib = torch_lib()
     at = os.path.dirname(torch.__file__)
     include = [os.path.join(at, "include"), os.path.join(at, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"]]
-    tmp = TORCH_LIB + ".tmp%d" % os.getpid()
+    tmp = lib + ".tmp%d" % os.getpid()
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, *("-I" + i for i in include),
            os.path.join(CSRC, "slz_tensors.cpp"), "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", tmp]
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if r.returncode != 0:
         raise RuntimeError("g++ failed for slz_tensors.cpp:\n%s" % r.stdout)
-    os.replace(tmp, TORCH_LIB)
+    os.replace(tmp, lib)
 
 
 def build(verbose: bool = False) -> str:
@@ -59,7 +66,7 @@ def build(verbose: bool = False) -> str:
     subprocess.check_call([_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs])
     os.replace(tmp, LIB)
     if verbose:
-        print("built", LIB, TORCH_LIB)
+        print("built", LIB, torch_lib())
     return LIB
 
 

@@ -90,9 +90,10 @@ def _tensors():
     """The reader of tensor lists (csrc/slz_tensors.cpp)."""
     import os
     from . import build
-    if not os.path.exists(build.TORCH_LIB):
+    lib = build.torch_lib()
+    if not os.path.exists(lib):
         build._build_tensors()
-    T = ctypes.PyDLL(build.TORCH_LIB)
+    T = ctypes.PyDLL(lib)
     T.slz_tensors_table.argtypes = [ctypes.py_object, ctypes.py_object, ctypes.c_int, ctypes.c_int, ctypes.c_void_p]
     T.slz_tensors_written.argtypes = [ctypes.py_object]
     return T

@@ -1,0 +1,24 @@
+"""The binding's reader of tensor lists is built for the torch that is loaded, and the C library without it."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2504_17785_amd import build, clear  # noqa: E402
+
+
+def test_a_reader_built_for_another_torch_is_not_loaded(monkeypatch):
+    asked = []
+
+    def stub():
+        asked.append(torch.__version__)
+        raise RuntimeError("no compiler")
+
+    monkeypatch.setattr(build, "_build_tensors", stub)
+    monkeypatch.setattr(torch, "__version__", "0.0.1+other")
+    clear._tensors.cache_clear()
+    try:
+        with pytest.raises(RuntimeError, match="no compiler"):
+            clear._tensors()
+        assert asked == ["0.0.1+other"]
+    finally:
+        clear._tensors.cache_clear()
