@@ -61,10 +61,10 @@ def build(verbose: bool = False) -> str:
     with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
         tensors = ex.submit(_build_tensors)
         objs = list(ex.map(_compile, SOURCES))
-        tensors.result()
     tmp = LIB + ".tmp%d" % os.getpid()
     subprocess.check_call([_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs])
     os.replace(tmp, LIB)
+    tensors.result()                                   # after the library, which needs neither torch nor Python
     if verbose:
         print("built", LIB, torch_lib())
     return LIB
