@@ -756,8 +756,12 @@ template <int TYPE, int SHIFT, int MI, int WN, int WK, int BUFFERS> static void 
     hipLaunchKernelGGL((k_rows_i4<TYPE, MI, WN, WK, BUFFERS, SHIFT>), dim3(tiles_m * tiles_n), dim3(WN * WK * 64), 0, s, p, tiles_m, tiles_n);
 }
 template <int TYPE, int SHIFT> static void stream_of(const i4_args &p, const i4_route &R, hipStream_t s) {
-    if (R.way == i4_route::THIN) p.N <= 8192 ? thin_launch<TYPE, SHIFT, 1>(p, s) : thin_launch<TYPE, SHIFT, 2>(p, s);
-    else if constexpr (TYPE == SLZ_F32) rows_launch<TYPE, SHIFT, 1, 2, 4, 1>(p, s);
+    if (R.way == i4_route::THIN) {
+        // 16 rows of weights a workgroup.  32 take fewer registers for each but half the workgroups: bf16, one row by 4096, 8192, 16384 x 4096: 5.2, 6.5, 8.9 us and 6.6, 7.4, 9.8.  f32 has
+        // three workgroups of 16 at once on a compute unit, and more than 768 of them begin a second time: two rows by 12288, 16384 x 1024: 6.5, 8.2 us and 7.2, 7.2 with 32.
+        if (TYPE == SLZ_F32 && p.N > 12288) thin_launch<TYPE, SHIFT, TYPE == SLZ_F32 ? 2 : 1>(p, s);
+        else thin_launch<TYPE, SHIFT, 1>(p, s);
+    } else if constexpr (TYPE == SLZ_F32) rows_launch<TYPE, SHIFT, 1, 2, 4, 1>(p, s);
     else if (R.kind == 0) rows_launch<TYPE, SHIFT, 1, 1, 8, 2>(p, s);
     else if (R.kind == 1) rows_launch<TYPE, SHIFT, 1, 2, 4, 2>(p, s);
     else if (R.kind == 2) rows_launch<TYPE, SHIFT, 2, 2, 4, 2>(p, s);
