@@ -94,7 +94,7 @@ typedef struct {
 } slz_i4_shape;
 
 /* y_ij = sum_k x_ik w_jk with the values w, summed in 32 bits and rounded to the type.  Few rows of x are multiplied by the entries as they are, and each group's sum by its
- * scale; for many (a thousand, about) the values are held in the type first: rounded to 8 bits for bf16 and to 11 for f16 (to fewer where the scale is below 2^-26 of the
+ * scale; for many (a thousand, about; from nine on where k is below 8) the values are held in the type first: rounded to 8 bits for bf16 and to 11 for f16 (to fewer where the scale is below 2^-26 of the
  * largest finite one), and carried in 24 for f32.  What of an f32 input lies below 2^-133 is lost.
  * A group's sum does not overflow before its scale brings it down.  bf16: where entries are multiplied as they are, what of a group's product lies below 2^-139 is lost.
  * An infinity or NaN in x makes its row's results infinite or NaN, a NaN scale its column's. */
@@ -105,7 +105,7 @@ int slz_linear_i4(const slz_i4_shape *shape, const void *x_dev, const uint8_t *q
 /* Gradients for dy [m][n] with respect to x and to the values (the rounding of a quantisation is passed straight through):
  *   dx_ik = sum_j dy_ij w_jk,  dw_jk = sum_i dy_ij x_ik.  dx is [m][k], dw [n][k]; either of the two may be null, and then x (without dw) or q and scale (without
  * dx) are not read.  For bf16 and f16 the values are rounded to 8 and 11 bits for dx (f16: to fewer where the scale is below 2^-26 of the largest
- * finite one); for f32 they are carried in 24 bits. */
+ * finite one); for f32 they are carried in 24 bits.  The workspace is that of both gradients. */
 int slz_linear_i4_grad_workspace(const slz_i4_shape *shape, const void *dy_dev, const void *x_dev, size_t *bytes);
 int slz_linear_i4_grad(const slz_i4_shape *shape, const void *dy_dev, const void *x_dev, const uint8_t *q_dev, const float *scale_dev, void *dx_dev,
                        int64_t ld_dx, void *dw_dev, int64_t ld_dw, void *workspace_dev, size_t workspace_bytes, void *hip_stream);

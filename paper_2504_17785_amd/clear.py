@@ -309,7 +309,8 @@ def values_i4(q, scale, cols: int, group: int = 128, dtype=torch.bfloat16):
 
 
 def linear_i4(x, q, scale, group: int = 128):
-    """slz_linear_i4: x [m][k] times the values of 4-bit rows q [n] with their scales -> y [m][n] of x's type."""
+    """slz_linear_i4: x [m][k] times the values of 4-bit rows q [n] with their scales -> y [m][n] of x's type.  For many rows (a thousand, about; nine
+    where k is below 8) of bf16 or f16 the values are rounded to that type first; for few nothing of them is rounded."""
     at_x = x.data_ptr()
     alike = (x.dtype, x.shape, x.stride(), x.get_device(), q.dtype, q.shape, q.stride(), q.get_device(), scale.dtype, scale.shape, scale.stride(), scale.get_device(), group, at_x & 15)
     known = _linear_i4_known.get(alike)
@@ -329,7 +330,7 @@ def linear_i4(x, q, scale, group: int = 128):
 
 def linear_i4_grad(dy, x, q, scale, group: int = 128, need_x: bool = True, need_w: bool = True):
     """slz_linear_i4_grad: dy [m][n] and what linear_i4 was called with -> (gradient of x [m][k], of the weights' values [n][k]), of dy's type; None for one
-    that is not needed."""
+    that is not needed.  For dx the values are rounded to bf16 or f16, if dy is of these."""
     at_dy, at_x = dy.data_ptr(), x.data_ptr()
     alike = (dy.dtype, dy.shape, dy.stride(), dy.get_device(), x.dtype, x.shape, x.stride(), x.get_device(), q.dtype, q.shape, q.stride(), q.get_device(),
              scale.dtype, scale.shape, scale.stride(), scale.get_device(), group, at_dy & 15, at_x & 15)
@@ -473,7 +474,8 @@ def grad_norm(grads):
 
 def clip_by_norm(grads, max_norm: float, eps: float = 1e-6, norm=None, out=None):
     """slz_clip_by_norm: all tensors of a list times max_norm / (their common norm + eps) where that is below 1, in place or into the tensors of `out`.  The norm, a float32
-    scalar tensor, is returned; one that is given is taken in its place (of gradients that are spread over several devices)."""
+    scalar tensor, is returned; one that is given is taken in its place (of gradients that are spread over several devices).  Gradients and outputs are contiguous tensors
+    or matrices with unit stride along their rows; dense tensors in another order, such as a transposed matrix, are refused."""
     grads, at_norm, device = _clip_norm(grads, norm)
     out = grads if out is None else list(out)
     if len(out) != len(grads):

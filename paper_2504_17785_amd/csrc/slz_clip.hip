@@ -26,7 +26,7 @@ __device__ __forceinline__ clip_desc clip_at(const clip_table &t, uint32_t i) { 
 template <class T> __device__ __forceinline__ uint32_t clip_find(const T &t, uint32_t count, uint32_t chunk) {
     uint32_t lo = 0, span = 1;
     const uint32_t lane = threadIdx.x & 63u;
-    while (span < count) span *= 64u;                  // at most 64^6 > 2^32: count is below 2^26
+    while (span < count) span *= 64u;                  // at most 64^5 = 2^30, as count is below 2^26
     while (span > 1) {
         span /= 64u;
         const uint32_t i = lo + lane * span;
@@ -123,7 +123,8 @@ __global__ void __launch_bounds__(256) k_norm(const double *__restrict__ partial
     const float n = clip_norm(partial, count, sums);
     if (threadIdx.x == 0) *norm = n;
 }
-// partial: null where the norm is given.  Every workgroup adds the sums itself: a launch less, and 16 KiB from the cache.  Bound by memory: 1 GiB read and written 397 us (5.4 TB/s).
+// partial: null where the norm is given.  Every workgroup adds the sums itself: a launch less, and 16 KiB from the cache.  Bound by memory: 1 GiB read and
+// written 397 us (5.4 TB/s).
 template <class T>
 __global__ void __launch_bounds__(256) k_clip(const T table, const clip_work work, const double *__restrict__ partial, uint32_t count, float max_norm, float eps, float *__restrict__ norm) {
     __shared__ double sums[4];
@@ -132,6 +133,7 @@ __global__ void __launch_bounds__(256) k_clip(const T table, const clip_work wor
         n = clip_norm(partial, count, sums);
         if (blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
     } else n = *norm;
+    // from the norm as it is given back, rounded to 32 bits: a caller that gives it gets the same bits
     const double limit = (double)n + (double)eps;
     const float f = limit > (double)max_norm ? (float)((double)max_norm / limit) : limit <= (double)max_norm ? 1.0f : __builtin_nanf("");
     for (uint32_t b = blockIdx.x; b < work.chunks; b += gridDim.x) {

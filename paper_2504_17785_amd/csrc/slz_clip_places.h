@@ -5,7 +5,8 @@
 // Memory of a matrix: from `begin` to `end`, rows of `row` bytes `step` apart (0: one run); row <= step, all of it below 2^51 bytes
 struct clip_place { uintptr_t begin, end; uint64_t row, step; uint32_t out; };
 
-// The least t >= 0 with l <= a t mod m <= r, or -1; 0 <= l <= r < m, 0 <= a < m.  Euclid's steps: where no multiple of a lies in the range, a t = m y + (l .. r) asks for m y mod a in (-r .. -l) mod a.
+// The least t >= 0 with l <= a t mod m <= r, or -1; 0 <= l <= r < m, 0 <= a < m.
+// Euclid's steps: where no multiple of a lies in the range, a t = m y + (l .. r) asks for m y mod a in (-r .. -l) mod a.
 static inline __int128 clip_first_in(uint64_t a, uint64_t m, uint64_t l, uint64_t r) {
     if (l == 0) return 0;
     if (a == 0) return -1;

@@ -21,8 +21,9 @@ __device__ __forceinline__ void i4_numbers(uint32_t word, int half, float scale,
 __device__ __forceinline__ uint32_t i4_place(uint32_t i) { return (i & ~15u) + (i & 3u) * 4u + (i >> 2 & 3u); }
 
 // ---- quantisation ------------------------------------------------------------------------------------------------------------------
-// How the kernels that go over whole matrices share them: a wave has 64 words of a row, or 32 or 16 of two or four rows where a row has no more, and as many of the three rows (or twos, or
-// fours) that follow.  In rows further apart 8192 x 8192 took 34.6 us instead of 32.6 (quantisation of bf16) and 91 instead of 83 (f32 values), in runs of 256 words of one row 37 and 83.
+// How the kernels that go over whole matrices share them: a wave has 64 words of a row, or 32 or 16 of two or four rows where a row has no more, and as many
+// of the three rows (or twos, or fours) that follow.  In rows further apart 8192 x 8192 took 34.6 us instead of 32.6 (quantisation of bf16) and 91 instead of
+// 83 (f32 values), in runs of 256 words of one row 37 and 83.
 #define I4_DOWN 4u
 struct i4_walk {
     uint32_t i, row, next, step;     // the lane's word within a row; its first row, those that follow it, and the distance to the next ones
@@ -43,9 +44,10 @@ static inline dim3 walk_grid(uint32_t rows, uint32_t words) {
 __device__ __forceinline__ uint32_t i4_max(uint32_t a, uint32_t b) { return a > b ? a : b; }
 template <int CONTROL> __device__ __forceinline__ uint32_t i4_dpp_max(uint32_t x) { return i4_max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CONTROL, 0xf, 0xf, true)); }
 
-// The eight entries of a word.  7 |v| / top, ties to even, exactly: for 16-bit types the quotient is a half exactly or at least 2^-15 from one (14 v - (2 n + 1) top is a whole number of eighths of top's
-// last place, of 2^12 of them at most), so the product with a reciprocal, less than 2^-19 off, is rounded to multiples of 2^-17 by adding 64: halves become exact, nothing else becomes one.  Adding 2^23
-// rounds it to a whole number in the last bits.  For f32 the same in 64 bits: 2^-28, 2^-30 by adding 2^22, and 2^52.
+// The eight entries of a word.  7 |v| / top, ties to even, exactly: for 16-bit types the quotient is a half exactly or at least 2^-15 from one (14 v - (2 n +
+// 1) top is a whole number of eighths of top's last place, of 2^12 of them at most), so the product with a reciprocal, less than 2^-19 off, is rounded to
+// multiples of 2^-17 by adding 64: halves become exact, nothing else becomes one.  Adding 2^23 rounds it to a whole number in the last bits.  For f32 the same
+// in 64 bits: 2^-28, 2^-30 by adding 2^22, and 2^52.
 template <int TYPE> __device__ __forceinline__ uint32_t i4_word(const row8<TYPE> &q, const float (&v)[8], float top) {
     uint32_t w = 0, sign;
     if constexpr (TYPE == SLZ_F32) {
@@ -194,8 +196,9 @@ extern "C" int slz_values_i4(const uint8_t *q, int64_t ld_q, const float *scale,
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------------------------------
-// The entries of a word as eight numbers of a matrix operand, exact.  As a byte, sign and magnitude in the lowest bits of its fields, an entry is a subnormal e4m3 number, 2^-9 times the
-// entry; the conversion to two bf16 or f16 takes a factor `by`, 512 or what i4_by says.  10 instructions a word (tables of the numbers' bytes by permutation: 15).
+// The entries of a word as eight numbers of a matrix operand, exact.  As a byte, sign and magnitude in the lowest bits of its fields, an entry is a subnormal
+// e4m3 number, 2^-9 times the entry; the conversion to two bf16 or f16 takes a factor `by`, 512 or what i4_by says.  10 instructions a word (tables of the
+// numbers' bytes by permutation: 15).
 template <int EL> __device__ __forceinline__ v4i32 i4_operand(uint32_t word, float by) {
     v4i32 o;
 #pragma unroll
@@ -212,8 +215,8 @@ template <int EL> __device__ __forceinline__ v4i32 i4_operand(uint32_t word, flo
     return o;
 }
 
-// What follows streams the weights past the matrix instructions with the entries as whole numbers; what a group sums up to in 32 bits is multiplied by its scale, so that no value is
-// rounded.  x lies in shared memory as operands.
+// What follows streams the weights past the matrix instructions with the entries as whole numbers; what a group sums up to in 32 bits is multiplied by its
+// scale, so that no value is rounded.  x lies in shared memory as operands.
 struct i4_args {
     const char *x, *q;
     const float *scale;
@@ -222,9 +225,10 @@ struct i4_args {
     uint32_t M, N, K, group;
 };
 template <int TYPE> constexpr int i4_pieces = TYPE == SLZ_F32 ? 3 : 1;
-// A group's sum is up to 7 * 128 times the largest element of x, which for bf16 and f32 may be more than 32 bits hold.  So their entries are multiplied times 2^-10 (exactly: elements of x
-// are multiples of 2^-133, and 2^-143 is one of 32 bits' numbers), and bf16's results times 2^10 at the end, where sums to multiples of 2^-139 are enough.  f32's are not to lose that, so
-// there each scale is taken times 2^10, and one of 2^100 or more as it is with whole entries: where x is large enough for its group's sum to overflow, its products do too.
+// A group's sum is up to 7 * 128 times the largest element of x, which for bf16 and f32 may be more than 32 bits hold.  So their entries are multiplied times
+// 2^-10 (exactly: elements of x are multiples of 2^-133, and 2^-143 is one of 32 bits' numbers), and bf16's results times 2^10 at the end, where sums to
+// multiples of 2^-139 are enough.  f32's are not to lose that, so there each scale is taken times 2^10, and one of 2^100 or more as it is with whole entries:
+// where x is large enough for its group's sum to overflow, its products do too.
 template <int EL, int PIECES> __device__ __forceinline__ float i4_by(float scale) { return EL == SLZ_EL_F16 || (PIECES > 1 && !(fabsf(scale) < 0x1p100f)) ? 512.0f : 0.5f; }
 template <int PIECES> __device__ __forceinline__ float i4_scale(float scale) { return PIECES > 1 && fabsf(scale) < 0x1p100f ? scale * 0x1p10f : scale; }
 template <int TYPE> constexpr float i4_sums_by = TYPE == SLZ_BF16 ? 0x1p10f : 1.0f;
@@ -321,10 +325,12 @@ __device__ __forceinline__ void i4_block(const v4i32 (&w)[NB], const v4f (&s)[NB
     }
 }
 
-// A few rows, all of x and of the scales that a workgroup needs in shared memory.  A workgroup of eight waves has 16 NB rows of weights, each wave an eighth of the blocks of k.
-// Loads return in order, so those of x and the scales go first, then the wave's first blocks, before anything is looked at; the eight waves' sums meet in shared memory.
-// One row by 8192 x 4096 bf16: 6.5 us (launch included; 17.9 MB), by 16384 x 4096 9.9; the waves wait for their loads 64 % of the time.  With x read where it is used by each wave 9.9 and
-// 15.5, with the scales also 12.4 and 16.1.
+// A few rows, all of x and of the scales that a workgroup needs in shared memory.  A workgroup of eight waves has 16 NB rows of weights, each wave an eighth
+// of the blocks of k.
+// Loads return in order, so those of x and the scales go first, then the wave's first blocks, before anything is looked at; the eight waves' sums meet in
+// shared memory.
+// One row by 8192 x 4096 bf16: 6.5 us (launch included; 17.9 MB), by 16384 x 4096 8.9; the waves wait for their loads 64 % of the time.  With x read where it
+// is used by each wave 9.9 and 15.5, with the scales also 12.4 and 16.1.
 #define THIN_SLOTS 2                 // octets of x, and scales, that a thread has under way
 template <int TYPE, int NB, int SHIFT>
 __global__ void __launch_bounds__(THIN_WAVES * 64) k_thin_i4(const i4_args p) {
@@ -424,11 +430,13 @@ __global__ void __launch_bounds__(THIN_WAVES * 64) k_thin_i4(const i4_args p) {
     }
 }
 
-// More rows: a workgroup has 16 MI rows of x and 32 WN of weights.  Its waves are WN by WK: in each phase WK blocks of k of x and the scales that go with them come to shared memory, on
-// the way through registers while the phase before is computed, and a wave multiplies one of the blocks by its 32 rows of weights, whose words come AHEAD phases before.  The WK waves'
-// sums meet in shared memory at the end.  Every phase does all loads (past the end those of the last phase again), so that the compiler can count what is under way.
-// 64 rows by 16384 x 4096 bf16: 17.5 us, 512 by 8192 x 4096 42 (820 TFLOP/s), 512 by 8192 x 8192 75 (917).  Bound by what a compute unit loads, 44 GB/s: without x's loads and stores (in a copy) 13.4 and
-// 33 us, without the products 17.0 and 33, without either 10.8 and 18; x two phases ahead instead of one was no faster.
+// More rows: a workgroup has 16 MI rows of x and 32 WN of weights.  Its waves are WN by WK: in each phase WK blocks of k of x and the scales that go with them
+// come to shared memory, on the way through registers while the phase before is computed, and a wave multiplies one of the blocks by its 32 rows of weights,
+// whose words come AHEAD phases before.  The WK waves' sums meet in shared memory at the end.  Every phase does all loads (past the end those of the last
+// phase again), so that the compiler can count what is under way.
+// 64 rows by 16384 x 4096 bf16: 17.5 us, 512 by 8192 x 4096 42 (820 TFLOP/s), 512 by 8192 x 8192 75 (917).  Bound by what a compute unit loads, 44 GB/s:
+// without x's loads and stores (in a copy) 13.4 and 33 us, without the products 17.0 and 33, without either 10.8 and 18; x two phases ahead instead of one was
+// no faster.
 template <int TYPE, int MI, int WN, int WK, int BUFFERS, int SHIFT>
 __global__ void __launch_bounds__(WN *WK * 64) k_rows_i4(const i4_args p, uint32_t tiles_m, uint32_t tiles_n) {
     constexpr int EL = TYPE == SLZ_F16 ? SLZ_EL_F16 : SLZ_EL_BF16, PIECES = i4_pieces<TYPE>, XB = TYPE == SLZ_F32 ? 4 : 2, NB = 2, AHEAD = 2, THREADS = WN * WK * 64;
@@ -655,8 +663,9 @@ __global__ void __launch_bounds__(256) k_values_operand(const i4_rows w, const i
         }
     }
 }
-// The transpose: out [cols][ld_out], rows of the entries' columns, so that a product that sums over the weights' rows has them in a row too (the tiled product takes 105 us instead of
-// 125 for 4096^3 then).  A workgroup has 128 rows by a block; a thread two rows' entries of a column as one word in shared memory, whose rows are 66 words so that a wave's words meet different banks.
+// The transpose: out [cols][ld_out], rows of the entries' columns, so that a product that sums over the weights' rows has them in a row too (the tiled product
+// takes 105 us instead of 125 for 4096^3 then).  A workgroup has 128 rows by a block; a thread two rows' entries of a column as one word in shared memory,
+// whose rows are 66 words so that a wave's words meet different banks.
 // 4096 x 4096 bf16 9.7 us (4.4 TB/s).
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_values_transposed(const i4_rows w, const i4_unit u, char *__restrict__ out, uint32_t ld_out, int64_t piece) {
@@ -757,8 +766,9 @@ template <int TYPE, int SHIFT, int MI, int WN, int WK, int BUFFERS> static void 
 }
 template <int TYPE, int SHIFT> static void stream_of(const i4_args &p, const i4_route &R, hipStream_t s) {
     if (R.way == i4_route::THIN) {
-        // 16 rows of weights a workgroup.  32 take fewer registers for each but half the workgroups: bf16, one row by 4096, 8192, 16384 x 4096: 5.2, 6.5, 8.9 us and 6.6, 7.4, 9.8.  f32 has
-        // three workgroups of 16 at once on a compute unit, and more than 768 of them begin a second time: two rows by 12288, 16384 x 1024: 6.5, 8.2 us and 7.2, 7.2 with 32.
+        // 16 rows of weights a workgroup.  With 32 there are half of them, each longer: bf16, one row by 4096, 8192, 16384 x 4096: 5.2, 6.5, 8.9
+        // us and 6.6, 7.4, 9.8.  f32 has three workgroups of 16 at once on a compute unit, and more than 768 of them begin a second time: two rows by 12288,
+        // 16384 x 1024: 6.5, 8.2 us and 7.2, 7.2 with 32.
         if (TYPE == SLZ_F32 && p.N > 12288) thin_launch<TYPE, SHIFT, TYPE == SLZ_F32 ? 2 : 1>(p, s);
         else thin_launch<TYPE, SHIFT, 1>(p, s);
     } else if constexpr (TYPE == SLZ_F32) rows_launch<TYPE, SHIFT, 1, 2, 4, 1>(p, s);
@@ -829,8 +839,8 @@ struct i4_grad_plan { size_t dy, x, values, ranges, total; slz_choice dx, dw; };
 static i4_grad_plan plan_i4_grad(const slz_i4_shape *sh, const void *dy, const void *x) {
     i4_grad_plan P;
     const uint32_t pairs = pairs_of(sh->type);
-    // a step with both operands' rows k takes 2.3 to 2.8 times what the choice reckons, which leaves sides as they are and makes ranges worth more: 1555 x 1001 by 777 deep f32 42 us for 63,
-    // 2000 x 500 by 1000 deep 37 for 48
+    // a step with both operands' rows k takes 2.3 to 2.8 times what the choice reckons, which leaves sides as they are and makes ranges worth more: 1555 x
+    // 1001 by 777 deep f32 42 us for 63, 2000 x 500 by 1000 deep 37 for 48
     P.dw = slz_choose(sh->n, sh->k, (sh->m + 63) / 64 * pairs * 5 / 2, 1, false, 16, true);
     // and one of small tiles twice as long: 777 x 1001 by 1555 deep f16 28.6 us with what lays out for 31.4, 256 x 1024 by 1024 15.9 for 17.5
     P.dx = slz_choose(sh->m, sh->k, (sh->n + 63) / 64 * pairs * 2, 1, false, 16);
