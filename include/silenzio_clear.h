@@ -94,8 +94,8 @@ typedef struct {
 } slz_i4_shape;
 
 /* y_ij = sum_k x_ik w_jk with the values w, summed in 32 bits and rounded to the type.  Few rows of x are multiplied by the entries as they are, and each group's sum by its
- * scale; for many (a thousand, about; from nine on where k is below 8) the values are held in the type first: rounded to 8 bits for bf16 and to 11 for f16 (to fewer where the scale is below 2^-26 of the
- * largest finite one), and carried in 24 for f32.  What of an f32 input lies below 2^-133 is lost.
+ * scale; for many (a thousand, about; from nine on where k is below 8) the values are held in the type first: rounded to 8 bits for bf16 and to 11 for f16 (to
+ * fewer where the scale is below 2^-26 of the largest finite one), and carried in 24 for f32.  What of an f32 input lies below 2^-133 is lost.
  * A group's sum does not overflow before its scale brings it down.  bf16: where entries are multiplied as they are, what of a group's product lies below 2^-139 is lost.
  * An infinity or NaN in x makes its row's results infinite or NaN, a NaN scale its column's. */
 int slz_linear_i4_workspace(const slz_i4_shape *shape, const void *x_dev, size_t *bytes);
@@ -171,10 +171,10 @@ typedef struct {
  * rounded to 32-bit floating point.  0 without elements; out, ld_out are not looked at. */
 int slz_clip_workspace(const slz_grad_tensor *tensors, uint32_t count, size_t *bytes);
 int slz_grad_norm(const slz_grad_tensor *tensors, uint32_t count, float *norm_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
-/* out = g f in 32 bits, rounded to the type, with f = 1 where norm + eps <= max_norm, else max_norm / (norm + eps) (in 64 bits, rounded to 32), and NaN where norm is NaN.  The norm is computed as by
- * slz_grad_norm and left in norm_dev, or, with norm_given, taken from there (the norm of more gradients than these).  Where f is 1 the elements keep their bits.
- * SLZ_E_INVALID_ARG also where max_norm or eps is negative or NaN, and where an output overlaps another one, another gradient or norm_dev,
- * or norm_dev, where it is written, a gradient. */
+/* out = g f in 32 bits, rounded to the type, with f = 1 where norm + eps <= max_norm, else max_norm / (norm + eps) (in 64 bits, rounded to 32), and NaN where
+ * norm is NaN.  The norm is computed as by slz_grad_norm and left in norm_dev, or, with norm_given, taken from there (the norm of more gradients than these).
+ * Where f is 1 the elements keep their bits. SLZ_E_INVALID_ARG also where max_norm or eps is negative or NaN, and where an output overlaps another one,
+ * another gradient or norm_dev, or norm_dev, where it is written, a gradient. */
 int slz_clip_by_norm(const slz_grad_tensor *tensors, uint32_t count, float max_norm, float eps, int norm_given, float *norm_dev, void *workspace_dev,
                      size_t workspace_bytes, void *hip_stream);
 
